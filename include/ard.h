@@ -523,6 +523,41 @@ int ard_lstm_tile_bwd(const ard_lstm_tile_desc* desc, const void* W, const void*
                       const void* dcT, void* ws, size_t ws_bytes, void* dX, float* dW, float* dbias, void* dh0,
                       void* dc0, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* Distillation from a teacher's top logits (device).                       */
+/* ------------------------------------------------------------------------ */
+/*
+ * The loss of each column of the logits Zt[V][B] against `top` entries of a
+ * teacher (classes top_idx[top][B], logits top_logits[top][B]) and a label:
+ *   p = softmax of top_logits / T over the column's valid entries,
+ *   q = softmax of Zt / T and q1 = softmax of Zt, both over all V classes,
+ *   loss = a T^2 sum_j p_j (log p_j - log q[top_idx_j]) - (1 - a) log q1[label]
+ * with T = temperature and a = soft_weight. An entry whose class is outside
+ * 0 .. V - 1 is not valid; a column without a valid entry (or whose entries
+ * are all -inf) has no first term, one whose label is outside 0 .. V - 1
+ * (labels NULL: every one) no second term, and one whose logits are all -inf
+ * neither: loss and gradient are then 0 there. Logits of -inf are masked
+ * classes: their gradient is 0, and a teacher's entry of positive weight there
+ * makes the loss +inf. NaN propagates within its column. An entry that names a
+ * class again adds its own share.
+ * fwd: loss[B]; stats[5][B] is kept for the backward.
+ * bwd: dloss[B] (NULL = 1) -> dZt[V][B], not in place.
+ */
+typedef struct {
+  int32_t dtype;       /* of Zt and dZt; everything else is fp32 */
+  int32_t batch;       /* B >= 1 */
+  int32_t classes;     /* V >= 1 */
+  int32_t top;         /* 0 .. 65536 */
+  float temperature;   /* > 0 */
+  float soft_weight;   /* 0 .. 1 */
+} ard_distill_desc;
+
+size_t ard_distill_workspace_bytes(const ard_distill_desc* desc);
+int ard_distill_fwd(const ard_distill_desc* desc, const void* Zt, const int32_t* top_idx, const float* top_logits,
+                    const int32_t* labels, float* loss, float* stats, void* ws, size_t ws_bytes, void* stream);
+int ard_distill_bwd(const ard_distill_desc* desc, const void* Zt, const int32_t* top_idx, const float* top_logits,
+                    const int32_t* labels, const float* stats, const float* dloss, void* dZt, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -66,6 +66,11 @@ class ard_lstm_tile_desc(ctypes.Structure):
                 ("hidden_size", c_i32), ("reserved", c_i32), ("weight_plan", ctypes.POINTER(ard_tile_plan))]
 
 
+class ard_distill_desc(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("batch", c_i32), ("classes", c_i32), ("top", c_i32), ("temperature", c_f32),
+                ("soft_weight", c_f32)]
+
+
 # name -> (restype, argtypes); every symbol the header declares.
 SIGNATURES = {
     "ard_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -124,6 +129,11 @@ SIGNATURES = {
                                     c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
     "ard_lstm_bwd": (ctypes.c_int, [ctypes.POINTER(ard_lstm_desc), c_vp, c_vp, c_vp, c_vp, c_vp,
                                     c_size, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
+    "ard_distill_workspace_bytes": (c_size, [ctypes.POINTER(ard_distill_desc)]),
+    "ard_distill_fwd": (ctypes.c_int, [ctypes.POINTER(ard_distill_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                       c_size, c_vp]),
+    "ard_distill_bwd": (ctypes.c_int, [ctypes.POINTER(ard_distill_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                       c_vp]),
 }
 
 _lib = None

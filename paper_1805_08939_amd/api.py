@@ -14,7 +14,8 @@ from ._ffi import (ARD_ACT_NONE, ARD_ACT_RELU, ARD_BF16, ARD_DROPPED_SKIP, ARD_D
                    ARD_ERR_INVALID_ARG, ARD_ERR_NOT_CONVERGED, ARD_F32, ARD_SEARCH_MIRROR, ARD_SEARCH_PLAIN,
                    ARD_WEIGHTS_COMPACT, ARD_WEIGHTS_COMPACT_GRAD, ARD_WEIGHTS_FULL, ARD_WEIGHTS_INPUT_MAJOR,
                    ard_fc_desc, ard_lstm_desc, ard_lstm_tile_desc, ard_row_plan, ard_search_info, ard_search_opts,
-                   ard_tile_desc, ard_tile_plan)
+                   ard_tile_desc, ard_tile_plan,
+                   ard_distill_desc)
 
 
 class ArdError(RuntimeError):
@@ -342,3 +343,25 @@ def ard_lstm_tile_bwd(desc, W, dHs, dhT, dcT, ws, dX, dW, dbias, dh0, dc0, strea
     _check(_ffi.lib().ard_lstm_tile_bwd(ctypes.byref(desc), _ptr(W), _ptr(dHs), _ptr(dhT), _ptr(dcT), _ptr(ws),
                                         nbytes, _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(dh0), _ptr(dc0),
                                         _stream(stream)))
+
+
+# --------------------------------------------------------------------------- distillation loss
+
+def distill_desc(dtype, batch, classes, top, temperature=1.0, soft_weight=1.0):
+    return ard_distill_desc(dtype, batch, classes, top, temperature, soft_weight)
+
+
+def ard_distill_workspace_bytes(desc):
+    return _ffi.lib().ard_distill_workspace_bytes(ctypes.byref(desc))
+
+
+def ard_distill_fwd(desc, Zt, top_idx, top_logits, labels, loss, stats, ws, stream=None):
+    """stats: 5 * batch floats, read by ard_distill_bwd."""
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_distill_fwd(ctypes.byref(desc), _ptr(Zt), _ptr(top_idx), _ptr(top_logits), _ptr(labels),
+                                      _ptr(loss), _ptr(stats), p, n, _stream(stream)))
+
+
+def ard_distill_bwd(desc, Zt, top_idx, top_logits, labels, stats, dloss, dZt, stream=None):
+    _check(_ffi.lib().ard_distill_bwd(ctypes.byref(desc), _ptr(Zt), _ptr(top_idx), _ptr(top_logits), _ptr(labels),
+                                      _ptr(stats), _ptr(dloss), _ptr(dZt), _stream(stream)))

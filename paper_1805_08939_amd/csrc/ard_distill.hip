@@ -1,0 +1,502 @@
+// Distillation from a teacher's top logits, forward and backward, on
+// feature-major logits Zt[V][B] (as ard_fc_fwd leaves them).
+//
+// Per column, with T the temperature and a the weight of the soft term:
+//   p_j  = softmax over the column's valid teacher entries of t_j / T
+//   q(T) = softmax over all V classes of z / T
+//   loss = a T^2 sum_j p_j (log p_j - log q(T)[idx_j]) - (1 - a) log q(1)[label]
+//   dZ   = dloss (a T (q(T) - p scattered to its classes) + (1 - a) (q(1) - onehot))
+//
+// Forward: one pass over the logits. A thread owns 16 bytes of neighbouring
+// columns and walks down its rows with a running maximum and two running sums
+// (one at temperature 1, one at T; T = 1 needs one); the row ranges of a column
+// meet in LDS and, across workgroups, in the workspace, added in a fixed order.
+// A second, small kernel joins them and does the teacher's entries, of which a
+// column has few. Backward: the dense part of the gradient in one pass from the
+// saved maximum and sums, then the few entries that a teacher's or a label's
+// class touches once more, each with its whole value, so that nothing is rounded
+// twice and no order of additions is left to chance.
+//
+// Bound by reading the logits (and writing the gradient).
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "ard_gemm_fast.hpp"
+#include "ard_internal.hpp"
+
+namespace ard {
+namespace {
+
+// exp of a value <= 0. bf16 logits: the hardware's power of two; its argument's
+// rounding costs at most 2^-24 |x| of relative error, which is far below what
+// the logits themselves are rounded by. fp32 logits: the library function.
+template <typename T>
+__device__ __forceinline__ float exp_neg(float x) {
+  if constexpr (sizeof(T) == 2)
+    return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f);
+  else
+    return expf(x);
+}
+
+// VE consecutive columns of a row, as fp32. Rows start at any element.
+template <typename T, int VE>
+__device__ __forceinline__ void load_cols(const T* p, float (&v)[VE]) {
+  if constexpr (VE == 1) {
+    v[0] = to_f32(*p);
+  } else {
+    const u32x4 raw = load16_any<sizeof(T)>(reinterpret_cast<const char*>(p));
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      if constexpr (sizeof(T) == 2)
+        v[e] = __uint_as_float((e & 1) ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16);
+      else
+        v[e] = __uint_as_float(raw[e]);
+    }
+  }
+}
+template <typename T, int VE>
+__device__ __forceinline__ void store_cols(T* p, const float (&v)[VE]) {
+  if constexpr (VE == 1) {
+    *p = from_f32<T>(v[0]);
+  } else {
+    typedef u32x4 u32x4_a2 __attribute__((aligned(2), may_alias));
+    T w[VE];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) w[e] = from_f32<T>(v[e]);
+    *reinterpret_cast<u32x4_a2*>(p) = *reinterpret_cast<const u32x4*>(w);
+  }
+}
+
+// How a launch lays its threads over the logits: tx threads side by side along
+// a row (a power of two), 256 / tx rows at a time, `splits` ranges of rows.
+struct Grid {
+  int32_t tx, blocks, splits;
+  int64_t rows;  // rows of a range
+};
+
+struct Columns {
+  int64_t col;  // first column of the thread
+  bool on;
+};
+
+// The thread's columns: chunk after chunk of VE, the last one moved back to end
+// at the last column (its columns are then computed twice, alike).
+template <int VE>
+__device__ __forceinline__ Columns columns_of(int32_t B, int32_t tx) {
+  const int64_t c = (static_cast<int64_t>(blockIdx.x) * tx + (threadIdx.x & (tx - 1))) * VE;
+  return {c + VE <= B ? c : static_cast<int64_t>(B) - VE, c < B};
+}
+
+// A running maximum m and the sums of exp(z - m) and exp((z - m) / T).
+struct Run {
+  float m, s1, sT;
+};
+
+// The reference of a maximum: 0 where there is no finite logit yet, so that
+// exp(-inf - ref) is 0 and not NaN.
+__device__ __forceinline__ float ref_of(float m) { return m == -__builtin_inff() ? 0.0f : m; }
+
+template <typename T, bool TWO>
+__device__ __forceinline__ void join(Run& a, const Run& b, float inv_t) {
+  const float m = fmaxf(a.m, b.m), r = ref_of(m);
+  a.s1 = a.s1 * exp_neg<T>(a.m - r) + b.s1 * exp_neg<T>(b.m - r);
+  if constexpr (TWO) a.sT = a.sT * exp_neg<T>((a.m - r) * inv_t) + b.sT * exp_neg<T>((b.m - r) * inv_t);
+  a.m = m;
+}
+
+template <typename T, int VE, bool TWO>
+__global__ void __launch_bounds__(256) distill_sums_kernel(const T* __restrict__ Z, int32_t V, int32_t B, Grid g,
+                                                           float inv_t, float* __restrict__ part) {
+  constexpr int U = 4;  // rows in flight
+  const Columns c = columns_of<VE>(B, g.tx);
+  const int ty = threadIdx.x / g.tx, ny = 256 / g.tx;
+  const int64_t r0 = blockIdx.y * g.rows;
+  const int64_t r1 = r0 + g.rows < V ? r0 + g.rows : V;
+  Run run[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) run[e] = {-__builtin_inff(), 0.0f, 0.0f};
+  if (c.on) {
+    const T* z = Z + c.col;
+    auto take = [&](const float(&x)[U][VE], int n) {  // n of the U rows
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        float m = run[e].m;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (u < n) m = fmaxf(m, x[u][e]);
+        const float r = ref_of(m), old = run[e].m - r;
+        float s1 = run[e].s1 * exp_neg<T>(old), sT = TWO ? run[e].sT * exp_neg<T>(old * inv_t) : 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (u < n) {
+            s1 += exp_neg<T>(x[u][e] - r);
+            if constexpr (TWO) sT += exp_neg<T>((x[u][e] - r) * inv_t);
+          }
+        }
+        run[e] = {m, s1, sT};
+      }
+    };
+    int64_t r = r0 + ty;
+    for (; r + static_cast<int64_t>(U - 1) * ny < r1; r += static_cast<int64_t>(U) * ny) {
+      float x[U][VE];
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_cols<T, VE>(z + (r + static_cast<int64_t>(u) * ny) * B, x[u]);
+      take(x, U);
+    }
+    for (; r < r1; r += ny) {
+      float x[U][VE];
+      load_cols<T, VE>(z + r * B, x[0]);
+      take(x, 1);
+    }
+  }
+  // the rows' threads of a column, halved step by step
+  __shared__ Run red[256];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) {
+    __syncthreads();
+    red[threadIdx.x] = run[e];
+    for (int h = ny / 2; h > 0; h >>= 1) {
+      __syncthreads();
+      if (ty < h) join<T, TWO>(red[threadIdx.x], red[threadIdx.x + h * g.tx], inv_t);
+    }
+    if (ty == 0 && c.on) {
+      float* p = part + static_cast<int64_t>(blockIdx.y) * 3 * B + c.col + e;
+      const Run& s = red[threadIdx.x];
+      p[0] = s.m;
+      p[B] = s.s1;
+      p[2 * static_cast<int64_t>(B)] = TWO ? s.sT : s.s1;
+    }
+  }
+}
+
+// Joins a column's ranges, then the teacher's entries and the label: 32 columns
+// of a workgroup, eight threads each.
+template <typename T, bool TWO>
+__global__ void __launch_bounds__(256) distill_loss_kernel(const T* __restrict__ Z, int32_t V, int32_t B, int32_t top,
+                                                           const int32_t* __restrict__ idx,
+                                                           const float* __restrict__ tl,
+                                                           const int32_t* __restrict__ labels, float temp,
+                                                           float weight, int32_t splits,
+                                                           const float* __restrict__ part, float* __restrict__ loss,
+                                                           float* __restrict__ stats) {
+  constexpr int NX = 32, NY = 8;
+  __shared__ Run red[256];
+  __shared__ float fred[256];
+  const int tx = threadIdx.x % NX, ty = threadIdx.x / NX;
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * NX + tx;
+  const bool on = col < B;
+  const float inv_t = 1.0f / temp;
+  Run a = {-__builtin_inff(), 0.0f, 0.0f};
+  if (on) {
+    for (int s = ty; s < splits; s += NY) {
+      const float* p = part + static_cast<int64_t>(s) * 3 * B + col;
+      join<T, TWO>(a, Run{p[0], p[B], p[2 * static_cast<int64_t>(B)]}, inv_t);
+    }
+  }
+  red[threadIdx.x] = a;
+  for (int h = NY / 2; h > 0; h >>= 1) {
+    __syncthreads();
+    if (ty < h) join<T, TWO>(red[threadIdx.x], red[threadIdx.x + h * NX], inv_t);
+  }
+  __syncthreads();
+  a = red[tx];
+  if (!TWO) a.sT = a.s1;
+  const float ref = ref_of(a.m);
+  // the teacher's maximum over the valid entries
+  float tm = -__builtin_inff();
+  if (on)
+    for (int64_t j = ty; j < top; j += NY) {
+      const int32_t v = idx[j * B + col];
+      if (v >= 0 && v < V) tm = fmaxf(tm, tl[j * B + col]);
+    }
+  fred[threadIdx.x] = tm;
+  __syncthreads();
+  for (int y = 0; y < NY; ++y) tm = fmaxf(tm, fred[y * NX + tx]);
+  const float tref = ref_of(tm);
+  // sums of e_j = exp((t_j - tm) / T) and of e_j ((t_j - tm) - (z_j - m)) / T
+  float es = 0.0f, ds = 0.0f;
+  if (on)
+    for (int64_t j = ty; j < top; j += NY) {
+      const int32_t v = idx[j * B + col];
+      if (v < 0 || v >= V) continue;
+      const float t = (tl[j * B + col] - tref) * inv_t, e = expf(t);
+      const float z = (to_f32(Z[static_cast<int64_t>(v) * B + col]) - ref) * inv_t;
+      es += e;
+      if (!(e == 0.0f)) ds += e * (t - z);
+    }
+  __syncthreads();
+  red[threadIdx.x] = {es, ds, 0.0f};
+  __syncthreads();
+  if (ty != 0 || !on) return;
+  es = ds = 0.0f;
+  for (int y = 0; y < NY; ++y) es += red[y * NX + tx].m, ds += red[y * NX + tx].s1;
+  float out = 0.0f;
+  // a column without a logit above -inf has s1 = 0 and no loss
+  if (weight > 0.0f && !(es == 0.0f) && !(a.sT == 0.0f)) out += weight * temp * temp * (ds / es + logf(a.sT / es));
+  const int32_t label = labels ? labels[col] : -1;
+  if (weight < 1.0f && label >= 0 && label < V && !(a.s1 == 0.0f))
+    out += (1.0f - weight) * (logf(a.s1) - (to_f32(Z[static_cast<int64_t>(label) * B + col]) - ref));
+  loss[col] = out;
+  const int64_t b = B;
+  stats[col] = ref;
+  stats[b + col] = a.s1;
+  stats[2 * b + col] = a.sT;
+  stats[3 * b + col] = tref;
+  stats[4 * b + col] = es;
+}
+
+// A column's factors of the gradient: dz = fT exp((z - m) / T) + f1 exp(z - m),
+// less cs p_j at the teacher's classes and ch at the label.
+struct Factors {
+  float m, fT, f1, cs, ch;
+};
+__device__ __forceinline__ Factors factors_of(int64_t col, int32_t V, int32_t B, const float* stats,
+                                              const int32_t* labels, const float* dloss, float temp, float weight) {
+  const int64_t b = B;
+  const float s1 = stats[b + col], sT = stats[2 * b + col], es = stats[4 * b + col];
+  const float dl = dloss ? dloss[col] : 1.0f;
+  const int32_t label = labels ? labels[col] : -1;
+  const bool soft = weight > 0.0f && !(es == 0.0f) && !(sT == 0.0f);
+  const bool hard = weight < 1.0f && label >= 0 && label < V && !(s1 == 0.0f);
+  Factors f;
+  f.m = stats[col];
+  f.cs = soft ? dl * weight * temp : 0.0f;
+  f.ch = hard ? dl * (1.0f - weight) : 0.0f;
+  f.fT = soft ? f.cs / sT : 0.0f;
+  f.f1 = hard ? f.ch / s1 : 0.0f;
+  return f;
+}
+
+template <typename T, bool TWO>
+__device__ __forceinline__ float dense_grad(float z, float m, float fT, float f1, float inv_t) {
+  const float x = z - m;
+  if constexpr (TWO) {
+    float g = 0.0f;
+    if (!(fT == 0.0f)) g += fT * exp_neg<T>(x * inv_t);
+    if (!(f1 == 0.0f)) g += f1 * exp_neg<T>(x);
+    return g;
+  } else {
+    const float f = fT + f1;
+    return f == 0.0f ? 0.0f : f * exp_neg<T>(x);
+  }
+}
+
+template <typename T, int VE, bool TWO>
+__global__ void __launch_bounds__(256) distill_dense_kernel(const T* __restrict__ Z, int32_t V, int32_t B, Grid g,
+                                                            const int32_t* __restrict__ labels,
+                                                            const float* __restrict__ stats,
+                                                            const float* __restrict__ dloss, float temp, float weight,
+                                                            T* __restrict__ dZ) {
+  constexpr int U = 4;
+  const Columns c = columns_of<VE>(B, g.tx);
+  if (!c.on) return;
+  const int ty = threadIdx.x / g.tx, ny = 256 / g.tx;
+  const float inv_t = 1.0f / temp;
+  float m[VE], fT[VE], f1[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) {
+    const Factors f = factors_of(c.col + e, V, B, stats, labels, dloss, temp, weight);
+    m[e] = f.m, fT[e] = f.fT, f1[e] = f.f1;
+  }
+  const int64_t r0 = blockIdx.y * g.rows;
+  const int64_t r1 = r0 + g.rows < V ? r0 + g.rows : V;
+  auto put = [&](int64_t r, float(&x)[VE]) {
+#pragma unroll
+    for (int e = 0; e < VE; ++e) x[e] = dense_grad<T, TWO>(x[e], m[e], fT[e], f1[e], inv_t);
+    store_cols<T, VE>(dZ + r * B + c.col, x);
+  };
+  int64_t r = r0 + ty;
+  for (; r + static_cast<int64_t>(U - 1) * ny < r1; r += static_cast<int64_t>(U) * ny) {
+    float x[U][VE];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_cols<T, VE>(Z + (r + static_cast<int64_t>(u) * ny) * B + c.col, x[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) put(r + static_cast<int64_t>(u) * ny, x[u]);
+  }
+  for (; r < r1; r += ny) {
+    float x[VE];
+    load_cols<T, VE>(Z + r * B + c.col, x);
+    put(r, x);
+  }
+}
+
+// The entries at the teacher's classes and the label, written whole: one thread
+// each (entry `top` is the label). A class that several entries name gets every
+// one's share from each of their threads, the same value in the same order.
+template <typename T, bool TWO>
+__global__ void __launch_bounds__(256) distill_sparse_kernel(const T* __restrict__ Z, int32_t V, int32_t B,
+                                                             int32_t top, const int32_t* __restrict__ idx,
+                                                             const float* __restrict__ tl,
+                                                             const int32_t* __restrict__ labels,
+                                                             const float* __restrict__ stats,
+                                                             const float* __restrict__ dloss, float temp,
+                                                             float weight, T* __restrict__ dZ) {
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63);
+  const int64_t j = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 6);
+  if (col >= B || j > top) return;
+  const int32_t label = labels ? labels[col] : -1;
+  const int32_t v = j < top ? idx[j * B + col] : label;
+  if (v < 0 || v >= V) return;
+  const float inv_t = 1.0f / temp;
+  const Factors f = factors_of(col, V, B, stats, labels, dloss, temp, weight);
+  const float tref = stats[3 * static_cast<int64_t>(B) + col], es = stats[4 * static_cast<int64_t>(B) + col];
+  float p = 0.0f;
+  if (!(f.cs == 0.0f))
+    for (int64_t i = 0; i < top; ++i)
+      if (idx[i * B + col] == v) p += expf((tl[i * B + col] - tref) * inv_t);
+  const int64_t at = static_cast<int64_t>(v) * B + col;
+  float g = dense_grad<T, TWO>(to_f32(Z[at]), f.m, f.fT, f.f1, inv_t);
+  if (!(f.cs == 0.0f)) g -= f.cs * (p / es);
+  if (v == label) g -= f.ch;
+  dZ[at] = from_f32<T>(g);
+}
+
+int need_ptr(const void* p, const char* name) {
+  if (!p) return fail(ARD_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned16(p)) return fail(ARD_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
+  return ARD_OK;
+}
+int may_ptr(const void* p, const char* name) {
+  if (p && !aligned16(p)) return fail(ARD_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
+  return ARD_OK;
+}
+
+int check_desc(const ard_distill_desc* d) {
+  if (!d) return fail(ARD_ERR_INVALID_ARG, "desc is NULL");
+  if (d->dtype != ARD_F32 && d->dtype != ARD_BF16) return fail(ARD_ERR_UNSUPPORTED, "dtype %d not supported", d->dtype);
+  if (d->batch < 1 || d->classes < 1)
+    return fail(ARD_ERR_INVALID_ARG, "sizes must be >= 1 (batch %d, classes %d)", d->batch, d->classes);
+  if (d->top < 0 || d->top > 65536) return fail(ARD_ERR_INVALID_ARG, "top %d outside 0..65536", d->top);
+  if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !std::isfinite(1.0f / d->temperature))
+    return fail(ARD_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (!(d->soft_weight >= 0.0f && d->soft_weight <= 1.0f))
+    return fail(ARD_ERR_INVALID_ARG, "soft_weight must be in [0, 1]");
+  return ARD_OK;
+}
+
+constexpr int kBlocks = 768;  // workgroups that fill the chip: three on a compute unit
+
+int vector_of(const ard_distill_desc* d) {
+  const int ve = d->dtype == ARD_BF16 ? 8 : 4;
+  return d->batch >= ve ? ve : 1;
+}
+
+// At least 8 rows for each thread, so that a range's sums outweigh joining them.
+Grid grid_of(const ard_distill_desc* d) {
+  const int64_t chunks = (static_cast<int64_t>(d->batch) + vector_of(d) - 1) / vector_of(d);
+  Grid g = {1, 0, 0, 0};
+  while (g.tx < 64 && g.tx < chunks) g.tx *= 2;
+  g.blocks = static_cast<int32_t>((chunks + g.tx - 1) / g.tx);
+  const int64_t least = 8 * (256 / g.tx);
+  int64_t splits = (kBlocks + g.blocks - 1) / g.blocks;
+  const int64_t most = (static_cast<int64_t>(d->classes) + least - 1) / least;
+  if (splits > most) splits = most;
+  g.rows = (static_cast<int64_t>(d->classes) + splits - 1) / splits;
+  g.splits = static_cast<int32_t>((static_cast<int64_t>(d->classes) + g.rows - 1) / g.rows);
+  return g;
+}
+
+size_t workspace_bytes(const ard_distill_desc* d) {
+  return static_cast<size_t>(grid_of(d).splits) * 3 * static_cast<size_t>(d->batch) * 4;
+}
+
+int check_teacher(const ard_distill_desc* d, const int32_t* idx, const float* tl, const int32_t* labels) {
+  int st;
+  if (d->top > 0 && ((st = need_ptr(idx, "top_idx")) || (st = need_ptr(tl, "top_logits")))) return st;
+  return may_ptr(labels, "labels");
+}
+
+template <typename T, int VE, bool TWO>
+int fwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, const float* tl, const int32_t* labels,
+             float* loss, float* stats, float* part, hipStream_t stream) {
+  const Grid g = grid_of(d);
+  const T* Z = static_cast<const T*>(Zt);
+  hipLaunchKernelGGL((distill_sums_kernel<T, VE, TWO>), dim3(g.blocks, g.splits), dim3(256), 0, stream, Z, d->classes,
+                     d->batch, g, 1.0f / d->temperature, part);
+  ARD_LAUNCH_CHECK();
+  hipLaunchKernelGGL((distill_loss_kernel<T, TWO>), dim3((d->batch - 1) / 32 + 1), dim3(256), 0, stream, Z, d->classes,
+                     d->batch, d->top, idx, tl, labels, d->temperature, d->soft_weight, g.splits, part, loss, stats);
+  ARD_LAUNCH_CHECK();
+  return ARD_OK;
+}
+
+template <typename T, int VE, bool TWO>
+int bwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, const float* tl, const int32_t* labels,
+             const float* stats, const float* dloss, void* dZt, hipStream_t stream) {
+  const Grid g = grid_of(d);
+  const T* Z = static_cast<const T*>(Zt);
+  T* dZ = static_cast<T*>(dZt);
+  hipLaunchKernelGGL((distill_dense_kernel<T, VE, TWO>), dim3(g.blocks, g.splits), dim3(256), 0, stream, Z,
+                     d->classes, d->batch, g, labels, stats, dloss, d->temperature, d->soft_weight, dZ);
+  ARD_LAUNCH_CHECK();
+  if (d->top > 0 || labels) {
+    hipLaunchKernelGGL((distill_sparse_kernel<T, TWO>), dim3((d->batch - 1) / 64 + 1, d->top / 4 + 1), dim3(256), 0,
+                       stream, Z, d->classes, d->batch, d->top, idx, tl, labels, stats, dloss, d->temperature,
+                       d->soft_weight, dZ);
+    ARD_LAUNCH_CHECK();
+  }
+  return ARD_OK;
+}
+
+// Calls f with a value of the element type, the columns per thread and whether
+// the two softmaxes differ.
+template <class F>
+int dispatch(const ard_distill_desc* d, F f) {
+  using std::integral_constant;
+  const bool two = d->temperature != 1.0f;
+  auto with = [&](auto t, auto ve) {
+    return two ? f(t, ve, std::true_type{}) : f(t, ve, std::false_type{});
+  };
+  const int ve = vector_of(d);
+  if (d->dtype == ARD_BF16)
+    return ve > 1 ? with(bf16{}, integral_constant<int, 8>{}) : with(bf16{}, integral_constant<int, 1>{});
+  return ve > 1 ? with(float{}, integral_constant<int, 4>{}) : with(float{}, integral_constant<int, 1>{});
+}
+
+}  // namespace
+}  // namespace ard
+
+using namespace ard;
+
+extern "C" {
+
+size_t ard_distill_workspace_bytes(const ard_distill_desc* desc) {
+  if (check_desc(desc) != ARD_OK) return 0;
+  return workspace_bytes(desc);
+}
+
+int ard_distill_fwd(const ard_distill_desc* desc, const void* Zt, const int32_t* top_idx, const float* top_logits,
+                    const int32_t* labels, float* loss, float* stats, void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  int st = check_desc(desc);
+  if (st != ARD_OK) return st;
+  if ((st = need_ptr(Zt, "Zt")) || (st = need_ptr(loss, "loss")) || (st = need_ptr(stats, "stats")) ||
+      (st = check_teacher(desc, top_idx, top_logits, labels)))
+    return st;
+  if (!ws || ws_bytes < workspace_bytes(desc))
+    return fail(ARD_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", workspace_bytes(desc), ws ? ws_bytes : 0);
+  if (!aligned16(ws)) return fail(ARD_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+  return dispatch(desc, [&](auto t, auto ve, auto two) {
+    return fwd_impl<decltype(t), decltype(ve)::value, decltype(two)::value>(
+        desc, Zt, top_idx, top_logits, labels, loss, stats, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
+  });
+}
+
+int ard_distill_bwd(const ard_distill_desc* desc, const void* Zt, const int32_t* top_idx, const float* top_logits,
+                    const int32_t* labels, const float* stats, const float* dloss, void* dZt, void* stream) {
+  clear_error();
+  int st = check_desc(desc);
+  if (st != ARD_OK) return st;
+  if ((st = need_ptr(Zt, "Zt")) || (st = need_ptr(stats, "stats")) || (st = need_ptr(dZt, "dZt")) ||
+      (st = may_ptr(dloss, "dloss")) || (st = check_teacher(desc, top_idx, top_logits, labels)))
+    return st;
+  if (dZt == Zt) return fail(ARD_ERR_INVALID_ARG, "dZt must not be Zt: the logits are read again after the first pass");
+  return dispatch(desc, [&](auto t, auto ve, auto two) {
+    return bwd_impl<decltype(t), decltype(ve)::value, decltype(two)::value>(
+        desc, Zt, top_idx, top_logits, labels, stats, dloss, dZt, static_cast<hipStream_t>(stream));
+  });
+}
+
+}  // extern "C"

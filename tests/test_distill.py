@@ -1,0 +1,181 @@
+"""The distillation loss: the oracle against finite differences and torch (CPU), refusals (CPU), and the kernels against
+the oracle (GPU).
+
+Tolerances, per column or value. Loss: the logarithms and sums of exponentials are off by a few units of 2^-24 (a sum's
+terms are added in chains of at most V / 8 and joined pairwise; the largest term is 1): 64 units of the loss's terms and
+of their factor weight T^2. Gradient: 64 units of the largest factor (weight T, 1) times the softmax value, and the
+rounding to the logits' type.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import distill as od
+from paper_1805_08939_amd import api, synth
+
+U32, UBF = 2.0 ** -24, 2.0 ** -8
+INF = float("inf")
+
+
+# ---------------------------------------------------------------- the oracle
+
+def test_oracle_gradient_is_the_loss_differenced():
+    r = np.random.default_rng(3)
+    z, idx, t = r.normal(size=9), [4, 0, 4, -1, 11], r.normal(size=5)  # a class named twice, two entries that are none
+    for T, a in ((1.0, 1.0), (2.5, 0.3), (0.7, 0.0)):
+        _, dz, _ = od.column(z, idx, t, 2, T, a)
+        for v in range(9):
+            e = np.eye(9)[v] * 1e-6
+            d = (od.column(z + e, idx, t, 2, T, a)[0] - od.column(z - e, idx, t, 2, T, a)[0]) / 2e-6
+            assert abs(d - dz[v]) < 1e-7
+
+
+def test_oracle_is_torch():
+    r = np.random.default_rng(4)
+    z, t = torch.tensor(r.normal(size=(6, 20))), torch.tensor(r.normal(size=(6, 20)))
+    T = 2.0
+    want = T * T * torch.nn.functional.kl_div(torch.log_softmax(z / T, 1), torch.softmax(t / T, 1), reduction="none").sum(1)
+    hard = torch.nn.functional.cross_entropy(z, torch.arange(6), reduction="none")
+    idx = np.tile(np.arange(20)[:, None], (1, 6))  # every class named: the whole teacher
+    loss, _, _ = od.batch(z.numpy().T, idx, t.numpy().T, np.arange(6), T, 0.6)
+    assert np.abs(loss - (0.6 * want + 0.4 * hard).numpy()).max() < 1e-12
+
+
+# ---------------------------------------------------------------- refusals
+
+def test_refuses_bad_calls():
+    a = 4096
+    good = dict(dtype=api.ARD_F32, batch=4, classes=9, top=3, temperature=2.0, soft_weight=0.5)
+
+    def refused(status, call, *args):
+        with pytest.raises(api.ArdError) as e:
+            call(*args, stream=0)
+        assert e.value.status == status and e.value.message
+
+    for bad, status in ((dict(dtype=3), 2), (dict(batch=0), 1), (dict(classes=0), 1), (dict(top=-1), 1),
+                        (dict(top=70000), 1), (dict(temperature=0.0), 1), (dict(temperature=float("nan")), 1),
+                        (dict(temperature=INF), 1), (dict(temperature=-1.0), 1), (dict(soft_weight=1.5), 1),
+                        (dict(soft_weight=float("nan")), 1)):
+        d = api.distill_desc(**{**good, **bad})
+        assert api.ard_distill_workspace_bytes(d) == 0
+        refused(status, api.ard_distill_fwd, d, a, a, a, a, a, a, (a, 1 << 30))
+        refused(status, api.ard_distill_bwd, d, a, a, a, a, a, a, 2 * a)
+    d = api.distill_desc(**good)
+    for i in (0, 1, 2, 4, 5):
+        args = [a] * 6
+        args[i] = None
+        refused(1, api.ard_distill_fwd, d, *args, (a, 1 << 30))
+        args[i] = a + 4
+        refused(1, api.ard_distill_fwd, d, *args, (a, 1 << 30))
+    refused(5, api.ard_distill_fwd, d, a, a, a, a, a, a, None)
+    refused(5, api.ard_distill_fwd, d, a, a, a, a, a, a, (a, 4))
+    refused(1, api.ard_distill_bwd, d, a, a, a, a, a, None, a)  # in place
+    refused(1, api.ard_distill_bwd, d, a, a, a, a, None, None, 2 * a)
+    refused(1, api.ard_distill_bwd, d, a, a, a, a, a, None, None)
+
+
+# ---------------------------------------------------------------- the kernels
+
+def _run(dtype, Z, idx, t, labels, T, a, dloss):
+    from gpu_util import ard_dtype, device, workspace
+    dev = device()
+    V, B = Z.shape
+    desc = api.distill_desc(ard_dtype(dtype), B, V, idx.shape[0], T, a)
+    put = lambda x: None if x is None or x.numel() == 0 else x.contiguous().to(dev)  # noqa: E731
+    z, i, tl, lab, dl = put(Z), put(idx), put(t), put(labels), put(dloss)
+    loss, stats = torch.full((B,), 7.0, device=dev), torch.empty(5, B, device=dev)
+    dZ = torch.full_like(z, 7.0)
+    ws = workspace(api.ard_distill_workspace_bytes(desc))
+    api.ard_distill_fwd(desc, z, i, tl, lab, loss, stats, ws)
+    api.ard_distill_bwd(desc, z, i, tl, lab, stats, dl, dZ)
+    torch.cuda.synchronize()
+    return loss.double().cpu().numpy(), dZ.double().cpu().numpy()
+
+
+def _check(dtype, Z, idx, t, labels, T, a, dloss):
+    got, dgot = _run(dtype, Z, idx, t, labels, T, a, dloss)
+    z = Z.double().numpy()
+    with np.errstate(invalid="ignore", over="ignore"):
+        loss, dz, size = od.batch(z, idx.numpy(), t.double().numpy(), None if labels is None else labels.numpy(), T, a)
+        loss[np.isinf(loss.astype(np.float32))] = INF  # past the range of the loss's type
+    dl = np.ones(Z.shape[1]) if dloss is None else dloss.double().numpy()
+    dz = dz * dl
+    fine = np.isfinite(loss)
+    assert np.array_equal(np.isposinf(loss), np.isposinf(got)) and np.isfinite(got[fine]).all()
+    span = 1 + np.abs(np.where(np.isfinite(z), z, 0)).max() / min(T, 1.0)
+    bound = 64 * U32 * (size + span * (a * T * T + 1 - a))
+    assert (np.abs(got - loss)[fine] <= bound[fine]).all(), np.abs(got - loss)[fine].max()
+    out = UBF if dtype == "bf16" else U32
+    assert np.isfinite(dgot).all()
+    bound = out * np.abs(dz) + (64 + 4 * span) * U32 * (a * T + 1 - a) * np.abs(dl) + 1e-38
+    assert (np.abs(dgot - dz) <= bound).all(), np.abs(dgot - dz).max()
+
+
+def _inputs(dtype, V, B, top, seed):
+    g = synth.generator(1805 + seed)
+    Z = synth.to_storage(synth.normal(g, (V, B), 3.0), dtype)
+    r = np.random.default_rng(seed)
+    idx = np.stack([r.permutation(V)[:top] if top <= V else r.integers(0, V, top) for _ in range(B)], 1)
+    return (Z, torch.tensor(idx.reshape(top, B).astype(np.int32)), synth.normal(g, (top, B), 2.0) + 5,
+            torch.tensor(r.integers(0, V, B).astype(np.int32)), synth.normal(g, (B,)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,B,top,T,a", [
+    (1, 1, 1, 1.0, 0.5), (2, 1, 2, 3.0, 1.0), (10, 128, 5, 4.0, 0.9), (10, 3, 10, 1.0, 0.5), (50, 7, 3, 2.0, 0.0),
+    (1000, 1, 64, 2.0, 0.5), (333, 9, 1, 1.0, 1.0), (257, 100, 17, 0.5, 0.5), (8800, 20, 20, 2.0, 0.5),
+    (1031, 65, 8, 1.0, 0.7), (64, 700, 4, 2.0, 0.3), (40, 1030, 6, 1.0, 0.6), (5003, 16, 300, 1.5, 0.4),
+    (7, 4, 12, 2.0, 0.5), (700, 12, 0, 2.0, 0.5)])
+def test_loss_and_gradient(dtype, V, B, top, T, a):
+    Z, idx, t, labels, dloss = _inputs(dtype, V, B, top, V + B)
+    _check(dtype, Z, idx, t, labels, T, a, dloss)
+    _check(dtype, Z, idx, t, None, T, a, None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1.0, 2.0])
+def test_masked_and_empty_columns(dtype, T):
+    V, B, top = 300, 24, 6
+    Z, idx, t, labels, dloss = _inputs(dtype, V, B, top, 77)
+    Z[5:250, 1] = -INF                       # masked classes, some of them the teacher's
+    Z[:, 2] = -INF                           # nothing left
+    Z[:, 3] = torch.finfo(Z.dtype).min       # the type's lowest value everywhere
+    Z[7:, 4] = torch.finfo(Z.dtype).min      # and as a mask
+    Z[:, 5] = 100.0
+    Z[17, 6] = 300.0                         # one class far above the others
+    idx[:, 7] = -1                           # no entry
+    idx[2:, 8] = V                           # entries outside
+    idx[:, 9] = 11                           # one class in every entry
+    idx[0, 10], idx[3, 10] = 5, 5            # a class named twice
+    t[:, 11] = -INF                          # a teacher without a finite logit
+    t[1:, 12] = -INF
+    t[:, 13] = 80.0
+    labels[14], labels[15], labels[16] = -1, V, -100
+    labels[9] = 11                           # label and teacher in one place
+    idx[:, 17], labels[17] = -1, -1          # no term at all
+    Z[:, 18] = Z[:, 18] * 20
+    _check(dtype, Z, idx, t, labels, T, 0.6, dloss)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nan_stays_in_its_column(dtype):
+    V, B, top = 120, 11, 4
+    Z, idx, t, labels, dloss = _inputs(dtype, V, B, top, 5)
+    clean, dclean = _run(dtype, Z, idx, t, labels, 2.0, 0.5, dloss)
+    Z[33, 4] = float("nan")
+    Z[70, 6] = INF
+    got, dgot = _run(dtype, Z, idx, t, labels, 2.0, 0.5, dloss)
+    rest = [b for b in range(B) if b not in (4, 6)]
+    assert np.isnan(got[[4, 6]]).all() and np.isnan(dgot[:, 4]).all()
+    assert np.array_equal(got[rest], clean[rest]) and np.array_equal(dgot[:, rest], dclean[:, rest])
+
+
+@pytest.mark.gpu
+def test_runs_alike():
+    Z, idx, t, labels, dloss = _inputs("bf16", 3001, 333, 9, 8)
+    idx[4] = idx[2]
+    a, b = (_run("bf16", Z, idx, t, labels, 2.0, 0.5, dloss) for _ in range(2))
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
