@@ -524,6 +524,48 @@ int ard_lstm_tile_bwd(const ard_lstm_tile_desc* desc, const void* W, const void*
                       void* dc0, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Gated feed-forward layer under a row pattern (device).                   */
+/* ------------------------------------------------------------------------ */
+/*
+ * Two projections of the same input, an activation of the first and their
+ * product, with the hidden units of a row pattern (Sec. III-A) dropped:
+ *   g = W[0] x + bias[0],  u = W[1] x + bias[1]
+ *   h = scale * act(g) * u on kept units, dropped units as `dropped` says.
+ * Layouts: Xt[K][B], W[2][N][K] (the gate's rows, then the other projection's),
+ * bias[2][N] fp32 (NULL = 0), Ht[N][B], Zt[2][N][B] = (g, u). The projection
+ * back is an ard_fc_* call whose in_plan is this layer's hidden_plan.
+ * fwd: Zt is what the backward needs; NULL where nothing is trained. Its
+ * dropped rows are not written.
+ * bwd: dHt[N][B] -> dXt[K][B], dW[2][N][K] and dbias[2][N] fp32 (each may be
+ * NULL). The derivatives of g and u are computed in fp32 (and summed into
+ * dbias so), rounded once to dtype and multiplied by W and X. dW is of
+ * grad_dtype: ARD_F32, as ard_fc_sgd_momentum reads it (once per projection),
+ * or, where dtype is ARD_BF16, ARD_BF16 for optimisers that keep gradients in
+ * the weights' type. Dropped rows of Ht, dW and dbias are 0 or untouched as
+ * `dropped` says; dropped rows of Zt and dHt are not read.
+ */
+enum { ARD_GLU_SILU = 0, ARD_GLU_GELU = 1 /* exact, by erf */, ARD_GLU_RELU = 2, ARD_GLU_SIGMOID = 3 };
+
+typedef struct {
+  int32_t dtype;
+  int32_t batch;            /* B >= 1 */
+  int32_t in_features;      /* K >= 1 */
+  int32_t hidden_features;  /* N >= 1 */
+  const ard_row_plan* hidden_plan;  /* n == N (a list is not needed), or NULL = every unit kept */
+  float scale;
+  int32_t act;              /* ARD_GLU_* */
+  int32_t dropped;          /* ARD_DROPPED_ZERO or ARD_DROPPED_SKIP */
+  int32_t grad_dtype;       /* of dW: ARD_F32, or dtype */
+} ard_glu_desc;
+
+/* Workspace of fwd and bwd (0 is possible; NULL is accepted then). */
+size_t ard_glu_workspace_bytes(const ard_glu_desc* desc);
+int ard_glu_fwd(const ard_glu_desc* desc, const void* Xt, const void* W, const float* bias, void* Zt, void* Ht,
+                void* ws, size_t ws_bytes, void* stream);
+int ard_glu_bwd(const ard_glu_desc* desc, const void* Xt, const void* W, const void* Zt, const void* dHt, void* dXt,
+                void* dW, float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Distillation from a teacher's top logits (device).                       */
 /* ------------------------------------------------------------------------ */
 /*

@@ -17,6 +17,7 @@ ARD_F32, ARD_BF16 = 0, 1
 ARD_SEARCH_PLAIN, ARD_SEARCH_MIRROR = 0, 1
 ARD_ACT_NONE, ARD_ACT_RELU = 0, 1
 ARD_DROPPED_ZERO, ARD_DROPPED_SKIP = 0, 1
+ARD_GLU_SILU, ARD_GLU_GELU, ARD_GLU_RELU, ARD_GLU_SIGMOID = 0, 1, 2, 3
 ARD_WEIGHTS_FULL, ARD_WEIGHTS_COMPACT, ARD_WEIGHTS_COMPACT_GRAD, ARD_WEIGHTS_INPUT_MAJOR = 0, 1, 2, 3
 
 
@@ -64,6 +65,12 @@ class ard_lstm_desc(ctypes.Structure):
 class ard_lstm_tile_desc(ctypes.Structure):
     _fields_ = [("dtype", c_i32), ("seq_len", c_i32), ("batch", c_i32), ("input_size", c_i32),
                 ("hidden_size", c_i32), ("reserved", c_i32), ("weight_plan", ctypes.POINTER(ard_tile_plan))]
+
+
+class ard_glu_desc(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("batch", c_i32), ("in_features", c_i32), ("hidden_features", c_i32),
+                ("hidden_plan", ctypes.POINTER(ard_row_plan)), ("scale", c_f32), ("act", c_i32), ("dropped", c_i32),
+                ("grad_dtype", c_i32)]
 
 
 class ard_distill_desc(ctypes.Structure):
@@ -129,6 +136,10 @@ SIGNATURES = {
                                     c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
     "ard_lstm_bwd": (ctypes.c_int, [ctypes.POINTER(ard_lstm_desc), c_vp, c_vp, c_vp, c_vp, c_vp,
                                     c_size, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
+    "ard_glu_workspace_bytes": (c_size, [ctypes.POINTER(ard_glu_desc)]),
+    "ard_glu_fwd": (ctypes.c_int, [ctypes.POINTER(ard_glu_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
+    "ard_glu_bwd": (ctypes.c_int, [ctypes.POINTER(ard_glu_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                   c_size, c_vp]),
     "ard_distill_workspace_bytes": (c_size, [ctypes.POINTER(ard_distill_desc)]),
     "ard_distill_fwd": (ctypes.c_int, [ctypes.POINTER(ard_distill_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
                                        c_size, c_vp]),

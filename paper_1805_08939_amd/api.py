@@ -11,11 +11,12 @@ import numpy as np
 
 from . import _ffi
 from ._ffi import (ARD_ACT_NONE, ARD_ACT_RELU, ARD_BF16, ARD_DROPPED_SKIP, ARD_DROPPED_ZERO,  # noqa: F401
-                   ARD_ERR_INVALID_ARG, ARD_ERR_NOT_CONVERGED, ARD_F32, ARD_SEARCH_MIRROR, ARD_SEARCH_PLAIN,
+                   ARD_ERR_INVALID_ARG, ARD_ERR_NOT_CONVERGED, ARD_F32, ARD_GLU_GELU, ARD_GLU_RELU, ARD_GLU_SIGMOID,
+                   ARD_GLU_SILU, ARD_SEARCH_MIRROR, ARD_SEARCH_PLAIN,
                    ARD_WEIGHTS_COMPACT, ARD_WEIGHTS_COMPACT_GRAD, ARD_WEIGHTS_FULL, ARD_WEIGHTS_INPUT_MAJOR,
                    ard_fc_desc, ard_lstm_desc, ard_lstm_tile_desc, ard_row_plan, ard_search_info, ard_search_opts,
                    ard_tile_desc, ard_tile_plan,
-                   ard_distill_desc)
+                   ard_glu_desc, ard_distill_desc)
 
 
 class ArdError(RuntimeError):
@@ -343,6 +344,32 @@ def ard_lstm_tile_bwd(desc, W, dHs, dhT, dcT, ws, dX, dW, dbias, dh0, dc0, strea
     _check(_ffi.lib().ard_lstm_tile_bwd(ctypes.byref(desc), _ptr(W), _ptr(dHs), _ptr(dhT), _ptr(dcT), _ptr(ws),
                                         nbytes, _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(dh0), _ptr(dc0),
                                         _stream(stream)))
+
+
+# --------------------------------------------------------------------------- gated feed-forward layer
+
+def glu_desc(dtype, batch, in_features, hidden_features, hidden_plan=None, scale=1.0, act=ARD_GLU_SILU,
+             dropped=ARD_DROPPED_ZERO, grad_dtype=ARD_F32):
+    d = ard_glu_desc(dtype, batch, in_features, hidden_features, _plan_ptr(hidden_plan), scale, act, dropped, grad_dtype)
+    d._keep = hidden_plan
+    return d
+
+
+def ard_glu_workspace_bytes(desc):
+    return _ffi.lib().ard_glu_workspace_bytes(ctypes.byref(desc))
+
+
+def ard_glu_fwd(desc, Xt, W, bias, Zt, Ht, ws=None, stream=None):
+    """Zt None: nothing is kept for a backward pass."""
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_glu_fwd(ctypes.byref(desc), _ptr(Xt), _ptr(W), _ptr(bias), _ptr(Zt), _ptr(Ht), p, n,
+                                  _stream(stream)))
+
+
+def ard_glu_bwd(desc, Xt, W, Zt, dHt, dXt, dW, dbias, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_glu_bwd(ctypes.byref(desc), _ptr(Xt), _ptr(W), _ptr(Zt), _ptr(dHt), _ptr(dXt), _ptr(dW),
+                                  _ptr(dbias), p, n, _stream(stream)))
 
 
 # --------------------------------------------------------------------------- distillation loss
