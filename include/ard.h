@@ -600,6 +600,55 @@ int ard_distill_fwd(const ard_distill_desc* desc, const void* Zt, const int32_t*
 int ard_distill_bwd(const ard_distill_desc* desc, const void* Zt, const int32_t* top_idx, const float* top_logits,
                     const int32_t* labels, const float* stats, const float* dloss, void* dZt, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* Linear attention with a decay for each head (device).                    */
+/* ------------------------------------------------------------------------ */
+/*
+ * For each sequence and head h, over the sequence's tokens t in order:
+ *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   o_t = scale * S_t^T q_t
+ * Layouts: a token is a column, as a sample is for the other layers:
+ * Qt[q_heads * key_dim][tokens], Kt[kv_heads * key_dim][tokens],
+ * Vt[kv_heads * value_dim][tokens], Ot[q_heads * value_dim][tokens] (dtype);
+ * log_decay[q_heads] fp32 (<= 0; -inf forgets at once), states
+ * S[n_seqs][q_heads][key_dim][value_dim] fp32. Head h reads the keys and
+ * values of head h / (q_heads / kv_heads). Sequence s is the columns
+ * d_offsets[s] .. d_offsets[s + 1] - 1 (device memory; at most max_len of
+ * them, none is allowed; entries are clamped to 0 .. tokens), or, with
+ * d_offsets NULL, the columns s * max_len .. (s + 1) * max_len - 1. Columns of
+ * no sequence are not touched.
+ * fwd: S0 (NULL = 0) is the state before the first token; ST (may be NULL)
+ * receives the one after the last; of an empty sequence it is S0.
+ * bwd: dOt and dST (NULL = 0) -> dQt, dKt, dVt (of a shared head the sum over
+ * the heads that read it) and dS0 (each may be NULL). The decays are constants
+ * and have no gradient.
+ * step: one token for each sequence (max_len 1, d_offsets NULL, tokens ==
+ * n_seqs), no workspace; ST may be S0.
+ */
+typedef struct {
+  int32_t dtype;
+  int32_t n_seqs;     /* >= 1 */
+  int32_t max_len;    /* >= 1 */
+  int32_t tokens;     /* row length of Qt, Kt, Vt, Ot; >= 1 */
+  int32_t q_heads;    /* a multiple of kv_heads */
+  int32_t kv_heads;   /* >= 1 */
+  int32_t key_dim;    /* 1 .. 128 */
+  int32_t value_dim;  /* 1 .. 128 */
+  float scale;
+  int32_t reserved;
+  const int32_t* d_offsets;  /* [n_seqs + 1], or NULL */
+} ard_linattn_desc;
+
+/* Workspace of fwd and bwd. */
+size_t ard_linattn_workspace_bytes(const ard_linattn_desc* desc);
+int ard_linattn_fwd(const ard_linattn_desc* desc, const void* Qt, const void* Kt, const void* Vt,
+                    const float* log_decay, const float* S0, void* Ot, float* ST, void* ws, size_t ws_bytes,
+                    void* stream);
+int ard_linattn_bwd(const ard_linattn_desc* desc, const void* Qt, const void* Kt, const void* Vt,
+                    const float* log_decay, const float* S0, const void* dOt, const float* dST, void* dQt, void* dKt,
+                    void* dVt, float* dS0, void* ws, size_t ws_bytes, void* stream);
+int ard_linattn_step(const ard_linattn_desc* desc, const void* Qt, const void* Kt, const void* Vt,
+                     const float* log_decay, const float* S0, void* Ot, float* ST, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

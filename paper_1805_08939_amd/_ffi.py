@@ -78,6 +78,12 @@ class ard_distill_desc(ctypes.Structure):
                 ("soft_weight", c_f32)]
 
 
+class ard_linattn_desc(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("n_seqs", c_i32), ("max_len", c_i32), ("tokens", c_i32), ("q_heads", c_i32),
+                ("kv_heads", c_i32), ("key_dim", c_i32), ("value_dim", c_i32), ("scale", c_f32), ("reserved", c_i32),
+                ("d_offsets", c_vp)]
+
+
 # name -> (restype, argtypes); every symbol the header declares.
 SIGNATURES = {
     "ard_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -145,6 +151,13 @@ SIGNATURES = {
                                        c_size, c_vp]),
     "ard_distill_bwd": (ctypes.c_int, [ctypes.POINTER(ard_distill_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
                                        c_vp]),
+    "ard_linattn_workspace_bytes": (c_size, [ctypes.POINTER(ard_linattn_desc)]),
+    "ard_linattn_fwd": (ctypes.c_int, [ctypes.POINTER(ard_linattn_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                       c_vp, c_size, c_vp]),
+    "ard_linattn_bwd": (ctypes.c_int, [ctypes.POINTER(ard_linattn_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                       c_vp, c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
+    "ard_linattn_step": (ctypes.c_int, [ctypes.POINTER(ard_linattn_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                        c_vp]),
 }
 
 _lib = None

@@ -16,7 +16,7 @@ from ._ffi import (ARD_ACT_NONE, ARD_ACT_RELU, ARD_BF16, ARD_DROPPED_SKIP, ARD_D
                    ARD_WEIGHTS_COMPACT, ARD_WEIGHTS_COMPACT_GRAD, ARD_WEIGHTS_FULL, ARD_WEIGHTS_INPUT_MAJOR,
                    ard_fc_desc, ard_lstm_desc, ard_lstm_tile_desc, ard_row_plan, ard_search_info, ard_search_opts,
                    ard_tile_desc, ard_tile_plan,
-                   ard_glu_desc, ard_distill_desc)
+                   ard_glu_desc, ard_distill_desc, ard_linattn_desc)
 
 
 class ArdError(RuntimeError):
@@ -392,3 +392,36 @@ def ard_distill_fwd(desc, Zt, top_idx, top_logits, labels, loss, stats, ws, stre
 def ard_distill_bwd(desc, Zt, top_idx, top_logits, labels, stats, dloss, dZt, stream=None):
     _check(_ffi.lib().ard_distill_bwd(ctypes.byref(desc), _ptr(Zt), _ptr(top_idx), _ptr(top_logits), _ptr(labels),
                                       _ptr(stats), _ptr(dloss), _ptr(dZt), _stream(stream)))
+
+
+# --------------------------------------------------------------------------- linear attention
+
+def linattn_desc(dtype, n_seqs, max_len, tokens, q_heads, kv_heads, key_dim, value_dim, scale=1.0, d_offsets=None):
+    """d_offsets: int32 device tensor of n_seqs + 1 column numbers, or None (n_seqs runs of max_len columns)."""
+    d = ard_linattn_desc(dtype, n_seqs, max_len, tokens, q_heads, kv_heads, key_dim, value_dim, scale, 0,
+                         _ptr(d_offsets))
+    d._keep = d_offsets
+    return d
+
+
+def ard_linattn_workspace_bytes(desc):
+    return _ffi.lib().ard_linattn_workspace_bytes(ctypes.byref(desc))
+
+
+def ard_linattn_fwd(desc, Qt, Kt, Vt, log_decay, S0, Ot, ST, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_linattn_fwd(ctypes.byref(desc), _ptr(Qt), _ptr(Kt), _ptr(Vt), _ptr(log_decay), _ptr(S0),
+                                      _ptr(Ot), _ptr(ST), p, n, _stream(stream)))
+
+
+def ard_linattn_bwd(desc, Qt, Kt, Vt, log_decay, S0, dOt, dST, dQt, dKt, dVt, dS0, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_linattn_bwd(ctypes.byref(desc), _ptr(Qt), _ptr(Kt), _ptr(Vt), _ptr(log_decay), _ptr(S0),
+                                      _ptr(dOt), _ptr(dST), _ptr(dQt), _ptr(dKt), _ptr(dVt), _ptr(dS0), p, n,
+                                      _stream(stream)))
+
+
+def ard_linattn_step(desc, Qt, Kt, Vt, log_decay, S0, Ot, ST, stream=None):
+    """One token for each sequence; ST may be S0 (the state is then updated in place)."""
+    _check(_ffi.lib().ard_linattn_step(ctypes.byref(desc), _ptr(Qt), _ptr(Kt), _ptr(Vt), _ptr(log_decay), _ptr(S0),
+                                       _ptr(Ot), _ptr(ST), _stream(stream)))
