@@ -71,35 +71,41 @@ __device__ __forceinline__ Span span_of(const MixArgs& g, int s) {
 struct Decay {
   float l2;
   __device__ __forceinline__ explicit Decay(float g) : l2((g < -1e30f ? -1e30f : g) * 1.44269504088896340736f) {}
-  __device__ __forceinline__ float pow(int n) const { return __builtin_amdgcn_exp2f(l2 * static_cast<float>(n)); }
+  __device__ __forceinline__ float pow(int n) const { return pow(static_cast<float>(n)); }
+  __device__ __forceinline__ float pow(float n) const { return __builtin_amdgcn_exp2f(l2 * n); }
 };
 
 // ------------------------------------------------------------------ LDS tiles
 // [rows][COLS] of 16-byte chunks, chunk c of row r at position c ^ swz(r), so that
 // neither 16 rows at one chunk (operands contiguous along the contraction) nor
 // rows r .. r + 3 and r + 8 .. r + 11 at neighbouring chunks (transposed reads, and
-// fp32's element reads of four rows) meet in a bank.
+// fp32's element reads of four rows) meet in a bank. swz depends on r % 16 only.
+template <int ES, int COLS>
+__device__ __forceinline__ int swz(int r) {
+  if constexpr (COLS * ES / 16 == 8) {
+    const int h = (r >> 1) & 7;
+    return ((h & 1) << 1) | (h & 4) | ((h >> 1) & 1);
+  } else if constexpr (ES == 4) {
+    return ((r & 3) << 2) | ((r >> 2) & 3);
+  } else {
+    return ((r & 3) << 1) | (r & 8);
+  }
+}
 template <int ES, int COLS>
 __device__ __forceinline__ int tile_off(int r, int c) {
-  constexpr int CPR = COLS * ES / 16;
-  int s;
-  if constexpr (CPR == 8) {
-    const int h = (r >> 1) & 7;
-    s = ((h & 1) << 1) | (h & 4) | ((h >> 1) & 1);
-  } else if constexpr (ES == 4) {
-    s = ((r & 3) << 2) | ((r >> 2) & 3);
-  } else {
-    s = ((r & 3) << 1) | (r & 8);
-  }
-  return (r * CPR + (c ^ s)) * 16;
+  return r * COLS * ES + ((c ^ swz<ES, COLS>(r)) << 4);
 }
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // MFMA operands of 16 x 16 blocks. Along: 16 rows of a tile, the contraction along
 // its columns (16 bytes of a lane). Across: 16 columns, the contraction along its
 // rows. bf16: a step of 32; fp32: Along 16 (four MFMAs, slot g holding 4 g + e),
-// Across 4.
+// Across 4. A lane's address is computed once per kind of read (base_*) for row and
+// column 0; constant columns enter by exclusive or, constant rows by addition, so
+// that a read costs no arithmetic and no register of its own.
 template <typename T>
 struct Ops;
 template <>
@@ -108,26 +114,40 @@ struct Ops<bf16> {
   using Across = bf16x8;
   static constexpr int ALONG = 32, ACROSS = 32;
   template <int COLS>
-  static __device__ __forceinline__ Along along(const char* t, int row, int col) {
-    const int lane = threadIdx.x & 63;
-    return *reinterpret_cast<const bf16x8*>(t + tile_off<2, COLS>(row + (lane & 15), (col >> 3) + (lane >> 4)));
+  static __device__ __forceinline__ int base_along() {
+    return tile_off<2, COLS>(threadIdx.x & 15, (threadIdx.x >> 4) & 3);
   }
   template <int COLS>
-  static __device__ __forceinline__ Across across(const char* t, int row, int col) {
-    const int lane = threadIdx.x & 63, s = lane & 15;
-    const int r = row + 8 * (lane >> 4) + (s >> 2), c = col + 4 * (s & 3);
-    const char* p0 = t + tile_off<2, COLS>(r, c >> 3) + (c & 7) * 2;
-    const char* p1 = t + tile_off<2, COLS>(r + 4, c >> 3) + (c & 7) * 2;
+  static __device__ __forceinline__ Along along(const char* t, int base, int row, int col) {
+    return *reinterpret_cast<const bf16x8*>(t + row * COLS * 2 + (base ^ (col * 2)));
+  }
+  struct Base {
+    int lo, hi;  // rows 8 g + 0 .. 3 and + 4 .. 7
+  };
+  template <int COLS>
+  static __device__ __forceinline__ Base base_across() {
+    const int lane = threadIdx.x & 63, s = lane & 15, r = 8 * (lane >> 4) + (s >> 2), c = 4 * (s & 3);
+    return {tile_off<2, COLS>(r, c >> 3) + (c & 7) * 2, tile_off<2, COLS>(r + 4, c >> 3) + (c & 7) * 2};
+  }
+  template <int COLS>
+  static __device__ __forceinline__ Across across(const char* t, Base base, int row, int col) {
+    const char* p0 = t + row * COLS * 2 + (base.lo ^ (col * 2));
+    const char* p1 = t + row * COLS * 2 + (base.hi ^ (col * 2));
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p0));
     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p1));
-    bf16x8 o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      o[e] = __builtin_bit_cast(bf16x4, lo)[e];
-      o[e + 4] = __builtin_bit_cast(bf16x4, hi)[e];
-    }
-    return o;
+    return __builtin_shufflevector(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
   }
+  // The four columns 4 g .. of a row, 16 rows: how a lane holds a product's block.
+  template <int COLS>
+  static __device__ __forceinline__ int base_block() {
+    const int g = (threadIdx.x >> 4) & 3;
+    return tile_off<2, COLS>(threadIdx.x & 15, g >> 1) + (g & 1) * 8;
+  }
+  template <int COLS>
+  static __device__ __forceinline__ bf16x4* block(char* t, int base, int row, int col) {
+    return reinterpret_cast<bf16x4*>(t + row * COLS * 2 + (base ^ (col * 2)));
+  }
+  static __device__ __forceinline__ bf16x4 round(f32x4 v) { return __builtin_convertvector(v, bf16x4); }
   static __device__ __forceinline__ f32x4 mma(Across a, Across b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
@@ -138,109 +158,179 @@ struct Ops<float> {
   using Across = float;
   static constexpr int ALONG = 16, ACROSS = 4;
   template <int COLS>
-  static __device__ __forceinline__ Along along(const char* t, int row, int col) {
-    const int lane = threadIdx.x & 63;
-    return *reinterpret_cast<const f32x4*>(t + tile_off<4, COLS>(row + (lane & 15), (col >> 2) + (lane >> 4)));
+  static __device__ __forceinline__ int base_along() {
+    return tile_off<4, COLS>(threadIdx.x & 15, (threadIdx.x >> 4) & 3);
   }
   template <int COLS>
-  static __device__ __forceinline__ Across across(const char* t, int row, int col) {
-    const int lane = threadIdx.x & 63;
-    const int r = row + (lane >> 4), c = col + (lane & 15);
-    return *reinterpret_cast<const float*>(t + tile_off<4, COLS>(r, c >> 2) + (c & 3) * 4);
+  static __device__ __forceinline__ Along along(const char* t, int base, int row, int col) {
+    return *reinterpret_cast<const f32x4*>(t + row * COLS * 4 + (base ^ (col * 4)));
   }
+  using Base = int;
+  template <int COLS>
+  static __device__ __forceinline__ Base base_across() {
+    const int lane = threadIdx.x & 63;
+    return tile_off<4, COLS>(lane >> 4, (lane & 15) >> 2) + (lane & 3) * 4;
+  }
+  template <int COLS>
+  static __device__ __forceinline__ Across across(const char* t, Base base, int row, int col) {
+    return *reinterpret_cast<const float*>(t + row * COLS * 4 + (base ^ (col * 4) ^ (((row >> 2) & 3) << 4)));
+  }
+  template <int COLS>
+  static __device__ __forceinline__ int base_block() {
+    return base_along<COLS>();
+  }
+  template <int COLS>
+  static __device__ __forceinline__ f32x4* block(char* t, int base, int row, int col) {
+    return reinterpret_cast<f32x4*>(t + row * COLS * 4 + (base ^ (col * 4)));
+  }
+  static __device__ __forceinline__ f32x4 round(f32x4 v) { return v; }
   static __device__ __forceinline__ f32x4 mma(Across a, Across b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
   }
 };
 
-// A thread's share of a [D][64] tile on its way from memory: rows past `rows` and
-// tokens past L are zero, and nothing past them is read.
-template <typename T, int D>
+// A thread's share of a [D][64] tile on its way from memory. Rows past `rows` and
+// tokens past L are zero. In a last, partial chunk the 16 bytes of a lane may reach
+// past its tokens: they are read from where they end with the tensor at the latest,
+// moved into place and cut, so that no lane reads outside the tensor and none waits
+// for element loads.
+template <typename T, int D, int NT>
 struct TileRegs {
-  static constexpr int ES = sizeof(T), EPC = 16 / ES, CPR = kChunk * ES / 16, PER = D * CPR / 256;
+  static constexpr int ES = sizeof(T), EPC = 16 / ES, CPR = kChunk * ES / 16, PER = D * CPR / NT, RPI = NT / CPR;
+  static_assert(D * CPR % NT == 0, "whole rounds");
   u32x4 v[PER];
 
-  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int L) {
+  // base: the chunk's first token of row 0; first, end: the tensor
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int L, const T* first, const T* end) {
+    const int r = threadIdx.x / CPR, c = threadIdx.x % CPR;
+    const char* p = reinterpret_cast<const char*>(base + r * ld + c * EPC);
+    const int64_t step = RPI * ld * ES;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = u32x4{0u, 0u, 0u, 0u};
+    if (L == kChunk) {  // uniform
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (r + i * RPI < rows) v[i] = load16_any<ES>(p + i * step);
+      return;
+    }
+    const int n = L - c * EPC;  // tokens of the lane
+    if (end - first < EPC) {    // uniform: a tensor of less than 16 bytes
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (r + i * RPI < rows) v[i] = load16_part<ES>(p + i * step, n);
+      return;
+    }
+    const char* last = reinterpret_cast<const char*>(end) - 16;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (r + i * RPI < rows && n > 0) v[i] = load16_any<ES>(p + i * step < last ? p + i * step : last);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = i * 256 + threadIdx.x, r = at / CPR, c = at % CPR;
-      const int n = r < rows ? L - c * EPC : 0;
-      const char* p = reinterpret_cast<const char*>(base + r * ld + c * EPC);
-      if (n >= EPC)
-        v[i] = load16_any<ES>(p);
-      else
-        v[i] = load16_part<ES>(p, n);
+      const int64_t past = p + i * step - last;
+      const int s = past > 0 && n > 0 && r + i * RPI < rows ? static_cast<int>(past) * 8 : 0;  // bits, < 128
+      uint64_t lo = v[i][0] | static_cast<uint64_t>(v[i][1]) << 32, hi = v[i][2] | static_cast<uint64_t>(v[i][3]) << 32;
+      if (s >= 64) lo = hi, hi = 0;
+      const int q = s & 63;
+      if (q) lo = lo >> q | hi << (64 - q), hi >>= q;
+      const int keep = n * ES * 8;  // bits
+      lo = keep >= 64 ? lo : keep > 0 ? lo & ((uint64_t{1} << keep) - 1) : 0;
+      hi = keep >= 128 ? hi : keep > 64 ? hi & ((uint64_t{1} << (keep - 64)) - 1) : 0;
+      v[i] = u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi),
+                   static_cast<uint32_t>(hi >> 32)};
     }
   }
   __device__ __forceinline__ void store(char* lds) const {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = i * 256 + threadIdx.x;
+      const int at = i * NT + threadIdx.x;
       *reinterpret_cast<u32x4*>(lds + tile_off<ES, kChunk>(at / CPR, at % CPR)) = v[i];
     }
   }
 };
 
-// fp32 as three bf16 that add up to it.
-__device__ __forceinline__ void split3(float f, bf16& a, bf16& b, bf16& c) {
-  a = static_cast<bf16>(f);
-  const float r = f - static_cast<float>(a);
-  b = static_cast<bf16>(r);
-  c = static_cast<bf16>(r - static_cast<float>(b));
+// Eight fp32 as N bf16 each that add up to it (N = 3: to its 24 bits; 2: to 17).
+template <int N>
+__device__ __forceinline__ void split(const float (&f)[8], bf16x8 (&s)[N]) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    f32x2 v = {f[e], f[e + 1]};
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      const bf16x2 h = __builtin_convertvector(v, bf16x2);
+      s[q][e] = h[0], s[q][e + 1] = h[1];
+      if (q + 1 < N) v[0] -= static_cast<float>(h[0]), v[1] -= static_cast<float>(h[1]);
+    }
+  }
 }
 
-template <typename T_, int YD_, int WD_, bool REV_, bool OUT_, bool PART_>
+template <typename T_, int YD_, int WD_, bool REV_, bool OUT_, bool PART_, int PARTS_ = 3>
 struct Mix {
   using T = T_;
   static constexpr int YD = YD_, WD = WD_;  // rows of x and y, of w, as padded
   static constexpr bool REV = REV_;
   static constexpr bool OUT = OUT_;    // outputs (else the states of segments only)
   static constexpr bool PART = PART_;  // outputs in fp32, to be added over the heads that share a row
+  static constexpr int PARTS = PARTS_;  // bf16 parts of y': 3, or 2 where the state ends in outputs only
   static constexpr int ES = sizeof(T), OS = PART ? 4 : ES;
-  static constexpr int YB = YD / 64, WB = WD / 16;  // 16-blocks: of a wave's part of y rows, of w rows
+  // a wave for each 16 rows of y (its part of the state); for the outputs, of which
+  // there are four blocks of 16 tokens, eight waves share the rows of w by halves
+  static constexpr int NW = YD / 16, NT = 64 * NW, HALVES = NW / 4;
+  static constexpr int WB = WD / 16, OB = WB / HALVES;  // 16-blocks of w rows: all, and a wave's
   static constexpr int XT = YD * kChunk * ES, WT = WD * kChunk * ES;
   static constexpr int ST = YD * WD * ES, OT = WD * kChunk * OS;
+  static constexpr int MINW = 2;
   static constexpr int LDS = OUT ? 2 * XT + WT + (ST > OT ? ST : OT) : XT + WT;
 };
 
-// The state's accumulators of a wave: 16 rows of y in a block (lane % 16), of which
-// wave wv holds blocks wv * YB .., by 16 rows of w (4 (lane / 16) + r).
+// The state's accumulators of a wave: its 16 rows of y (lane % 16) by blocks of 16
+// rows of w (4 (lane / 16) + r).
 template <class M>
 struct State {
-  f32x4 a[M::WB][M::YB];
-  __device__ __forceinline__ int y(int wv, int b) const { return (wv * M::YB + b) * 16 + (threadIdx.x & 15); }
+  f32x4 a[M::WB];
+  __device__ __forceinline__ int y(int wv) const { return wv * 16 + (threadIdx.x & 15); }
   __device__ __forceinline__ int w(int b) const { return b * 16 + 4 * ((threadIdx.x >> 4) & 3); }
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < M::WB; ++i)
-#pragma unroll
-      for (int j = 0; j < M::YB; ++j) a[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < M::WB; ++i) a[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   // a state of the caller's: [ydim][wdim] or its transpose; w0: first row of w of this tile
   template <bool STORE>
   __device__ __forceinline__ void given(float* p, const MixArgs& g, int wv, int w0) {
+    const int yr = y(wv);
+    if (yr >= g.ydim) return;
+    if (!g.s_trans && g.wdim % 4 == 0) {  // 16 bytes of a row (states are 16-byte aligned)
+#pragma unroll
+      for (int i = 0; i < M::WB; ++i) {
+        const int wr = w0 + w(i);
+        f32x4* at = reinterpret_cast<f32x4*>(p + yr * g.wdim + wr);
+        if (wr < g.wdim) {
+          if constexpr (STORE) *at = a[i];
+          else a[i] = *at;
+        }
+      }
+      return;
+    }
+    const int ys = g.s_trans ? 1 : g.wdim, ws = g.s_trans ? g.ydim : 1;
 #pragma unroll
     for (int i = 0; i < M::WB; ++i)
 #pragma unroll
-      for (int j = 0; j < M::YB; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int yr = y(wv, j), wr = w0 + w(i) + r;
-          if (yr < g.ydim && wr < g.wdim) {
-            float* at = p + (g.s_trans ? wr * g.ydim + yr : yr * g.wdim + wr);
-            if constexpr (STORE) *at = a[i][j][r];
-            else a[i][j][r] = *at;
-          }
+      for (int r = 0; r < 4; ++r) {
+        const int wr = w0 + w(i) + r;
+        float* at = p + yr * ys + wr * ws;
+        if (wr < g.wdim) {
+          if constexpr (STORE) *at = a[i][r];
+          else a[i][r] = *at;
         }
+      }
   }
   // a segment's, in the accumulators' own order
-  __device__ __forceinline__ f32x4* place(float* p, int wv, int i, int j) const {
-    return reinterpret_cast<f32x4*>(p) + ((wv * M::WB + i) * M::YB + j) * 64 + (threadIdx.x & 63);
+  __device__ __forceinline__ f32x4* place(float* p, int wv, int i) const {
+    return reinterpret_cast<f32x4*>(p) + (wv * M::WB + i) * 64 + (threadIdx.x & 63);
   }
 };
 
 template <class M>
-__global__ void __launch_bounds__(256) mix_kernel(MixArgs g) {
+__global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   using T = typename M::T;
   using O = Ops<T>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -272,9 +362,7 @@ __global__ void __launch_bounds__(256) mix_kernel(MixArgs g) {
   if (M::OUT) {
     if (g.nseg > 1) {
 #pragma unroll
-      for (int i = 0; i < M::WB; ++i)
-#pragma unroll
-        for (int j = 0; j < M::YB; ++j) st.a[i][j] = *st.place(segp, wv, i, j);
+      for (int i = 0; i < M::WB; ++i) st.a[i] = *st.place(segp, wv, i);
       have = true;
     } else if (g.s0) {
       st.template given<false>(const_cast<float*>(g.s0) + hs * sdim, g, wv, w0);
@@ -286,20 +374,69 @@ __global__ void __launch_bounds__(256) mix_kernel(MixArgs g) {
   auto rows = [&](const void* p, int shared, int dim) {
     return static_cast<const T*>(p) + (static_cast<int64_t>(shared ? head / g.group : head) * dim) * ld + sp.first;
   };
+  auto end = [&](const void* p, int shared, int dim) {
+    return static_cast<const T*>(p) + (static_cast<int64_t>(shared ? g.heads / g.group : g.heads) * dim) * ld;
+  };
   const T* xp = M::OUT ? rows(g.x, g.x_shared, g.ydim) : nullptr;
   const T* yp = rows(g.y, g.y_shared, g.ydim);
   const T* wp = rows(g.w, g.w_shared, g.wdim) + w0 * ld;
 
+  const int at_along = O::template base_along<kChunk>(), at_block = O::template base_block<kChunk>();
+  const int at_state = O::template base_block<M::WD>();
+  const auto at_cols = O::template base_across<kChunk>();
+  auto at_scols = O::template base_across<M::WD>();
+  // the wave's 16 columns: part of the lane's address, since they differ by wave
+  using OutOps = Ops<typename std::conditional<M::PART, float, T>::type>;
+  auto at_icols = at_cols;
+  const int ic = (wv & 3) * 16 * M::ES, sc = M::HALVES > 1 ? (wv >> 2) * (M::WD / 2) * M::ES : 0;
+  if constexpr (M::ES == 2) at_icols.lo ^= ic, at_icols.hi ^= ic, at_scols.lo ^= sc, at_scols.hi ^= sc;
+  else at_icols ^= ic, at_scols ^= sc;
+  const int at_out = OutOps::template base_block<kChunk>() ^ ((wv & 3) * 16 * M::OS);
+
   const int nchunk = (t1 - t0 + kChunk - 1) / kChunk;
   auto first_of = [&](int c) { return t0 + (M::REV ? nchunk - 1 - c : c) * kChunk; };
-  TileRegs<T, M::YD> xr, yr;
-  TileRegs<T, M::WD> wr;
+  TileRegs<T, M::YD, M::NT> xr, yr;
+  TileRegs<T, M::WD, M::NT> wr;
   auto fetch = [&](int c) {
     const int t = first_of(c), L = min(kChunk, t1 - t);
-    if (M::OUT) xr.load(xp + t, ld, g.ydim, L);
-    yr.load(yp + t, ld, g.ydim, L);
-    wr.load(wp + t, ld, wrows, L);
+    if (M::OUT)
+      xr.load(xp + t, ld, g.ydim, L, static_cast<const T*>(g.x), end(g.x, g.x_shared, g.ydim));
+    yr.load(yp + t, ld, g.ydim, L, static_cast<const T*>(g.y), end(g.y, g.y_shared, g.ydim));
+    wr.load(wp + t, ld, wrows, L, static_cast<const T*>(g.w), end(g.w, g.w_shared, g.wdim));
   };
+  // The weights, of a lane: those of the inner products (its token i, the tokens j =
+  // 16 jb + 4 grp + r), of x R (tokens 16 ib + 4 grp + r) and of y' (of each step's
+  // tokens). Only the last two know the chunk's length: they change for a partial one.
+  constexpr int NA = 16 / M::ES;  // tokens of a lane in a step of the state's product
+  const int ib = wv & 3, grp = lane >> 4;
+  f32x4 pw[M::OUT ? 4 : 1], wx;
+  float fy[kChunk / O::ALONG][NA];
+  if constexpr (M::OUT) {
+#pragma unroll
+    for (int jb = 0; jb < 4; ++jb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int n = (M::REV ? -1 : 1) * (16 * (ib - jb) + (lane & 15) - 4 * grp - r);
+        pw[jb][r] = n >= 0 ? g.cp * a.pow(n) : 0.0f;
+      }
+  }
+  auto weigh = [&](int L) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = 16 * ib + 4 * grp + r;
+      wx[r] = g.cx * a.pow(max(M::REV ? L - 1 - i : i + 1, 0));
+    }
+#pragma unroll
+    for (int k = 0; k < kChunk / O::ALONG; ++k)
+#pragma unroll
+      for (int e = 0; e < NA; ++e) {
+        const int tok = k * O::ALONG + NA * grp + e;
+        fy[k][e] = g.cy * a.pow(M::REV ? tok + 1 : max(L - 1 - tok, 0));
+      }
+  };
+  int weighed = kChunk;
+  weigh(kChunk);
+
   if (nchunk > 0) fetch(0);
   for (int c = 0; c < nchunk; ++c) {
     const int t = first_of(c), L = min(kChunk, t1 - t);
@@ -310,152 +447,100 @@ __global__ void __launch_bounds__(256) mix_kernel(MixArgs g) {
       if (have) {
 #pragma unroll
         for (int i = 0; i < M::WB; ++i)
-#pragma unroll
-          for (int j = 0; j < M::YB; ++j) {
-            const int r = st.y(wv, j), cc = st.w(i);
-            char* p = S + tile_off<M::ES, M::WD>(r, cc * M::ES / 16);
-            if constexpr (M::ES == 4) {
-              *reinterpret_cast<f32x4*>(p) = st.a[i][j];
-            } else {
-              bf16x4 b;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) b[e] = static_cast<bf16>(st.a[i][j][e]);
-              *reinterpret_cast<bf16x4*>(p + (cc & 7) * 2) = b;
-            }
-          }
+          *O::template block<M::WD>(S + wv * 16 * M::WD * M::ES, at_state, 0, 16 * i) = O::round(st.a[i]);
       }
     }
     __syncthreads();
     if (c + 1 < nchunk) fetch(c + 1);
+    if (L != weighed) weigh(weighed = L);
     if constexpr (M::OUT) {
-      // outputs of 16 tokens i: out[w][i] = sum_y R[y][w] x[y][i], weighted, plus the chunk's own
-      const int i0 = wv * 16, i = i0 + (lane & 15), grp = lane >> 4;
-      f32x4 acc[M::WB];
+      // outputs of 16 tokens i: out[i][w] = sum_y x[y][i] R[y][w], weighted, plus the chunk's own.
+      // A lane of p holds token i = i0 + lane % 16 and tokens j = 16 jb + 4 grp + r; one of acc
+      // tokens i = i0 + 4 grp + r and row w = 16 b + lane % 16. A token that is not finite
+      // spoils its chunk's other outputs: weights of 0 do not keep it from them.
+      const int b0 = M::HALVES > 1 ? (wv >> 2) * M::OB : 0, i0 = ib * 16;
+      char* Wo = W + b0 * 16 * kChunk * M::ES;
+      f32x4 acc[M::OB];
 #pragma unroll
-      for (int b = 0; b < M::WB; ++b) acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      f32x4 p[4];
-#pragma unroll
-      for (int jb = 0; jb < 4; ++jb) p[jb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int b = 0; b < M::OB; ++b) acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       if (i0 < L) {
-#pragma unroll 4
+        f32x4 p[4];
+#pragma unroll
+        for (int jb = 0; jb < 4; ++jb) p[jb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
         for (int k = 0; k < M::YD; k += O::ACROSS) {
-          const auto xf = O::template across<kChunk>(X, k, i0);
+          const auto xf = O::template across<kChunk>(X, at_icols, k, 0);
           if (have) {
 #pragma unroll
-            for (int b = 0; b < M::WB; ++b) acc[b] = O::mma(O::template across<M::WD>(S, k, 16 * b), xf, acc[b]);
+            for (int b = 0; b < M::OB; ++b) acc[b] = O::mma(xf, O::template across<M::WD>(S, at_scols, k, 16 * b), acc[b]);
           }
 #pragma unroll
           for (int jb = 0; jb < 4; ++jb)
-            if (M::REV ? jb >= wv : jb <= wv) p[jb] = O::mma(O::template across<kChunk>(Y, k, 16 * jb), xf, p[jb]);
+            if (M::REV ? jb >= ib : jb <= ib) p[jb] = O::mma(O::template across<kChunk>(Y, at_cols, k, 16 * jb), xf, p[jb]);
         }
-        const float wx = g.cx * a.pow(max(M::REV ? L - 1 - i : i + 1, 0));
+        if (have) {
 #pragma unroll
-        for (int b = 0; b < M::WB; ++b) acc[b] *= wx;
+          for (int b = 0; b < M::OB; ++b) acc[b] *= wx;
+        }
 #pragma unroll
-        for (int jb = 0; jb < 4; ++jb)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int n = M::REV ? jb * 16 + 4 * grp + r - i : i - (jb * 16 + 4 * grp + r);
-            p[jb][r] = n >= 0 ? p[jb][r] * (g.cp * a.pow(max(n, 0))) : 0.0f;
-          }
+        for (int jb = 0; jb < 4; ++jb) p[jb] *= pw[jb];
         if constexpr (M::ES == 2) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {  // 32 tokens j
-            if (M::REV ? 2 * h + 1 < wv : 2 * h > wv) continue;
-            bf16x8 pf;
+            if (M::REV ? 2 * h + 1 < ib : 2 * h > ib) continue;
+            const bf16x8 pf = __builtin_shufflevector(O::round(p[2 * h]), O::round(p[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              pf[r] = static_cast<bf16>(p[2 * h][r]);
-              pf[r + 4] = static_cast<bf16>(p[2 * h + 1][r]);
-            }
-#pragma unroll
-            for (int b = 0; b < M::WB; ++b) {
-              const int row = 16 * b + (lane & 15), col = 32 * h + 4 * grp;
-              const bf16x4 lo = *reinterpret_cast<const bf16x4*>(W + tile_off<2, kChunk>(row, col >> 3) + (col & 7) * 2);
-              const bf16x4 hi =
-                  *reinterpret_cast<const bf16x4*>(W + tile_off<2, kChunk>(row, (col + 16) >> 3) + (col & 7) * 2);
-              bf16x8 wf;
-#pragma unroll
-              for (int r = 0; r < 4; ++r) wf[r] = lo[r], wf[r + 4] = hi[r];
-              acc[b] = O::mma(wf, pf, acc[b]);
+            for (int b = 0; b < M::OB; ++b) {
+              const bf16x4 lo = *O::template block<kChunk>(Wo, at_block, 16 * b, 32 * h);
+              const bf16x4 hi = *O::template block<kChunk>(Wo, at_block, 16 * b, 32 * h + 16);
+              acc[b] = O::mma(pf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), acc[b]);
             }
           }
         } else {
 #pragma unroll
           for (int jb = 0; jb < 4; ++jb) {
-            if (M::REV ? jb < wv : jb > wv) continue;
+            if (M::REV ? jb < ib : jb > ib) continue;
 #pragma unroll
-            for (int b = 0; b < M::WB; ++b) {
-              const auto wf = O::template along<kChunk>(W, 16 * b, 16 * jb);
+            for (int b = 0; b < M::OB; ++b) {
+              const auto wf = O::template along<kChunk>(Wo, at_along, 16 * b, 16 * jb);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) acc[b] = O::mma(wf[r], p[jb][r], acc[b]);
+              for (int r = 0; r < 4; ++r) acc[b] = O::mma(p[jb][r], wf[r], acc[b]);
             }
           }
         }
       }
       __syncthreads();  // no wave reads X or S any more
-      using OutT = typename std::conditional<M::PART, float, T>::type;
 #pragma unroll
-      for (int b = 0; b < M::WB; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 16 * b + 4 * grp + r;
-          *reinterpret_cast<OutT*>(S + tile_off<M::OS, kChunk>(row, i * M::OS / 16) + (i * M::OS & 15)) =
-              from_f32<OutT>(acc[b][r]);
-        }
+      for (int b = 0; b < M::OB; ++b)
+        *OutOps::template block<kChunk>(S + b0 * 16 * kChunk * M::OS, at_out, 16 * b, 0) = OutOps::round(acc[b]);
     }
     // the state past this chunk
     {
       const float aL = a.pow(L);
 #pragma unroll
-      for (int i = 0; i < M::WB; ++i)
-#pragma unroll
-        for (int j = 0; j < M::YB; ++j) st.a[i][j] *= aL;
-      const int grp = lane >> 4;
+      for (int i = 0; i < M::WB; ++i) st.a[i] *= aL;
+      char* Yw = Y + wv * 16 * kChunk * M::ES;
 #pragma unroll
       for (int k = 0; k < kChunk; k += O::ALONG) {
-        constexpr int N = 16 / M::ES;  // tokens of a lane
-        float f[N];
+        const auto yf = O::template along<kChunk>(Yw, at_along, 0, k);
+        float f[NA];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const int tok = k + N * grp + e;
-          f[e] = g.cy * a.pow(M::REV ? tok + 1 : max(L - 1 - tok, 0));
-        }
+        for (int e = 0; e < NA; ++e) f[e] = static_cast<float>(yf[e]) * fy[k / O::ALONG][e];
         if constexpr (M::ES == 2) {
-          bf16x8 y3[M::YB][3];
-#pragma unroll
-          for (int j = 0; j < M::YB; ++j) {
-            const bf16x8 yf = O::template along<kChunk>(Y, (wv * M::YB + j) * 16, k);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-              bf16 s0, s1, s2;
-              split3(static_cast<float>(yf[e]) * f[e], s0, s1, s2);
-              y3[j][0][e] = s0, y3[j][1][e] = s1, y3[j][2][e] = s2;
-            }
-          }
+          bf16x8 ys[M::PARTS];
+          split(f, ys);
 #pragma unroll
           for (int i = 0; i < M::WB; ++i) {
-            const bf16x8 wf = O::template along<kChunk>(W, 16 * i, k);
+            const bf16x8 wf = O::template along<kChunk>(W, at_along, 16 * i, k);
 #pragma unroll
-            for (int j = 0; j < M::YB; ++j)
-#pragma unroll
-              for (int q = 2; q >= 0; --q) st.a[i][j] = O::mma(wf, y3[j][q], st.a[i][j]);
+            for (int q = M::PARTS - 1; q >= 0; --q) st.a[i] = O::mma(wf, ys[q], st.a[i]);
           }
         } else {
-          f32x4 yf[M::YB];
-#pragma unroll
-          for (int j = 0; j < M::YB; ++j) {
-            yf[j] = O::template along<kChunk>(Y, (wv * M::YB + j) * 16, k);
-#pragma unroll
-            for (int e = 0; e < N; ++e) yf[j][e] *= f[e];
-          }
 #pragma unroll
           for (int i = 0; i < M::WB; ++i) {
-            const f32x4 wf = O::template along<kChunk>(W, 16 * i, k);
+            const f32x4 wf = O::template along<kChunk>(W, at_along, 16 * i, k);
 #pragma unroll
-            for (int j = 0; j < M::YB; ++j)
-#pragma unroll
-              for (int e = 0; e < N; ++e) st.a[i][j] = O::mma(wf[e], yf[j][e], st.a[i][j]);
+            for (int e = 0; e < NA; ++e) st.a[i] = O::mma(wf[e], f[e], st.a[i]);
           }
         }
       }
@@ -468,8 +553,8 @@ __global__ void __launch_bounds__(256) mix_kernel(MixArgs g) {
       OutT* op = static_cast<OutT*>(g.out) + (static_cast<int64_t>(head) * g.wdim + w0) * ld + sp.first + t;
       typedef u32x4 u32x4_any __attribute__((aligned(2), may_alias));
 #pragma unroll
-      for (int q = 0; q < M::WD * CPR / 256; ++q) {
-        const int at = q * 256 + threadIdx.x, r = at / CPR, cc = at % CPR, n = L - cc * EPC;
+      for (int q = 0; q < M::WD * CPR / M::NT; ++q) {
+        const int at = q * M::NT + threadIdx.x, r = at / CPR, cc = at % CPR, n = L - cc * EPC;
         if (r >= wrows || n <= 0) continue;
         const u32x4 v = *reinterpret_cast<const u32x4*>(S + tile_off<M::OS, kChunk>(r, cc));
         OutT* p = op + r * ld + cc * EPC;
@@ -489,9 +574,7 @@ __global__ void __launch_bounds__(256) mix_kernel(MixArgs g) {
   }
   if (!M::OUT) {
 #pragma unroll
-    for (int i = 0; i < M::WB; ++i)
-#pragma unroll
-      for (int j = 0; j < M::YB; ++j) *st.place(segp, wv, i, j) = st.a[i][j];
+    for (int i = 0; i < M::WB; ++i) *st.place(segp, wv, i) = st.a[i];
   } else if (g.nseg == 1 && g.sT) {
     st.template given<true>(g.sT + hs * sdim, g, wv, w0);
   }
@@ -508,8 +591,8 @@ __global__ void __launch_bounds__(256) mix_scan_kernel(MixArgs g) {
   const Span sp = span_of(g, seq);
   const Decay a(g.decay[head]);
   const int at = blockIdx.y * 256 + threadIdx.x;  // of YD * WD / 4
-  const int lane = at & 63, j = (at >> 6) % M::YB, i = (at >> 6) / M::YB % M::WB, wv = (at >> 6) / M::YB / M::WB;
-  const int yr = (wv * M::YB + j) * 16 + (lane & 15), wr = wt * M::WD + i * 16 + 4 * (lane >> 4);
+  const int lane = at & 63, i = (at >> 6) % M::WB, wv = (at >> 6) / M::WB;
+  const int yr = wv * 16 + (lane & 15), wr = wt * M::WD + i * 16 + 4 * (lane >> 4);
   const int64_t hs = static_cast<int64_t>(seq) * g.heads + head, sdim = static_cast<int64_t>(g.ydim) * g.wdim;
   auto given = [&](int r) {
     return hs * sdim + (g.s_trans ? static_cast<int64_t>(wr + r) * g.ydim + yr
@@ -692,7 +775,7 @@ hipError_t launch_mix(const MixArgs& g, hipStream_t stream) {
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, M::LDS);
   if (attr != hipSuccess) return attr;
   const unsigned blocks = static_cast<unsigned>(g.n_seqs) * g.heads * g.wtiles * g.nseg;
-  hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), M::LDS, stream, g);
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(M::NT), M::LDS, stream, g);
   return hipGetLastError();
 }
 
@@ -705,8 +788,12 @@ hipError_t run_mix(const MixArgs& g, bool part, hipStream_t stream) {
     hipLaunchKernelGGL(mix_scan_kernel<U>, dim3(g.n_seqs * g.heads * g.wtiles, YD * WD / 1024), dim3(256), 0, stream, g);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  return part ? launch_mix<Mix<T, YD, WD, REV, true, true>>(g, stream)
-              : launch_mix<Mix<T, YD, WD, REV, true, false>>(g, stream);
+  // the segments' states came from the pass above; within one the state ends in outputs only
+  if (g.nseg > 1)
+    return part ? launch_mix<Mix<T, YD, WD, REV, true, true, 2>>(g, stream)
+                : launch_mix<Mix<T, YD, WD, REV, true, false, 2>>(g, stream);
+  return part ? launch_mix<Mix<T, YD, WD, REV, true, true, 3>>(g, stream)
+              : launch_mix<Mix<T, YD, WD, REV, true, false, 3>>(g, stream);
 }
 
 template <typename T, bool REV>
