@@ -189,61 +189,74 @@ struct Ops<float> {
   }
 };
 
-// A thread's share of a [D][64] tile on its way from memory. Rows past `rows` and
-// tokens past L are zero. In a last, partial chunk the 16 bytes of a lane may reach
-// past its tokens: they are read from where they end with the tensor at the latest,
-// moved into place and cut, so that no lane reads outside the tensor and none waits
-// for element loads.
+// A thread's share of a [D][64] tile on its way from memory. Rows past the operand's
+// and tokens past L are zero in LDS; every load is made all the same, of the last
+// row or, in a partial chunk, of whatever follows (branches around the loads would
+// keep them from running together). The 16 bytes that would reach past the tensor
+// itself (of its last rows only) are read again, token by token.
 template <typename T, int D, int NT>
 struct TileRegs {
   static constexpr int ES = sizeof(T), EPC = 16 / ES, CPR = kChunk * ES / 16, PER = D * CPR / NT, RPI = NT / CPR;
   static_assert(D * CPR % NT == 0, "whole rounds");
   u32x4 v[PER];
+  const char* p[PER];  // the thread's bytes at the sequence's first token
+  const char* last;    // where 16 bytes of the tensor may start at the latest
+  const T* base;       // row 0 at the sequence's first token
+  const T* end;
+  int64_t ld;
+  int rows;
 
-  // base: the chunk's first token of row 0; first, end: the tensor
-  __device__ __forceinline__ void load(const T* base, int64_t ld, int rows, int L, const T* first, const T* end) {
+  // base: row 0 at the sequence's first token; first, end: the tensor (of a tensor
+  // below 16 bytes, which starts on 16, the 16 that it starts are read)
+  __device__ __forceinline__ void init(const T* base_, int64_t ld_, int rows_, const T* first, const T* end_) {
+    base = base_, ld = ld_, rows = rows_, end = end_;
+    last = reinterpret_cast<const char*>(end - first < EPC ? first : end - EPC);
     const int r = threadIdx.x / CPR, c = threadIdx.x % CPR;
-    const char* p = reinterpret_cast<const char*>(base + r * ld + c * EPC);
-    const int64_t step = RPI * ld * ES;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) v[i] = u32x4{0u, 0u, 0u, 0u};
-    if (L == kChunk) {  // uniform
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (r + i * RPI < rows) v[i] = load16_any<ES>(p + i * step);
-      return;
-    }
-    const int n = L - c * EPC;  // tokens of the lane
-    if (end - first < EPC) {    // uniform: a tensor of less than 16 bytes
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (r + i * RPI < rows) v[i] = load16_part<ES>(p + i * step, n);
-      return;
-    }
-    const char* last = reinterpret_cast<const char*>(end) - 16;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      if (r + i * RPI < rows && n > 0) v[i] = load16_any<ES>(p + i * step < last ? p + i * step : last);
+      p[i] = reinterpret_cast<const char*>(base + static_cast<int64_t>(min(r + i * RPI, rows - 1)) * ld + c * EPC);
+  }
+  __device__ __forceinline__ void load(int t) {  // a whole chunk
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = load16_any<ES>(p[i] + static_cast<int64_t>(t) * ES);
+  }
+  __device__ __forceinline__ void load_part(int t) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int64_t past = p + i * step - last;
-      const int s = past > 0 && n > 0 && r + i * RPI < rows ? static_cast<int>(past) * 8 : 0;  // bits, < 128
-      uint64_t lo = v[i][0] | static_cast<uint64_t>(v[i][1]) << 32, hi = v[i][2] | static_cast<uint64_t>(v[i][3]) << 32;
-      if (s >= 64) lo = hi, hi = 0;
-      const int q = s & 63;
-      if (q) lo = lo >> q | hi << (64 - q), hi >>= q;
-      const int keep = n * ES * 8;  // bits
-      lo = keep >= 64 ? lo : keep > 0 ? lo & ((uint64_t{1} << keep) - 1) : 0;
-      hi = keep >= 128 ? hi : keep > 64 ? hi & ((uint64_t{1} << (keep - 64)) - 1) : 0;
-      v[i] = u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi),
-                   static_cast<uint32_t>(hi >> 32)};
+      const char* q = p[i] + static_cast<int64_t>(t) * ES;
+      v[i] = load16_any<ES>(q < last ? q : last);
     }
   }
-  __device__ __forceinline__ void store(char* lds) const {
+  __device__ __forceinline__ void store(char* lds, int t, int L) {
+    const int r = threadIdx.x / CPR, c = threadIdx.x % CPR, n = L - c * EPC;
+    if (L < kChunk || rows < D) {  // uniform
+      u32x4 keep;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int m = (n - q * (EPC / 4)) * ES * 8;  // valid bits of the word
+        keep[q] = m >= 32 ? ~0u : m <= 0 ? 0u : 0xffffu;
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) v[i] &= r + i * RPI < rows ? keep : u32x4{0u, 0u, 0u, 0u};
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int at = i * NT + threadIdx.x;
       *reinterpret_cast<u32x4*>(lds + tile_off<ES, kChunk>(at / CPR, at % CPR)) = v[i];
+    }
+    if (L < kChunk && base + t + (rows - 1) * ld + (L + EPC - 1) / EPC * EPC > end) {  // uniform
+#pragma unroll 1
+      for (int i = 0; i < PER; ++i) {
+        const int row = r + i * RPI;
+        if (row >= rows || n <= 0) continue;
+        const T* q = base + t + row * ld + c * EPC;
+        T e[EPC];
+#pragma unroll
+        for (int u = 0; u < EPC; ++u) e[u] = q[u < n ? u : n - 1];
+        T* to = reinterpret_cast<T*>(lds + tile_off<ES, kChunk>(row, c));
+#pragma unroll
+        for (int u = 0; u < EPC; ++u) to[u] = u < n ? e[u] : from_f32<T>(0.0f);
+      }
     }
   }
 };
@@ -279,7 +292,7 @@ struct Mix {
   static constexpr int XT = YD * kChunk * ES, WT = WD * kChunk * ES;
   static constexpr int ST = YD * WD * ES, OT = WD * kChunk * OS;
   static constexpr int MINW = 2;
-  static constexpr int LDS = OUT ? 2 * XT + WT + (ST > OT ? ST : OT) : XT + WT;
+  static constexpr int LDS = OUT ? 2 * XT + WT + ST + OT : XT + WT;
 };
 
 // The state's accumulators of a wave: its 16 rows of y (lane % 16) by blocks of 16
@@ -337,7 +350,8 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   char* Y = smem;
   char* W = Y + M::XT;
   char* X = W + M::WT;
-  char* S = X + M::XT;  // the state as an operand, then the outputs on their way out
+  char* S = X + M::XT;   // the state as an operand
+  char* Out = S + M::ST;  // the outputs on their way out
 
   // workgroup -> segment, tile of w, head, sequence (neighbours on one XCD)
   int id = xcd_position(blockIdx.x, gridDim.x);
@@ -358,15 +372,12 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   const Decay a(g.decay[head]);
   State<M> st;
   st.clear();
-  bool have = false;
   if (M::OUT) {
     if (g.nseg > 1) {
 #pragma unroll
       for (int i = 0; i < M::WB; ++i) st.a[i] = *st.place(segp, wv, i);
-      have = true;
     } else if (g.s0) {
       st.template given<false>(const_cast<float*>(g.s0) + hs * sdim, g, wv, w0);
-      have = true;
     }
   }
 
@@ -375,12 +386,16 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
     return static_cast<const T*>(p) + (static_cast<int64_t>(shared ? head / g.group : head) * dim) * ld + sp.first;
   };
   auto end = [&](const void* p, int shared, int dim) {
-    return static_cast<const T*>(p) + (static_cast<int64_t>(shared ? g.heads / g.group : g.heads) * dim) * ld;
+    const int64_t n = static_cast<int64_t>(shared ? g.heads / g.group : g.heads) * dim * ld;
+    return static_cast<const T*>(p) + n;
   };
-  const T* xp = M::OUT ? rows(g.x, g.x_shared, g.ydim) : nullptr;
-  const T* yp = rows(g.y, g.y_shared, g.ydim);
-  const T* wp = rows(g.w, g.w_shared, g.wdim) + w0 * ld;
-
+  TileRegs<T, M::YD, M::NT> xr, yr;
+  TileRegs<T, M::WD, M::NT> wr;
+  if (M::OUT)
+    xr.init(rows(g.x, g.x_shared, g.ydim), ld, g.ydim, static_cast<const T*>(g.x), end(g.x, g.x_shared, g.ydim));
+  yr.init(rows(g.y, g.y_shared, g.ydim), ld, g.ydim, static_cast<const T*>(g.y), end(g.y, g.y_shared, g.ydim));
+  wr.init(rows(g.w, g.w_shared, g.wdim) + w0 * ld, ld, wrows, static_cast<const T*>(g.w),
+          end(g.w, g.w_shared, g.wdim));
   const int at_along = O::template base_along<kChunk>(), at_block = O::template base_block<kChunk>();
   const int at_state = O::template base_block<M::WD>();
   const auto at_cols = O::template base_across<kChunk>();
@@ -395,14 +410,17 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
 
   const int nchunk = (t1 - t0 + kChunk - 1) / kChunk;
   auto first_of = [&](int c) { return t0 + (M::REV ? nchunk - 1 - c : c) * kChunk; };
-  TileRegs<T, M::YD, M::NT> xr, yr;
-  TileRegs<T, M::WD, M::NT> wr;
   auto fetch = [&](int c) {
-    const int t = first_of(c), L = min(kChunk, t1 - t);
-    if (M::OUT)
-      xr.load(xp + t, ld, g.ydim, L, static_cast<const T*>(g.x), end(g.x, g.x_shared, g.ydim));
-    yr.load(yp + t, ld, g.ydim, L, static_cast<const T*>(g.y), end(g.y, g.y_shared, g.ydim));
-    wr.load(wp + t, ld, wrows, L, static_cast<const T*>(g.w), end(g.w, g.w_shared, g.wdim));
+    const int t = first_of(c);
+    if (t1 - t >= kChunk) {
+      if (M::OUT) xr.load(t);
+      yr.load(t);
+      wr.load(t);
+    } else {
+      if (M::OUT) xr.load_part(t);
+      yr.load_part(t);
+      wr.load_part(t);
+    }
   };
   // The weights, of a lane: those of the inner products (its token i, the tokens j =
   // 16 jb + 4 grp + r), of x R (tokens 16 ib + 4 grp + r) and of y' (of each step's
@@ -434,88 +452,85 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
         fy[k][e] = g.cy * a.pow(M::REV ? tok + 1 : max(L - 1 - tok, 0));
       }
   };
-  int weighed = kChunk;
-  weigh(kChunk);
+  int weighed = -1;
 
+  // The barriers order LDS only: the next chunk's loads and this one's stores stay in flight.
   if (nchunk > 0) fetch(0);
   for (int c = 0; c < nchunk; ++c) {
     const int t = first_of(c), L = min(kChunk, t1 - t);
-    yr.store(Y);
-    wr.store(W);
+    yr.store(Y, t, L);
+    wr.store(W, t, L);
     if constexpr (M::OUT) {
-      xr.store(X);
-      if (have) {
+      xr.store(X, t, L);
 #pragma unroll
-        for (int i = 0; i < M::WB; ++i)
-          *O::template block<M::WD>(S + wv * 16 * M::WD * M::ES, at_state, 0, 16 * i) = O::round(st.a[i]);
-      }
+      for (int i = 0; i < M::WB; ++i)
+        *O::template block<M::WD>(S + wv * 16 * M::WD * M::ES, at_state, 0, 16 * i) = O::round(st.a[i]);
     }
-    __syncthreads();
+    lds_barrier();
     if (c + 1 < nchunk) fetch(c + 1);
     if (L != weighed) weigh(weighed = L);
-    if constexpr (M::OUT) {
+    // The outputs read the state in LDS, the state's update the one in registers: neither
+    // waits for the other.
+    auto outputs = [&]() {
       // outputs of 16 tokens i: out[i][w] = sum_y x[y][i] R[y][w], weighted, plus the chunk's own.
-      // A lane of p holds token i = i0 + lane % 16 and tokens j = 16 jb + 4 grp + r; one of acc
-      // tokens i = i0 + 4 grp + r and row w = 16 b + lane % 16. A token that is not finite
+      // A lane of p holds token i = 16 ib + lane % 16 and tokens j = 16 jb + 4 grp + r; one of acc
+      // tokens i = 16 ib + 4 grp + r and row w = 16 b + lane % 16. A token that is not finite
       // spoils its chunk's other outputs: weights of 0 do not keep it from them.
-      const int b0 = M::HALVES > 1 ? (wv >> 2) * M::OB : 0, i0 = ib * 16;
+      const int b0 = M::HALVES > 1 ? (wv >> 2) * M::OB : 0;
       char* Wo = W + b0 * 16 * kChunk * M::ES;
       f32x4 acc[M::OB];
 #pragma unroll
       for (int b = 0; b < M::OB; ++b) acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (i0 < L) {
-        f32x4 p[4];
+      f32x4 p[4];
 #pragma unroll
-        for (int jb = 0; jb < 4; ++jb) p[jb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int jb = 0; jb < 4; ++jb) p[jb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 0; k < M::YD; k += O::ACROSS) {
-          const auto xf = O::template across<kChunk>(X, at_icols, k, 0);
-          if (have) {
+      for (int k = 0; k < M::YD; k += O::ACROSS) {
+        const auto xf = O::template across<kChunk>(X, at_icols, k, 0);
 #pragma unroll
-            for (int b = 0; b < M::OB; ++b) acc[b] = O::mma(xf, O::template across<M::WD>(S, at_scols, k, 16 * b), acc[b]);
-          }
+        for (int b = 0; b < M::OB; ++b) acc[b] = O::mma(xf, O::template across<M::WD>(S, at_scols, k, 16 * b), acc[b]);
+        if constexpr (M::ES == 2) {  // every block of j: branches would cost more than the products
 #pragma unroll
-          for (int jb = 0; jb < 4; ++jb)
-            if (M::REV ? jb >= ib : jb <= ib) p[jb] = O::mma(O::template across<kChunk>(Y, at_cols, k, 16 * jb), xf, p[jb]);
+          for (int jb = 0; jb < 4; ++jb) p[jb] = O::mma(O::template across<kChunk>(Y, at_cols, k, 16 * jb), xf, p[jb]);
         }
-        if (have) {
+      }
 #pragma unroll
-          for (int b = 0; b < M::OB; ++b) acc[b] *= wx;
-        }
+      for (int b = 0; b < M::OB; ++b) acc[b] *= wx;
+      if constexpr (M::ES == 2) {
 #pragma unroll
-        for (int jb = 0; jb < 4; ++jb) p[jb] *= pw[jb];
-        if constexpr (M::ES == 2) {
+        for (int h = 0; h < 2; ++h) {  // 32 tokens j
+          const bf16x8 pf =
+              __builtin_shufflevector(O::round(p[2 * h] * pw[2 * h]), O::round(p[2 * h + 1] * pw[2 * h + 1]), 0, 1, 2, 3,
+                                      4, 5, 6, 7);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {  // 32 tokens j
-            if (M::REV ? 2 * h + 1 < ib : 2 * h > ib) continue;
-            const bf16x8 pf = __builtin_shufflevector(O::round(p[2 * h]), O::round(p[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-            for (int b = 0; b < M::OB; ++b) {
-              const bf16x4 lo = *O::template block<kChunk>(Wo, at_block, 16 * b, 32 * h);
-              const bf16x4 hi = *O::template block<kChunk>(Wo, at_block, 16 * b, 32 * h + 16);
-              acc[b] = O::mma(pf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), acc[b]);
-            }
+          for (int b = 0; b < M::OB; ++b) {
+            const bf16x4 lo = *O::template block<kChunk>(Wo, at_block, 16 * b, 32 * h);
+            const bf16x4 hi = *O::template block<kChunk>(Wo, at_block, 16 * b, 32 * h + 16);
+            acc[b] = O::mma(pf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), acc[b]);
           }
-        } else {
+        }
+      } else {
 #pragma unroll
-          for (int jb = 0; jb < 4; ++jb) {
-            if (M::REV ? jb < ib : jb > ib) continue;
+        for (int jb = 0; jb < 4; ++jb) {
+          if (M::REV ? jb < ib : jb > ib) continue;
 #pragma unroll
-            for (int b = 0; b < M::OB; ++b) {
-              const auto wf = O::template along<kChunk>(Wo, at_along, 16 * b, 16 * jb);
+          for (int k = 0; k < M::YD; k += O::ACROSS)
+            p[jb] = O::mma(O::template across<kChunk>(Y, at_cols, k, 16 * jb),
+                           O::template across<kChunk>(X, at_icols, k, 0), p[jb]);
+          p[jb] *= pw[jb];
 #pragma unroll
-              for (int r = 0; r < 4; ++r) acc[b] = O::mma(p[jb][r], wf[r], acc[b]);
-            }
+          for (int b = 0; b < M::OB; ++b) {
+            const auto wf = O::template along<kChunk>(Wo, at_along, 16 * b, 16 * jb);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[b] = O::mma(p[jb][r], wf[r], acc[b]);
           }
         }
       }
-      __syncthreads();  // no wave reads X or S any more
 #pragma unroll
       for (int b = 0; b < M::OB; ++b)
-        *OutOps::template block<kChunk>(S + b0 * 16 * kChunk * M::OS, at_out, 16 * b, 0) = OutOps::round(acc[b]);
-    }
-    // the state past this chunk
-    {
+        *OutOps::template block<kChunk>(Out + b0 * 16 * kChunk * M::OS, at_out, 16 * b, 0) = OutOps::round(acc[b]);
+    };
+    auto update = [&]() {  // the state past this chunk
       const float aL = a.pow(L);
 #pragma unroll
       for (int i = 0; i < M::WB; ++i) st.a[i] *= aL;
@@ -544,9 +559,10 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
           }
         }
       }
-      have = true;
-    }
-    __syncthreads();  // the outputs are whole; no wave reads Y or W any more
+    };
+    if constexpr (M::OUT) outputs();
+    update();
+    lds_barrier();  // the outputs are whole; no wave reads the tiles or the state any more
     if (M::OUT && g.out) {
       constexpr int EPC = 16 / M::OS, CPR = kChunk * M::OS / 16;
       using OutT = typename std::conditional<M::PART, float, T>::type;
@@ -556,20 +572,16 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
       for (int q = 0; q < M::WD * CPR / M::NT; ++q) {
         const int at = q * M::NT + threadIdx.x, r = at / CPR, cc = at % CPR, n = L - cc * EPC;
         if (r >= wrows || n <= 0) continue;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(S + tile_off<M::OS, kChunk>(r, cc));
+        const u32x4 v = *reinterpret_cast<const u32x4*>(Out + tile_off<M::OS, kChunk>(r, cc));
         OutT* p = op + r * ld + cc * EPC;
         if (n >= EPC) {
           *reinterpret_cast<u32x4_any*>(p) = v;
         } else {
-          const OutT* e = reinterpret_cast<const OutT*>(&v);
-#pragma unroll
-          for (int u = 0; u < EPC; ++u)
-            if (u < n) p[u] = e[u];
+          const OutT* e = reinterpret_cast<const OutT*>(Out + tile_off<M::OS, kChunk>(r, cc));
+#pragma unroll 1
+          for (int u = 0; u < n; ++u) p[u] = e[u];
         }
       }
-    }
-    if constexpr (M::OUT) {
-      if (c + 1 < nchunk) __syncthreads();  // the next chunk's state goes where the outputs were
     }
   }
   if (!M::OUT) {
@@ -605,14 +617,22 @@ __global__ void __launch_bounds__(256) mix_scan_kernel(MixArgs g) {
       if (yr < g.ydim && wr + r < g.wdim) run[r] = g.s0[given(r)];
   }
   f32x4* p = reinterpret_cast<f32x4*>(g.seg) + (hs * g.wtiles + wt) * g.nseg * (M::YD * M::WD / 4) + at;
-  for (int q = 0; q < g.nseg; ++q) {
-    const int seg = M::REV ? g.nseg - 1 - q : q;
-    const int len = min(sp.len - seg * g.seg_len, g.seg_len);
-    if (len <= 0) continue;
-    f32x4* s = p + static_cast<int64_t>(seg) * (M::YD * M::WD / 4);
-    const f32x4 u = *s;
-    *s = run;
-    run = run * a.pow(len) + u;
+  constexpr int AHEAD = 4;  // segments read ahead: their states do not wait for each other
+  for (int q0 = 0; q0 < g.nseg; q0 += AHEAD) {
+    f32x4 u[AHEAD];
+    auto seg_of = [&](int q) { return M::REV ? g.nseg - 1 - q : q; };
+    auto len_of = [&](int q) { return q < g.nseg ? min(sp.len - seg_of(q) * g.seg_len, g.seg_len) : 0; };
+    auto at_of = [&](int q) { return p + static_cast<int64_t>(seg_of(q)) * (M::YD * M::WD / 4); };
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q)
+      if (len_of(q0 + q) > 0) u[q] = *at_of(q0 + q);
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      const int len = len_of(q0 + q);
+      if (len <= 0) continue;
+      *at_of(q0 + q) = run;
+      run = run * a.pow(len) + u[q];
+    }
   }
   if (g.sT) {
 #pragma unroll
@@ -729,7 +749,7 @@ int check_desc(const ard_linattn_desc* d) {
   return ARD_OK;
 }
 
-constexpr int kFill = 512;  // workgroups that fill the chip
+constexpr int kFill4 = 512, kFill8 = 256;  // workgroups of four or eight waves that fill the chip
 
 int pad_dim(int d) { return d <= 64 ? 64 : 128; }
 
@@ -742,8 +762,11 @@ MixPlan plan_mix(const ard_linattn_desc* d, int ydim, int wdim) {
   p.yd = pad_dim(ydim);
   p.wd = d->dtype == ARD_BF16 ? pad_dim(wdim) : 64;
   p.wtiles = (wdim + p.wd - 1) / p.wd;
-  const int64_t base = static_cast<int64_t>(d->n_seqs) * d->q_heads * p.wtiles;
-  int64_t n = base >= kFill / 2 ? 1 : (kFill + base - 1) / base;
+  // as many sequences as there can be of the longest length: of ragged ones, most are shorter
+  const int64_t full = std::min<int64_t>(d->n_seqs, (d->tokens - 1) / d->max_len + 1);
+  const int64_t base = full * d->q_heads * p.wtiles, fill = p.yd == 64 ? kFill4 : kFill8;
+  // fp32 is bound by its products, which a second pass adds to, but not by as much as idle units
+  int64_t n = base >= (d->dtype == ARD_BF16 ? fill / 2 : fill) ? 1 : (fill + base - 1) / base;
   const int64_t chunks = (static_cast<int64_t>(d->max_len) + kChunk - 1) / kChunk;
   n = std::max<int64_t>(1, std::min(n, chunks / 4));  // four chunks at least
   const int64_t per = (chunks + n - 1) / n;
