@@ -40,22 +40,23 @@ __device__ __forceinline__ float exp_neg(float x) {
     return expf(x);
 }
 
-// VE consecutive columns of a row, as fp32. Rows start at any element.
+// VE consecutive columns of a row as loaded, and as fp32. Rows start at any element.
 template <typename T, int VE>
-__device__ __forceinline__ void load_cols(const T* p, float (&v)[VE]) {
-  if constexpr (VE == 1) {
-    v[0] = to_f32(*p);
-  } else {
-    const u32x4 raw = load16_any<sizeof(T)>(reinterpret_cast<const char*>(p));
-#pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      if constexpr (sizeof(T) == 2)
-        v[e] = __uint_as_float((e & 1) ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16);
-      else
-        v[e] = __uint_as_float(raw[e]);
-    }
+struct Cols {
+  typename std::conditional<VE == 1, T, u32x4>::type raw;
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (VE == 1) raw = *p;
+    else raw = load16_any<sizeof(T)>(reinterpret_cast<const char*>(p));
   }
-}
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (VE == 1)
+      return to_f32(raw);
+    else if constexpr (sizeof(T) == 2)
+      return __uint_as_float((e & 1) ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16);
+    else
+      return __uint_as_float(raw[e]);
+  }
+};
 template <typename T, int VE>
 __device__ __forceinline__ void store_cols(T* p, const float (&v)[VE]) {
   if constexpr (VE == 1) {
@@ -106,132 +107,75 @@ __device__ __forceinline__ void join(Run& a, const Run& b, float inv_t) {
   a.m = m;
 }
 
-template <typename T, int VE, bool TWO>
-__global__ void __launch_bounds__(256) distill_sums_kernel(const T* __restrict__ Z, int32_t V, int32_t B, Grid g,
-                                                           float inv_t, float* __restrict__ part) {
-  constexpr int U = 4;  // rows in flight
-  const Columns c = columns_of<VE>(B, g.tx);
-  const int ty = threadIdx.x / g.tx, ny = 256 / g.tx;
-  const int64_t r0 = blockIdx.y * g.rows;
-  const int64_t r1 = r0 + g.rows < V ? r0 + g.rows : V;
-  Run run[VE];
-#pragma unroll
-  for (int e = 0; e < VE; ++e) run[e] = {-__builtin_inff(), 0.0f, 0.0f};
-  if (c.on) {
-    const T* z = Z + c.col;
-    auto take = [&](const float(&x)[U][VE], int n) {  // n of the U rows
-#pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        float m = run[e].m;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (u < n) m = fmaxf(m, x[u][e]);
-        const float r = ref_of(m), old = run[e].m - r;
-        float s1 = run[e].s1 * exp_neg<T>(old), sT = TWO ? run[e].sT * exp_neg<T>(old * inv_t) : 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (u < n) {
-            s1 += exp_neg<T>(x[u][e] - r);
-            if constexpr (TWO) sT += exp_neg<T>((x[u][e] - r) * inv_t);
-          }
-        }
-        run[e] = {m, s1, sT};
-      }
-    };
-    int64_t r = r0 + ty;
-    for (; r + static_cast<int64_t>(U - 1) * ny < r1; r += static_cast<int64_t>(U) * ny) {
-      float x[U][VE];
-#pragma unroll
-      for (int u = 0; u < U; ++u) load_cols<T, VE>(z + (r + static_cast<int64_t>(u) * ny) * B, x[u]);
-      take(x, U);
-    }
-    for (; r < r1; r += ny) {
-      float x[U][VE];
-      load_cols<T, VE>(z + r * B, x[0]);
-      take(x, 1);
-    }
-  }
-  // the rows' threads of a column, halved step by step
-  __shared__ Run red[256];
-#pragma unroll
-  for (int e = 0; e < VE; ++e) {
-    __syncthreads();
-    red[threadIdx.x] = run[e];
-    for (int h = ny / 2; h > 0; h >>= 1) {
-      __syncthreads();
-      if (ty < h) join<T, TWO>(red[threadIdx.x], red[threadIdx.x + h * g.tx], inv_t);
-    }
-    if (ty == 0 && c.on) {
-      float* p = part + static_cast<int64_t>(blockIdx.y) * 3 * B + c.col + e;
-      const Run& s = red[threadIdx.x];
-      p[0] = s.m;
-      p[B] = s.s1;
-      p[2 * static_cast<int64_t>(B)] = TWO ? s.sT : s.s1;
-    }
-  }
-}
-
-// Joins a column's ranges, then the teacher's entries and the label: 32 columns
-// of a workgroup, eight threads each.
+// What the teacher's entries and the label add to a column's sums: its loss and the
+// values kept for the backward. NY threads for each of NX columns (neighbouring
+// threads neighbouring columns), `a` the column's joined sums; entries four at a time,
+// so that their loads run together.
 template <typename T, bool TWO>
-__global__ void __launch_bounds__(256) distill_loss_kernel(const T* __restrict__ Z, int32_t V, int32_t B, int32_t top,
-                                                           const int32_t* __restrict__ idx,
-                                                           const float* __restrict__ tl,
-                                                           const int32_t* __restrict__ labels, float temp,
-                                                           float weight, int32_t splits,
-                                                           const float* __restrict__ part, float* __restrict__ loss,
-                                                           float* __restrict__ stats) {
-  constexpr int NX = 32, NY = 8;
-  __shared__ Run red[256];
-  __shared__ float fred[256];
-  const int tx = threadIdx.x % NX, ty = threadIdx.x / NX;
-  const int64_t col = static_cast<int64_t>(blockIdx.x) * NX + tx;
-  const bool on = col < B;
+__device__ __forceinline__ void finish_column(Run a, int64_t col, bool on, int tx, int ty, int NX, int NY,
+                                              const T* __restrict__ Z, int32_t V, int32_t B, int32_t top,
+                                              const int32_t* __restrict__ idx, const float* __restrict__ tl,
+                                              const int32_t* __restrict__ labels, float temp, float weight,
+                                              float* __restrict__ loss, float* __restrict__ stats, float* red) {
+  constexpr int U = 4;
   const float inv_t = 1.0f / temp;
-  Run a = {-__builtin_inff(), 0.0f, 0.0f};
-  if (on) {
-    for (int s = ty; s < splits; s += NY) {
-      const float* p = part + static_cast<int64_t>(s) * 3 * B + col;
-      join<T, TWO>(a, Run{p[0], p[B], p[2 * static_cast<int64_t>(B)]}, inv_t);
-    }
-  }
-  red[threadIdx.x] = a;
-  for (int h = NY / 2; h > 0; h >>= 1) {
-    __syncthreads();
-    if (ty < h) join<T, TWO>(red[threadIdx.x], red[threadIdx.x + h * NX], inv_t);
-  }
-  __syncthreads();
-  a = red[tx];
   if (!TWO) a.sT = a.s1;
   const float ref = ref_of(a.m);
+  const bool read = on && weight > 0.0f;
   // the teacher's maximum over the valid entries
   float tm = -__builtin_inff();
-  if (on)
-    for (int64_t j = ty; j < top; j += NY) {
-      const int32_t v = idx[j * B + col];
-      if (v >= 0 && v < V) tm = fmaxf(tm, tl[j * B + col]);
+  if (read)
+    for (int64_t j = ty; j < top; j += U * NY) {
+      int32_t v[U];
+      float t[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t q = j + u * NY < top ? j + u * NY : j;
+        v[u] = idx[q * B + col], t[u] = tl[q * B + col];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (v[u] >= 0 && v[u] < V) tm = fmaxf(tm, t[u]);
     }
-  fred[threadIdx.x] = tm;
+  red[ty * NX + tx] = tm;
   __syncthreads();
-  for (int y = 0; y < NY; ++y) tm = fmaxf(tm, fred[y * NX + tx]);
+  for (int y = 0; y < NY; ++y) tm = fmaxf(tm, red[y * NX + tx]);
+  __syncthreads();
   const float tref = ref_of(tm);
   // sums of e_j = exp((t_j - tm) / T) and of e_j ((t_j - tm) - (z_j - m)) / T
   float es = 0.0f, ds = 0.0f;
-  if (on)
-    for (int64_t j = ty; j < top; j += NY) {
-      const int32_t v = idx[j * B + col];
-      if (v < 0 || v >= V) continue;
-      const float t = (tl[j * B + col] - tref) * inv_t, e = expf(t);
-      const float z = (to_f32(Z[static_cast<int64_t>(v) * B + col]) - ref) * inv_t;
-      es += e;
-      if (!(e == 0.0f)) ds += e * (t - z);
+  if (read)
+    for (int64_t j = ty; j < top; j += U * NY) {
+      int32_t v[U];
+      float t[U], z[U];
+      bool ok[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t q = j + u * NY < top ? j + u * NY : j;
+        v[u] = idx[q * B + col], t[u] = tl[q * B + col];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        ok[u] = v[u] >= 0 && v[u] < V && j + u * NY < top;
+        z[u] = to_f32(Z[static_cast<int64_t>(ok[u] ? v[u] : 0) * B + col]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float x = (t[u] - tref) * inv_t, e = ok[u] ? expf(x) : 0.0f;
+        es += e;
+        if (!(e == 0.0f)) ds += e * (x - (z[u] - ref) * inv_t);
+      }
     }
+  red[ty * NX + tx] = es;
   __syncthreads();
-  red[threadIdx.x] = {es, ds, 0.0f};
+  es = 0.0f;
+  for (int y = 0; y < NY; ++y) es += red[y * NX + tx];
+  __syncthreads();
+  red[ty * NX + tx] = ds;
   __syncthreads();
   if (ty != 0 || !on) return;
-  es = ds = 0.0f;
-  for (int y = 0; y < NY; ++y) es += red[y * NX + tx].m, ds += red[y * NX + tx].s1;
+  ds = 0.0f;
+  for (int y = 0; y < NY; ++y) ds += red[y * NX + tx];
   float out = 0.0f;
   // a column without a logit above -inf has s1 = 0 and no loss
   if (weight > 0.0f && !(es == 0.0f) && !(a.sT == 0.0f)) out += weight * temp * temp * (ds / es + logf(a.sT / es));
@@ -245,6 +189,134 @@ __global__ void __launch_bounds__(256) distill_loss_kernel(const T* __restrict__
   stats[2 * b + col] = a.sT;
   stats[3 * b + col] = tref;
   stats[4 * b + col] = es;
+}
+
+// The running sums of a range of rows; ONE: of all rows, and with them the loss.
+template <typename T, int VE, bool TWO, bool ONE>
+__global__ void __launch_bounds__(256) distill_sums_kernel(const T* __restrict__ Z, int32_t V, int32_t B, Grid g,
+                                                           int32_t top, const int32_t* __restrict__ idx,
+                                                           const float* __restrict__ tl,
+                                                           const int32_t* __restrict__ labels, float temp,
+                                                           float weight, float* __restrict__ part,
+                                                           float* __restrict__ loss, float* __restrict__ stats) {
+  constexpr int U = 4;  // rows in flight
+  const float inv_t = 1.0f / temp;
+  const Columns c = columns_of<VE>(B, g.tx);
+  const int tx = threadIdx.x & (g.tx - 1), ty = threadIdx.x / g.tx, ny = 256 / g.tx;
+  const int64_t r0 = blockIdx.y * g.rows;
+  const int64_t r1 = r0 + g.rows < V ? r0 + g.rows : V;
+  Run run[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) run[e] = {-__builtin_inff(), 0.0f, 0.0f};
+  if (c.on) {
+    const T* z = Z + c.col;
+    auto take = [&](const Cols<T, VE>(&x)[U], int n) {  // n of the U rows
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        float m = run[e].m;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (u < n) m = fmaxf(m, x[u].at(e));
+        const float r = ref_of(m), old = run[e].m - r;
+        float s1 = run[e].s1 * exp_neg<T>(old), sT = TWO ? run[e].sT * exp_neg<T>(old * inv_t) : 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (u < n) {
+            s1 += exp_neg<T>(x[u].at(e) - r);
+            if constexpr (TWO) sT += exp_neg<T>((x[u].at(e) - r) * inv_t);
+          }
+        }
+        run[e] = {m, s1, sT};
+      }
+    };
+    // the next rows are on their way while these are added
+    const int64_t step = static_cast<int64_t>(U) * ny;
+    Cols<T, VE> x[2][U];
+    auto load = [&](int64_t r, Cols<T, VE>(&to)[U]) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) to[u].load(z + (r + static_cast<int64_t>(u) * ny) * B);
+    };
+    int64_t r = r0 + ty;
+    const int64_t whole = r1 - (U - 1) * static_cast<int64_t>(ny);  // first rows below it have all U
+    if (r < whole) load(r, x[0]);
+    for (; r < whole; r += 2 * step) {
+      if (r + step < whole) load(r + step, x[1]);
+      take(x[0], U);
+      if (r + step >= whole) {
+        r += step;
+        break;
+      }
+      if (r + 2 * step < whole) load(r + 2 * step, x[0]);
+      take(x[1], U);
+    }
+    for (; r < r1; r += ny) {
+      x[0][0].load(z + r * B);
+      take(x[0], 1);
+    }
+  }
+  // the rows' threads of a column, halved step by step
+  __shared__ Run red[256];
+  __shared__ float fin[256];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) {
+    __syncthreads();
+    red[threadIdx.x] = run[e];
+    for (int h = ny / 2; h > 0; h >>= 1) {
+      __syncthreads();
+      if (ty < h) join<T, TWO>(red[threadIdx.x], red[threadIdx.x + h * g.tx], inv_t);
+    }
+    if constexpr (ONE) {
+      __syncthreads();
+      finish_column<T, TWO>(red[tx], c.col + e, c.on, tx, ty, g.tx, ny, Z, V, B, top, idx, tl, labels, temp, weight,
+                            loss, stats, fin);
+    } else if (ty == 0 && c.on) {
+      float* p = part + static_cast<int64_t>(blockIdx.y) * 3 * B + c.col + e;
+      const Run& s = red[threadIdx.x];
+      p[0] = s.m;
+      p[B] = s.s1;
+      p[2 * static_cast<int64_t>(B)] = TWO ? s.sT : s.s1;
+    }
+  }
+}
+
+// Joins a column's ranges, then the teacher's entries and the label: 16 columns
+// of a workgroup, sixteen threads each.
+template <typename T, bool TWO>
+__global__ void __launch_bounds__(256) distill_loss_kernel(const T* __restrict__ Z, int32_t V, int32_t B, int32_t top,
+                                                           const int32_t* __restrict__ idx,
+                                                           const float* __restrict__ tl,
+                                                           const int32_t* __restrict__ labels, float temp,
+                                                           float weight, int32_t splits,
+                                                           const float* __restrict__ part, float* __restrict__ loss,
+                                                           float* __restrict__ stats) {
+  constexpr int NX = 16, NY = 16, U = 4;
+  __shared__ Run red[256];
+  __shared__ float fin[256];
+  const int tx = threadIdx.x % NX, ty = threadIdx.x / NX;
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * NX + tx;
+  const bool on = col < B;
+  const float inv_t = 1.0f / temp;
+  Run a = {-__builtin_inff(), 0.0f, 0.0f};
+  if (on) {
+    for (int s = ty; s < splits; s += U * NY) {
+      Run b[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float* p = part + static_cast<int64_t>(s + u * NY < splits ? s + u * NY : s) * 3 * B + col;
+        b[u] = {p[0], p[B], TWO ? p[2 * static_cast<int64_t>(B)] : 0.0f};
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (s + u * NY < splits) join<T, TWO>(a, b[u], inv_t);
+    }
+  }
+  red[threadIdx.x] = a;
+  for (int h = NY / 2; h > 0; h >>= 1) {
+    __syncthreads();
+    if (ty < h) join<T, TWO>(red[threadIdx.x], red[threadIdx.x + h * NX], inv_t);
+  }
+  __syncthreads();
+  finish_column<T, TWO>(red[tx], col, on, tx, ty, NX, NY, Z, V, B, top, idx, tl, labels, temp, weight, loss, stats, fin);
 }
 
 // A column's factors of the gradient: dz = fT exp((z - m) / T) + f1 exp(z - m),
@@ -283,48 +355,90 @@ __device__ __forceinline__ float dense_grad(float z, float m, float fT, float f1
   }
 }
 
-template <typename T, int VE, bool TWO>
+// An entry at a teacher's class or the label, written whole (entry `top` is the
+// label). A class that several entries name gets every one's share from each of
+// their threads, the same value in the same order.
+template <typename T, bool TWO>
+__device__ __forceinline__ void sparse_entry(int64_t j, int64_t col, const Factors& f, const T* __restrict__ Z,
+                                             int32_t V, int32_t B, int32_t top, const int32_t* __restrict__ idx,
+                                             const float* __restrict__ tl, int32_t label, float tref, float es,
+                                             float inv_t, T* dZ) {
+  const int32_t v = j < top ? idx[j * B + col] : label;
+  if (v < 0 || v >= V) return;
+  const int64_t at = static_cast<int64_t>(v) * B + col;
+  const float z = to_f32(Z[at]);
+  float p = 0.0f;
+  if (!(f.cs == 0.0f)) {
+    constexpr int U = 8;  // entries in flight
+    for (int64_t i = 0; i < top; i += U) {
+      int32_t w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = idx[(i + u < top ? i + u : i) * B + col];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (w[u] == v && i + u < top) p += expf((tl[(i + u) * B + col] - tref) * inv_t);
+    }
+  }
+  float g = dense_grad<T, TWO>(z, f.m, f.fT, f.f1, inv_t);
+  if (!(f.cs == 0.0f)) g -= f.cs * (p / es);
+  if (v == label) g -= f.ch;
+  dZ[at] = from_f32<T>(g);
+}
+
+// The dense part of a range of rows; ONE: of all rows, and the entries after it.
+template <typename T, int VE, bool TWO, bool ONE>
 __global__ void __launch_bounds__(256) distill_dense_kernel(const T* __restrict__ Z, int32_t V, int32_t B, Grid g,
+                                                            int32_t top, const int32_t* __restrict__ idx,
+                                                            const float* __restrict__ tl,
                                                             const int32_t* __restrict__ labels,
                                                             const float* __restrict__ stats,
                                                             const float* __restrict__ dloss, float temp, float weight,
-                                                            T* __restrict__ dZ) {
+                                                            T* dZ) {
   constexpr int U = 4;
   const Columns c = columns_of<VE>(B, g.tx);
-  if (!c.on) return;
   const int ty = threadIdx.x / g.tx, ny = 256 / g.tx;
   const float inv_t = 1.0f / temp;
-  float m[VE], fT[VE], f1[VE];
+  if (c.on) {
+    float m[VE], fT[VE], f1[VE];
 #pragma unroll
-  for (int e = 0; e < VE; ++e) {
-    const Factors f = factors_of(c.col + e, V, B, stats, labels, dloss, temp, weight);
-    m[e] = f.m, fT[e] = f.fT, f1[e] = f.f1;
+    for (int e = 0; e < VE; ++e) {
+      const Factors f = factors_of(c.col + e, V, B, stats, labels, dloss, temp, weight);
+      m[e] = f.m, fT[e] = f.fT, f1[e] = f.f1;
+    }
+    const int64_t r0 = blockIdx.y * g.rows;
+    const int64_t r1 = r0 + g.rows < V ? r0 + g.rows : V;
+    auto put = [&](int64_t r, const Cols<T, VE>& x) {
+      float d[VE];
+#pragma unroll
+      for (int e = 0; e < VE; ++e) d[e] = dense_grad<T, TWO>(x.at(e), m[e], fT[e], f1[e], inv_t);
+      store_cols<T, VE>(dZ + r * B + c.col, d);
+    };
+    int64_t r = r0 + ty;
+    for (; r + static_cast<int64_t>(U - 1) * ny < r1; r += static_cast<int64_t>(U) * ny) {
+      Cols<T, VE> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u].load(Z + (r + static_cast<int64_t>(u) * ny) * B + c.col);
+#pragma unroll
+      for (int u = 0; u < U; ++u) put(r + static_cast<int64_t>(u) * ny, x[u]);
+    }
+    for (; r < r1; r += ny) {
+      Cols<T, VE> x;
+      x.load(Z + r * B + c.col);
+      put(r, x);
+    }
   }
-  const int64_t r0 = blockIdx.y * g.rows;
-  const int64_t r1 = r0 + g.rows < V ? r0 + g.rows : V;
-  auto put = [&](int64_t r, float(&x)[VE]) {
-#pragma unroll
-    for (int e = 0; e < VE; ++e) x[e] = dense_grad<T, TWO>(x[e], m[e], fT[e], f1[e], inv_t);
-    store_cols<T, VE>(dZ + r * B + c.col, x);
-  };
-  int64_t r = r0 + ty;
-  for (; r + static_cast<int64_t>(U - 1) * ny < r1; r += static_cast<int64_t>(U) * ny) {
-    float x[U][VE];
-#pragma unroll
-    for (int u = 0; u < U; ++u) load_cols<T, VE>(Z + (r + static_cast<int64_t>(u) * ny) * B + c.col, x[u]);
-#pragma unroll
-    for (int u = 0; u < U; ++u) put(r + static_cast<int64_t>(u) * ny, x[u]);
-  }
-  for (; r < r1; r += ny) {
-    float x[VE];
-    load_cols<T, VE>(Z + r * B + c.col, x);
-    put(r, x);
+  if constexpr (ONE) {
+    __syncthreads();  // waits for the stores above
+    for (int e = 0; e < VE && c.on; ++e) {
+      const int64_t col = c.col + e, b = B;
+      const Factors f = factors_of(col, V, B, stats, labels, dloss, temp, weight);
+      for (int64_t j = ty; j <= top; j += ny)
+        sparse_entry<T, TWO>(j, col, f, Z, V, B, top, idx, tl, labels ? labels[col] : -1, stats[3 * b + col],
+                             stats[4 * b + col], inv_t, dZ);
+    }
   }
 }
 
-// The entries at the teacher's classes and the label, written whole: one thread
-// each (entry `top` is the label). A class that several entries name gets every
-// one's share from each of their threads, the same value in the same order.
 template <typename T, bool TWO>
 __global__ void __launch_bounds__(256) distill_sparse_kernel(const T* __restrict__ Z, int32_t V, int32_t B,
                                                              int32_t top, const int32_t* __restrict__ idx,
@@ -332,25 +446,13 @@ __global__ void __launch_bounds__(256) distill_sparse_kernel(const T* __restrict
                                                              const int32_t* __restrict__ labels,
                                                              const float* __restrict__ stats,
                                                              const float* __restrict__ dloss, float temp,
-                                                             float weight, T* __restrict__ dZ) {
-  const int64_t col = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63);
+                                                             float weight, T* dZ) {
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63), b = B;
   const int64_t j = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 6);
   if (col >= B || j > top) return;
-  const int32_t label = labels ? labels[col] : -1;
-  const int32_t v = j < top ? idx[j * B + col] : label;
-  if (v < 0 || v >= V) return;
-  const float inv_t = 1.0f / temp;
   const Factors f = factors_of(col, V, B, stats, labels, dloss, temp, weight);
-  const float tref = stats[3 * static_cast<int64_t>(B) + col], es = stats[4 * static_cast<int64_t>(B) + col];
-  float p = 0.0f;
-  if (!(f.cs == 0.0f))
-    for (int64_t i = 0; i < top; ++i)
-      if (idx[i * B + col] == v) p += expf((tl[i * B + col] - tref) * inv_t);
-  const int64_t at = static_cast<int64_t>(v) * B + col;
-  float g = dense_grad<T, TWO>(to_f32(Z[at]), f.m, f.fT, f.f1, inv_t);
-  if (!(f.cs == 0.0f)) g -= f.cs * (p / es);
-  if (v == label) g -= f.ch;
-  dZ[at] = from_f32<T>(g);
+  sparse_entry<T, TWO>(j, col, f, Z, V, B, top, idx, tl, labels ? labels[col] : -1, stats[3 * b + col],
+                       stats[4 * b + col], 1.0f / temp, dZ);
 }
 
 int need_ptr(const void* p, const char* name) {
@@ -376,16 +478,23 @@ int check_desc(const ard_distill_desc* d) {
   return ARD_OK;
 }
 
-constexpr int kBlocks = 768;  // workgroups that fill the chip: three on a compute unit
+constexpr int kBlocks = 512;  // workgroups that fill the chip: two on a compute unit
+
+// Few classes: one column per thread and 16 threads down its rows, the whole pass in
+// one launch. A launch costs what the reading of some hundred rows does (10 classes,
+// 128 columns, fp32, forward and backward: 18.5 us in four launches of wide rows).
+constexpr int kOneLaunch = 256;
+bool one_launch(const ard_distill_desc* d) { return d->classes <= kOneLaunch; }
 
 int vector_of(const ard_distill_desc* d) {
   const int ve = d->dtype == ARD_BF16 ? 8 : 4;
-  return d->batch >= ve ? ve : 1;
+  return d->batch >= ve && !one_launch(d) ? ve : 1;
 }
 
 // At least 8 rows for each thread, so that a range's sums outweigh joining them.
 Grid grid_of(const ard_distill_desc* d) {
   const int64_t chunks = (static_cast<int64_t>(d->batch) + vector_of(d) - 1) / vector_of(d);
+  if (one_launch(d)) return {16, static_cast<int32_t>((chunks + 15) / 16), 1, d->classes};
   Grid g = {1, 0, 0, 0};
   while (g.tx < 64 && g.tx < chunks) g.tx *= 2;
   g.blocks = static_cast<int32_t>((chunks + g.tx - 1) / g.tx);
@@ -399,7 +508,7 @@ Grid grid_of(const ard_distill_desc* d) {
 }
 
 size_t workspace_bytes(const ard_distill_desc* d) {
-  return static_cast<size_t>(grid_of(d).splits) * 3 * static_cast<size_t>(d->batch) * 4;
+  return one_launch(d) ? 0 : static_cast<size_t>(grid_of(d).splits) * 3 * static_cast<size_t>(d->batch) * 4;
 }
 
 int check_teacher(const ard_distill_desc* d, const int32_t* idx, const float* tl, const int32_t* labels) {
@@ -408,30 +517,33 @@ int check_teacher(const ard_distill_desc* d, const int32_t* idx, const float* tl
   return may_ptr(labels, "labels");
 }
 
-template <typename T, int VE, bool TWO>
+template <typename T, int VE, bool TWO, bool ONE>
 int fwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, const float* tl, const int32_t* labels,
              float* loss, float* stats, float* part, hipStream_t stream) {
   const Grid g = grid_of(d);
   const T* Z = static_cast<const T*>(Zt);
-  hipLaunchKernelGGL((distill_sums_kernel<T, VE, TWO>), dim3(g.blocks, g.splits), dim3(256), 0, stream, Z, d->classes,
-                     d->batch, g, 1.0f / d->temperature, part);
+  hipLaunchKernelGGL((distill_sums_kernel<T, VE, TWO, ONE>), dim3(g.blocks, g.splits), dim3(256), 0, stream, Z,
+                     d->classes, d->batch, g, d->top, idx, tl, labels, d->temperature, d->soft_weight, part, loss,
+                     stats);
   ARD_LAUNCH_CHECK();
-  hipLaunchKernelGGL((distill_loss_kernel<T, TWO>), dim3((d->batch - 1) / 32 + 1), dim3(256), 0, stream, Z, d->classes,
+  if (ONE) return ARD_OK;
+  hipLaunchKernelGGL((distill_loss_kernel<T, TWO>), dim3((d->batch - 1) / 16 + 1), dim3(256), 0, stream, Z, d->classes,
                      d->batch, d->top, idx, tl, labels, d->temperature, d->soft_weight, g.splits, part, loss, stats);
   ARD_LAUNCH_CHECK();
   return ARD_OK;
 }
 
-template <typename T, int VE, bool TWO>
+template <typename T, int VE, bool TWO, bool ONE>
 int bwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, const float* tl, const int32_t* labels,
              const float* stats, const float* dloss, void* dZt, hipStream_t stream) {
   const Grid g = grid_of(d);
   const T* Z = static_cast<const T*>(Zt);
   T* dZ = static_cast<T*>(dZt);
-  hipLaunchKernelGGL((distill_dense_kernel<T, VE, TWO>), dim3(g.blocks, g.splits), dim3(256), 0, stream, Z,
-                     d->classes, d->batch, g, labels, stats, dloss, d->temperature, d->soft_weight, dZ);
+  hipLaunchKernelGGL((distill_dense_kernel<T, VE, TWO, ONE>), dim3(g.blocks, g.splits), dim3(256), 0, stream, Z,
+                     d->classes, d->batch, g, d->top, idx, tl, labels, stats, dloss, d->temperature, d->soft_weight,
+                     dZ);
   ARD_LAUNCH_CHECK();
-  if (d->top > 0 || labels) {
+  if (!ONE && (d->top > 0 || labels)) {
     hipLaunchKernelGGL((distill_sparse_kernel<T, TWO>), dim3((d->batch - 1) / 64 + 1, d->top / 4 + 1), dim3(256), 0,
                        stream, Z, d->classes, d->batch, d->top, idx, tl, labels, stats, dloss, d->temperature,
                        d->soft_weight, dZ);
@@ -440,19 +552,21 @@ int bwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, cons
   return ARD_OK;
 }
 
-// Calls f with a value of the element type, the columns per thread and whether
-// the two softmaxes differ.
+// Calls f with a value of the element type, the columns per thread, whether the two
+// softmaxes differ and whether one launch does it all.
 template <class F>
 int dispatch(const ard_distill_desc* d, F f) {
   using std::integral_constant;
   const bool two = d->temperature != 1.0f;
-  auto with = [&](auto t, auto ve) {
-    return two ? f(t, ve, std::true_type{}) : f(t, ve, std::false_type{});
+  auto with = [&](auto t, auto ve, auto one) {
+    return two ? f(t, ve, std::true_type{}, one) : f(t, ve, std::false_type{}, one);
   };
-  const int ve = vector_of(d);
-  if (d->dtype == ARD_BF16)
-    return ve > 1 ? with(bf16{}, integral_constant<int, 8>{}) : with(bf16{}, integral_constant<int, 1>{});
-  return ve > 1 ? with(float{}, integral_constant<int, 4>{}) : with(float{}, integral_constant<int, 1>{});
+  auto typed = [&](auto t, auto wide) {
+    if (one_launch(d)) return with(t, integral_constant<int, 1>{}, std::true_type{});
+    if (vector_of(d) == 1) return with(t, integral_constant<int, 1>{}, std::false_type{});
+    return with(t, wide, std::false_type{});
+  };
+  return d->dtype == ARD_BF16 ? typed(bf16{}, integral_constant<int, 8>{}) : typed(float{}, integral_constant<int, 4>{});
 }
 
 }  // namespace
@@ -475,11 +589,11 @@ int ard_distill_fwd(const ard_distill_desc* desc, const void* Zt, const int32_t*
   if ((st = need_ptr(Zt, "Zt")) || (st = need_ptr(loss, "loss")) || (st = need_ptr(stats, "stats")) ||
       (st = check_teacher(desc, top_idx, top_logits, labels)))
     return st;
-  if (!ws || ws_bytes < workspace_bytes(desc))
+  if (workspace_bytes(desc) > 0 && (!ws || ws_bytes < workspace_bytes(desc)))
     return fail(ARD_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", workspace_bytes(desc), ws ? ws_bytes : 0);
-  if (!aligned16(ws)) return fail(ARD_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
-  return dispatch(desc, [&](auto t, auto ve, auto two) {
-    return fwd_impl<decltype(t), decltype(ve)::value, decltype(two)::value>(
+  if ((st = may_ptr(ws, "workspace"))) return st;
+  return dispatch(desc, [&](auto t, auto ve, auto two, auto one) {
+    return fwd_impl<decltype(t), decltype(ve)::value, decltype(two)::value, decltype(one)::value>(
         desc, Zt, top_idx, top_logits, labels, loss, stats, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
   });
 }
@@ -493,8 +607,8 @@ int ard_distill_bwd(const ard_distill_desc* desc, const void* Zt, const int32_t*
       (st = may_ptr(dloss, "dloss")) || (st = check_teacher(desc, top_idx, top_logits, labels)))
     return st;
   if (dZt == Zt) return fail(ARD_ERR_INVALID_ARG, "dZt must not be Zt: the logits are read again after the first pass");
-  return dispatch(desc, [&](auto t, auto ve, auto two) {
-    return bwd_impl<decltype(t), decltype(ve)::value, decltype(two)::value>(
+  return dispatch(desc, [&](auto t, auto ve, auto two, auto one) {
+    return bwd_impl<decltype(t), decltype(ve)::value, decltype(two)::value, decltype(one)::value>(
         desc, Zt, top_idx, top_logits, labels, stats, dloss, dZt, static_cast<hipStream_t>(stream));
   });
 }
