@@ -1,8 +1,9 @@
 // Gated feed-forward layer under a row pattern on its hidden units:
 //   g = W0 x + b0,  u = W1 x + b1,  h = scale act(g) u  on the kept units.
 //
-// Forward: both projections of the kept rows as one batched product, then the
-// activation and the product. Backward: one pass writes the derivatives
+// Forward: one kernel, for a few columns bound by reading the weights once, for many by
+// the matrix cores; grids too small for its tiles (and weights past 2^31 bytes) run both
+// projections as a batched product and join them. Backward: one pass writes the derivatives
 //   dg = scale dh u act'(g),  du = scale dh act(g)
 // of the kept rows (rounded to the element type once) and their row sums, the
 // bias gradients, from the unrounded values; then dX = W0^T dg + W1^T du as one
@@ -20,17 +21,25 @@
 namespace ard {
 namespace {
 
-// The activation and its derivative, in fp32.
+// The activation and its derivative, in fp32. With bf16 data the exponential and the
+// reciprocal are the hardware's, to a few 2^-24: far below what the results are
+// rounded by, and a tenth of the library functions' instructions, which the epilogue
+// of a product does not hide.
 struct Act {
   float f, d;
 };
+template <typename T>
 __device__ __forceinline__ Act act_of(int act, float g) {
   if (act == ARD_GLU_RELU) return {g > 0.0f ? g : (g == g ? 0.0f : g), g > 0.0f ? 1.0f : 0.0f};
   if (act == ARD_GLU_GELU) {
     const float cdf = 0.5f * erfcf(g * -0.70710678118654752440f);  // to its own last bits where it is small
     return {g * cdf, cdf + g * 0.39894228040143267794f * expf(-0.5f * g * g)};
   }
-  const float s = 1.0f / (1.0f + expf(-g));
+  float s;
+  if constexpr (sizeof(T) == 2)
+    s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504088896340736f));
+  else
+    s = 1.0f / (1.0f + expf(-g));
   if (act == ARD_GLU_SIGMOID) return {s, s * (1.0f - s)};
   return {g * s, s * (1.0f + g * (1.0f - s))};
 }
@@ -60,7 +69,7 @@ __global__ void __launch_bounds__(256) glu_join_kernel(GluShape s, const float* 
   const float b0 = bias ? bias[n] : 0.0f, b1 = bias ? bias[s.N + n] : 0.0f;
   for (int b = threadIdx.x; b < s.B; b += 256) {
     const float g = gf[b] + b0, u = uf[b] + b1;
-    h[b] = from_f32<T>(scale * act_of(act, g).f * u);
+    h[b] = from_f32<T>(scale * act_of<T>(act, g).f * u);
     if (Z) {
       Z[n * s.B + b] = from_f32<T>(g);
       Z[(s.N + n) * s.B + b] = from_f32<T>(u);
@@ -68,22 +77,398 @@ __global__ void __launch_bounds__(256) glu_join_kernel(GluShape s, const float* 
   }
 }
 
-// The derivatives D[2][kept][ldd] and their row sums: a workgroup per kept unit.
+// ------------------------------------------------------------------ few columns
+// Up to 64 columns (single tokens of as many sequences): bound by reading the kept
+// weights once. A workgroup takes PAIRS hidden units (16, or 8 so that a small layer
+// still reaches every compute unit: both projections then share one block of 16
+// rows); its eight waves split the inputs and read the weights straight into MFMA
+// operands, 16 bytes of a lane, nothing shared through LDS. The columns' part is read
+// as it lies, [k][batch], and turned in wave-private LDS (bf16; fp32 operands are
+// single elements). The waves' sums meet in LDS, where the layer is finished.
+// NB: blocks of 16 columns; 0: one column, whose inputs are contiguous already.
+constexpr int kSmallWaves = 8;
+
+template <typename T, int PAIRS, int NB>
+struct Small {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int NC = NB == 0 ? 1 : NB;         // blocks of columns
+  static constexpr int FR = PAIRS == 16 ? 2 : 1;      // blocks of weight rows
+  static constexpr int STEP = BF ? 32 : 16;           // k of one step
+  static constexpr int U = NC >= 4 ? 2 : 4;           // steps in flight
+  static constexpr int XB = BF && NB > 0 ? STEP * NB * 32 : 0;  // bytes of a step's columns in LDS
+  static constexpr int RED = kSmallWaves * FR * NC * 1024;
+  static constexpr int LDS = kSmallWaves * U * XB > RED ? kSmallWaves * U * XB : RED;
+};
+
+template <typename T, int PAIRS, int NB>
+__global__ void __launch_bounds__(64 * kSmallWaves) glu_small_kernel(GluShape s, const T* __restrict__ X,
+                                                                     const T* __restrict__ W,
+                                                                     const float* __restrict__ bias, int act,
+                                                                     float scale, T* __restrict__ Z,
+                                                                     T* __restrict__ H) {
+  using C = Small<T, PAIRS, NB>;
+  constexpr int ES = sizeof(T), VE = 16 / ES;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int row = lane & 15, grp = lane >> 4;
+  const int i0 = xcd_position(blockIdx.x, gridDim.x) * PAIRS;
+  const int64_t K = s.K, B = s.B;
+
+  // the lane's weight rows: gate and other projection, or (8 units) one of them
+  const T* wp[C::FR];
+#pragma unroll
+  for (int f = 0; f < C::FR; ++f) {
+    const int half = PAIRS == 16 ? f : row >> 3;
+    const int i = min(i0 + (PAIRS == 16 ? row : row & 7), s.kept - 1);  // past the last: its results are discarded
+    wp[f] = W + (half * static_cast<int64_t>(s.N) + s.offset + static_cast<int64_t>(i) * s.period) * K + VE * grp;
+  }
+  f32x4 acc[C::FR][C::NC];
+#pragma unroll
+  for (int f = 0; f < C::FR; ++f)
+#pragma unroll
+    for (int c = 0; c < C::NC; ++c) acc[f][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  // a step's products: a = 16 bytes of each weight row, x = the columns' operand
+  auto mma = [&](const u32x4 a, const u32x4 x, f32x4& to) {
+    if constexpr (C::BF) {
+      to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, x), to, 0, 0, 0);
+    } else {
+      const f32x4 af = __builtin_bit_cast(f32x4, a), xf = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to = __builtin_amdgcn_mfma_f32_16x16x4f32(af[e], xf[e], to, 0, 0, 0);
+    }
+  };
+  // Steps of this wave. A whole step reads 16 bytes at a time and stays inside the
+  // operands: the columns' reads reach up to 16 NB - B elements past the last row read.
+  const int steps = static_cast<int>((K + C::STEP - 1) / C::STEP);
+  const int q0 = steps * wv / kSmallWaves, q1 = steps * (wv + 1) / kSmallWaves;
+  int64_t whole = K / C::STEP;
+  if (C::BF && NB > 0)
+    while (whole > 0 && (whole * C::STEP - 1) * B + 16 * NB > K * B) --whole;
+  const int qw = min(q1, static_cast<int>(whole));
+  char* xl = smem + wv * C::U * C::XB;
+  for (int q = q0; q < qw; q += C::U) {
+    u32x4 a[C::U][C::FR], x[C::U][C::NC];
+#pragma unroll
+    for (int u = 0; u < C::U; ++u) {
+      const int64_t k = static_cast<int64_t>(min(q + u, qw - 1)) * C::STEP;  // past the last: read again, not used
+#pragma unroll
+      for (int f = 0; f < C::FR; ++f) a[u][f] = load16_any<ES>(reinterpret_cast<const char*>(wp[f] + k));
+      if constexpr (NB == 0) {
+        x[u][0] = load16_any<ES>(reinterpret_cast<const char*>(X + k + VE * grp));
+      } else if constexpr (C::BF) {
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+          const int at = c * 64 + lane, r = at / (2 * NB), ch = at % (2 * NB);
+          x[u][c] = load16_any<ES>(reinterpret_cast<const char*>(X + (k + r) * B + 8 * ch));
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[u][c][e] = __float_as_uint(X[(k + 4 * grp + e) * B + min(static_cast<int64_t>(16 * c + row), B - 1)]);
+      }
+    }
+    if constexpr (C::XB > 0) {
+#pragma unroll
+      for (int u = 0; u < C::U; ++u)
+#pragma unroll
+        for (int c = 0; c < NB; ++c) *reinterpret_cast<u32x4*>(xl + u * C::XB + (c * 64 + lane) * 16) = x[u][c];
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int u = 0; u < C::U; ++u)
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+          // 8 k of one column: two transposed reads of 4 k by 16 columns
+          const char* p = xl + u * C::XB + (8 * grp + (row >> 2)) * (NB * 32) + c * 32 + (row & 3) * 8;
+          const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p));
+          const i16x4 hi =
+              __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p + 4 * NB * 32));
+          typedef short i16x8 __attribute__((ext_vector_type(8)));
+          x[u][c] = __builtin_bit_cast(u32x4, static_cast<i16x8>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
+        }
+      __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int u = 0; u < C::U; ++u) {
+      if (q + u >= qw) break;
+#pragma unroll
+      for (int f = 0; f < C::FR; ++f)
+#pragma unroll
+        for (int c = 0; c < C::NC; ++c) mma(a[u][f], x[u][c], acc[f][c]);
+    }
+  }
+  // the last steps, element by element
+#pragma unroll 1
+  for (int q = max(q0, qw); q < q1; ++q) {
+    const int64_t k = static_cast<int64_t>(q) * C::STEP + VE * grp;
+    u32x4 a[C::FR], x[C::NC];
+    auto gather = [&](const T* p, int64_t stride) {  // VE elements from p (element k), 0 past K
+      T e[VE];
+      u32x4 v;
+#pragma unroll
+      for (int j = 0; j < VE; ++j) e[j] = p[(k + j < K ? j : 0) * stride];
+#pragma unroll
+      for (int j = 0; j < VE; ++j) reinterpret_cast<T*>(&v)[j] = k + j < K ? e[j] : from_f32<T>(0.0f);
+      return v;
+    };
+    const int64_t kc = k < K ? k : K - 1;
+#pragma unroll
+    for (int f = 0; f < C::FR; ++f) a[f] = gather(wp[f] + (kc - VE * grp), 1);
+#pragma unroll
+    for (int c = 0; c < C::NC; ++c) {
+      const int64_t col = NB == 0 ? 0 : min(static_cast<int64_t>(16 * c + row), B - 1);
+      x[c] = gather(X + kc * B + col, B);
+    }
+#pragma unroll
+    for (int f = 0; f < C::FR; ++f)
+#pragma unroll
+      for (int c = 0; c < C::NC; ++c) mma(a[f], x[c], acc[f][c]);
+  }
+
+  // the waves' sums, and the layer: output block rows 4 grp + r, column lane % 16
+  __syncthreads();
+  f32x4* red = reinterpret_cast<f32x4*>(smem);
+#pragma unroll
+  for (int f = 0; f < C::FR; ++f)
+#pragma unroll
+    for (int c = 0; c < C::NC; ++c) red[((wv * C::FR + f) * C::NC + c) * 64 + lane] = acc[f][c];
+  __syncthreads();
+  auto sum = [&](int f, int m, int b) {  // row m of block f, column b
+    const float* p = reinterpret_cast<const float*>(red + (f * C::NC + b / 16) * 64 + (m >> 2) * 16 + b % 16) + (m & 3);
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kSmallWaves; ++w) v += p[w * C::FR * C::NC * 256];
+    return v;
+  };
+  for (int64_t e = threadIdx.x; e < PAIRS * B; e += 64 * kSmallWaves) {
+    const int m = static_cast<int>(e / B), b = static_cast<int>(e % B);
+    if (i0 + m >= s.kept) break;
+    const int64_t n = s.offset + static_cast<int64_t>(i0 + m) * s.period;
+    float g = sum(0, m, b), u = PAIRS == 16 ? sum(C::FR - 1, m, b) : sum(0, m + 8, b);
+    if (bias) g += bias[n], u += bias[s.N + n];
+    H[n * B + b] = from_f32<T>(scale * act_of<T>(act, g).f * u);
+    if (Z) {
+      Z[n * B + b] = from_f32<T>(g);
+      Z[(s.N + n) * B + b] = from_f32<T>(u);
+    }
+  }
+  // the dropped rows behind each kept one (and those in front of the first)
+  if (s.zero && s.period > 1) {
+    const int64_t first = i0 == 0 ? 0 : s.offset + static_cast<int64_t>(i0) * s.period;
+    const int64_t end = i0 + PAIRS >= s.kept ? s.N : s.offset + static_cast<int64_t>(i0 + PAIRS) * s.period;
+    for (int64_t e = first * B + threadIdx.x; e < end * B; e += 64 * kSmallWaves)
+      if (static_cast<int32_t>(e / B % s.period) != s.offset) H[e] = from_f32<T>(0.0f);
+  }
+}
+
+// ------------------------------------------------------------------ one product
+// Both projections in one product of the fast kernel's tiles: a tile's rows are blocks
+// of 32 kept gate rows and the same 32 units' other rows in turn, so that a wave holds
+// g and u of the same places in neighbouring accumulators, and activation and product
+// are the epilogue: nothing of the 2 x kept x batch sums passes through memory in fp32.
+// Bound by the matrix cores.
+struct GluTileArgs {
+  GluShape s;
+  const void* X;
+  const void* W;
+  const float* bias;
+  void* Z;
+  void* H;
+  int32_t act;
+  float scale;
+};
+
+// LDS: the stages, then the outputs of each wave on their way out (g, u, h: 32 rows
+// each, and the biases of its units).
+template <class Cfg, int LD>
+struct GluLds {
+  static constexpr int ROW = Cfg::TN * 2 + 16, PART = 32 * ROW, PAIRS = Cfg::TM / 2;
+  static constexpr int WAVE = 3 * PART + 2 * PAIRS * 4;
+  static constexpr int STAGES = LD == LOAD_ANY ? Cfg::LDS_REG : Cfg::LDS;
+  static constexpr int BYTES = Cfg::NW * WAVE > STAGES ? Cfg::NW * WAVE : STAGES;
+};
+
+template <class Cfg, int LD>
+__global__ void __launch_bounds__(Cfg::NT) glu_tile_kernel(GluTileArgs g) {
+  static_assert(Cfg::TM % 64 == 0 && Cfg::KSPLIT == 1 && Cfg::ES == 2, "whole pairs of 32 rows in a wave");
+  constexpr int ES = Cfg::ES;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const GluShape& s = g.s;
+  int tile_row, tile_col;
+  grouped_tile(blockIdx.x, (s.B + Cfg::BN - 1) / Cfg::BN, (s.kept + Cfg::BM / 2 - 1) / (Cfg::BM / 2), tile_row, tile_col);
+  const int p0 = tile_row * (Cfg::BM / 2), n0 = tile_col * Cfg::BN;  // first pair, first column
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wv / Cfg::WGN, wn = wv % Cfg::WGN;
+  f32x16 acc[Cfg::FM][Cfg::FN];
+#pragma unroll
+  for (int i = 0; i < Cfg::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < Cfg::FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  const int nslab = (s.K + Cfg::BK - 1) / Cfg::BK;
+  auto row_of = [&](int r) {  // tile row -> row of W[2 N][K]; past the last pair: the last one, discarded
+    const int p = min(p0 + (r >> 6) * 32 + (r & 31), s.kept - 1);
+    return ((r >> 5) & 1) * s.N + s.offset + p * s.period;
+  };
+  using Loader = typename std::conditional<LD == LOAD_ANY, RegLoader<Cfg, false, true>, SlabLoader<Cfg, false, true>>::type;
+  Loader ld;
+  ld.wv = wv;
+  ld.da.init_rows(s.K, row_of, wv);
+  ld.db.init(s.B, n0, s.B, wv);
+  ld.K = s.K;
+  ld.ik = 0;
+  ld.a_step = static_cast<int64_t>(Cfg::BK) * ES;
+  ld.b_step = static_cast<int64_t>(s.B) * Cfg::BK * ES;
+  ld.a_wrap = ld.b_wrap = 0;
+  ld.na = uniform_ptr(static_cast<const char*>(g.W));
+  ld.nb = uniform_ptr(static_cast<const char*>(g.X));
+  if constexpr (LD == LOAD_ANY) {
+    run_slabs_reg<Cfg, false, true, false>(ld, nslab, acc, wm, wn, 0, smem, nullptr);
+  } else {
+    ld.lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+    ld.is = 0;
+    ld.left = nslab - 1;
+    run_slabs<Cfg, false, true, true, false>(ld, nslab, s.K, 0, acc, wm, wn, 0, smem);
+  }
+
+  // Each block of 32 units passes through the wave's own LDS, g, u and h side by side,
+  // and is written 16 bytes of a row at a time. The units' biases come first, every
+  // load in flight together.
+  using L = GluLds<Cfg, LD>;
+  constexpr int ROW = L::ROW, PART = L::PART, CPRW = Cfg::TN / 8, RPI = 64 / CPRW, PAIRS = L::PAIRS;
+  lds_barrier();  // every wave is done with the stages
+  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
+  char* region = smem + wv * L::WAVE;
+  float* bl = reinterpret_cast<float*>(region + 3 * PART);
+  const int pw = p0 + wm * PAIRS;  // the wave's first pair
+  auto unit = [&](int p) { return s.offset + static_cast<int64_t>(pw + p) * s.period; };
+  if (g.bias) {
+#pragma unroll
+    for (int e = 0; e < 2 * PAIRS; e += 64)
+      if (e + lane < 2 * PAIRS) {
+        const int p = (e + lane) % PAIRS;
+        bl[e + lane] = g.bias[(e + lane) / PAIRS * static_cast<int64_t>(s.N) + unit(min(pw + p, s.kept - 1) - pw)];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < Cfg::FM; i += 2) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int rl = 8 * (r >> 2) + 4 * lh + (r & 3);
+      const float b0 = g.bias ? bl[16 * i + rl] : 0.0f, b1 = g.bias ? bl[PAIRS + 16 * i + rl] : 0.0f;
+#pragma unroll
+      for (int j = 0; j < Cfg::FN; ++j) {
+        const float x = acc[i][j][r] + b0, u = acc[i + 1][j][r] + b1;
+        bf16* at = reinterpret_cast<bf16*>(region + rl * ROW) + 32 * j + lr;
+        if (g.Z) {
+          at[0] = static_cast<bf16>(x);
+          at[PART / 2] = static_cast<bf16>(u);
+        }
+        at[PART] = static_cast<bf16>(g.scale * act_of<bf16>(g.act, x).f * u);
+      }
+    }
+    for (int part = g.Z ? 0 : 2; part < 3; ++part) {
+      bf16* out = part == 2 ? static_cast<bf16*>(g.H)
+                            : static_cast<bf16*>(g.Z) + (part == 1 ? static_cast<int64_t>(s.N) * s.B : 0);
+#pragma unroll
+      for (int t = 0; t < 32 / RPI; ++t) {
+        const int rl = lane / CPRW + RPI * t, n = n0 + wn * Cfg::TN + 8 * (lane % CPRW);
+        const char* from = region + part * PART + rl * ROW + (lane % CPRW) * 16;
+        if (pw + 16 * i + rl >= s.kept || n >= s.B) continue;
+        bf16* o = out + unit(16 * i + rl) * s.B + n;
+        typedef u32x4 u32x4_a2 __attribute__((aligned(2), may_alias));
+        if (n + 8 <= s.B) {
+          *reinterpret_cast<u32x4_a2*>(o) = *reinterpret_cast<const u32x4*>(from);
+        } else {
+          for (int e = 0; n + e < s.B; ++e) o[e] = reinterpret_cast<const bf16*>(from)[e];
+        }
+      }
+    }
+  }
+}
+
+// Clears the dropped rows of H.
 template <typename T>
+__global__ void __launch_bounds__(256) glu_clear_kernel(GluShape s, T* __restrict__ H) {
+  const int64_t n = blockIdx.x;
+  if (static_cast<int32_t>(n % s.period) == s.offset) return;
+  T* h = H + n * s.B;
+  constexpr int E = 16 / static_cast<int>(sizeof(T));
+  if (s.B % E == 0) {
+    for (int b = threadIdx.x; b < s.B / E; b += 256) reinterpret_cast<u32x4*>(h)[b] = u32x4{0u, 0u, 0u, 0u};
+  } else {
+    for (int b = threadIdx.x; b < s.B; b += 256) h[b] = from_f32<T>(0.0f);
+  }
+}
+
+// The derivatives D[2][kept][ldd] and their row sums, a workgroup per hidden unit; that
+// of a dropped one clears its rows of dW and entries of dbias, if asked. Bound by
+// reading g, u and dH and writing both derivatives (16 bytes of a lane at a time where
+// the rows start on 16).
+template <typename T, typename G>
 __global__ void __launch_bounds__(256) glu_derive_kernel(GluShape s, const T* __restrict__ Z,
-                                                         const T* __restrict__ dH, int act, float scale,
-                                                         T* __restrict__ D, float* __restrict__ dbias) {
-  const int64_t i = blockIdx.x, n = s.offset + i * s.period;
+                                                         const T* __restrict__ dH, int act, float scale, int vec,
+                                                         T* __restrict__ D, G* __restrict__ dW,
+                                                         float* __restrict__ dbias) {
+  const int64_t n = blockIdx.x;
+  if (static_cast<int32_t>(n % s.period) != s.offset) {
+    if (!s.zero) return;
+    if (dW) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        G* row = dW + (h * static_cast<int64_t>(s.N) + n) * s.K;
+        constexpr int E = 16 / static_cast<int>(sizeof(G));
+        if (static_cast<int64_t>(s.K) * sizeof(G) % 16 == 0) {
+          for (int64_t k = threadIdx.x; k < s.K / E; k += 256)
+            reinterpret_cast<u32x4*>(row)[k] = u32x4{0u, 0u, 0u, 0u};
+        } else {
+          for (int64_t k = threadIdx.x; k < s.K; k += 256) row[k] = from_f32<G>(0.0f);
+        }
+      }
+    }
+    if (dbias && threadIdx.x < 2) dbias[threadIdx.x * static_cast<int64_t>(s.N) + n] = 0.0f;
+    return;
+  }
+  const int64_t i = (n - s.offset) / s.period;
   const T *gp = Z + n * s.B, *up = Z + (s.N + n) * s.B, *hp = dH + n * s.B;
   T *dg = D + i * s.ldd, *du = D + (s.kept + i) * s.ldd;
   float sg = 0.0f, su = 0.0f;
-  for (int b = threadIdx.x; b < s.B; b += 256) {
-    const Act a = act_of(act, to_f32(gp[b]));
-    const float d = scale * to_f32(hp[b]), g = d * to_f32(up[b]) * a.d, u = d * a.f;
-    dg[b] = from_f32<T>(g);
-    du[b] = from_f32<T>(u);
-    sg += g;
-    su += u;
+  auto one = [&](float z, float u, float h, float& og, float& ou) {
+    const Act a = act_of<T>(act, z);
+    const float d = scale * h;
+    og = d * u * a.d;
+    ou = d * a.f;
+    sg += og;
+    su += ou;
+  };
+  if (vec) {
+    constexpr int E = 16 / static_cast<int>(sizeof(T));
+    for (int b = threadIdx.x * E; b < s.B; b += 256 * E) {
+      const u32x4 rg = *reinterpret_cast<const u32x4*>(gp + b), ru = *reinterpret_cast<const u32x4*>(up + b);
+      const u32x4 rh = *reinterpret_cast<const u32x4*>(hp + b);
+      u32x4 og, ou;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        float x, y;
+        one(to_f32(reinterpret_cast<const T*>(&rg)[e]), to_f32(reinterpret_cast<const T*>(&ru)[e]),
+            to_f32(reinterpret_cast<const T*>(&rh)[e]), x, y);
+        reinterpret_cast<T*>(&og)[e] = from_f32<T>(x);
+        reinterpret_cast<T*>(&ou)[e] = from_f32<T>(y);
+      }
+      *reinterpret_cast<u32x4*>(dg + b) = og;
+      *reinterpret_cast<u32x4*>(du + b) = ou;
+    }
+  } else {
+    for (int b = threadIdx.x; b < s.B; b += 256) {
+      float x, y;
+      one(to_f32(gp[b]), to_f32(up[b]), to_f32(hp[b]), x, y);
+      dg[b] = from_f32<T>(x);
+      du[b] = from_f32<T>(y);
+    }
   }
   if (!dbias) return;
   __shared__ float red[8];
@@ -96,16 +481,6 @@ __global__ void __launch_bounds__(256) glu_derive_kernel(GluShape s, const T* __
     dbias[n] = (red[0] + red[1]) + (red[2] + red[3]);
     dbias[s.N + n] = (red[4] + red[5]) + (red[6] + red[7]);
   }
-}
-
-// Clears the dropped rows of dW[2][N][K] and entries of dbias[2][N].
-template <typename T>
-__global__ void __launch_bounds__(256) glu_clear_kernel(GluShape s, T* __restrict__ dW, float* __restrict__ dbias) {
-  const int64_t n = blockIdx.x;  // of 2 N
-  if (static_cast<int32_t>(n % s.N % s.period) == s.offset) return;
-  if (dW)
-    for (int64_t k = threadIdx.x; k < s.K; k += 256) dW[n * s.K + k] = from_f32<T>(0.0f);
-  if (dbias && threadIdx.x == 0) dbias[n] = 0.0f;
 }
 
 // 0 to every 16 bytes and the rest behind them (a fill kernel: a caller may capture the call).
@@ -176,6 +551,39 @@ size_t partial_floats(int M, int N, int K, int kbatch, int batch) {
   return s > 1 ? static_cast<size_t>(s) * batch * M * N : 0;
 }
 
+// Whether the forward runs on glu_small_kernel. Measured against the products and the
+// join (4096 -> 8192 / 1024 -> 2048, us): bf16 batch 1 30.7 to 92.0 / 9 to 16, 16 32.9 to
+// 42.6 / 9 to 12.5, 64 43.5 to 46.0 / 9 to 12.5; fp32 batch 1 57 to 77 / 9 to 17, 16 67 to
+// 66 / 9 to 17, but 32 81 to 66 and 64 137 to 96 / 14 to 14.
+bool small_batch(const GluShape& s) { return s.B <= (s.es == 2 ? 64 : 16) && s.kept > 0; }
+
+// The tile of glu_tile_kernel with the least modelled time: rounds of the chip times a
+// tile's work over the rate that it reaches with the chip full (FastKind; -1: none). bf16
+// only: fp32 products are planned by the layers' cost model, split contractions and
+// 64 x 64 tiles included, and what a fused epilogue saved there (1 to 5 us) the tiles
+// with 64 rows in a wave lost several times over (700 x 1500 -> 2000 units 113 to 94 us).
+int plan_tile(const GluShape& s) {
+  if (s.es != 2 || 4 * static_cast<int64_t>(s.N) * s.K + 4096 >= int64_t{1} << 31 ||
+      514 * static_cast<int64_t>(s.B) >= int64_t{1} << 31)
+    return -1;
+  struct Tile {
+    int kind, bm, bn;
+    double rate;  // flop/s of a compute unit
+  };
+  static constexpr Tile tiles[] = {
+      {FAST_HUGE, 256, 256, 4.2e12}, {FAST_WIDE, 128, 256, 3.5e12}, {FAST_TALL, 256, 128, 3.4e12}, {FAST_BIG, 128, 128, 2.7e12}};
+  int best = -1;
+  double best_t = 1e300;
+  for (const Tile& c : tiles) {
+    const int64_t n = (static_cast<int64_t>(s.kept) + c.bm / 2 - 1) / (c.bm / 2) * ((s.B + c.bn - 1) / c.bn);
+    if (n < kTargetBlocks * 5 / 8) continue;
+    const double t = static_cast<double>((n + kTargetBlocks - 1) / kTargetBlocks) * 2.0 * c.bm * c.bn * s.K / c.rate;
+    if (t < best_t) best_t = t, best = c.kind;
+  }
+  return best;
+}
+bool one_product(const GluShape& s) { return s.kept > 0 && !small_batch(s) && plan_tile(s) >= 0; }
+
 // The workspace: what the products read or write first, their partial sums behind it.
 struct Space {
   size_t head, part;
@@ -183,7 +591,7 @@ struct Space {
 };
 template <typename T>
 Space fwd_space(const GluShape& s) {
-  if (s.kept == 0) return {0, 0};
+  if (s.kept == 0 || small_batch(s) || one_product(s)) return {0, 0};
   return {al256(static_cast<size_t>(2) * s.kept * s.B * 4), al256(4 * partial_floats<T>(s.kept, s.B, s.K, 1, 2))};
 }
 template <typename T>
@@ -228,9 +636,76 @@ hipError_t product(const GemmArgs& g, int batch, hipStream_t stream, float* part
                                                                 floats ? partial : nullptr);
 }
 
+template <typename T, int PAIRS, int NB>
+hipError_t launch_small_pairs(const ard_glu_desc* d, const GluShape& s, const void* X, const void* W, const float* bias,
+                              void* Z, void* H, hipStream_t stream) {
+  using C = Small<T, PAIRS, NB>;
+  auto kern = glu_small_kernel<T, PAIRS, NB>;
+  static const hipError_t attr =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL(kern, dim3((s.kept + PAIRS - 1) / PAIRS), dim3(64 * kSmallWaves), C::LDS, stream, s,
+                     static_cast<const T*>(X), static_cast<const T*>(W), bias, d->act, d->scale, static_cast<T*>(Z),
+                     static_cast<T*>(H));
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_small_fwd(const ard_glu_desc* d, const GluShape& s, const void* X, const void* W, const float* bias,
+                            void* Z, void* H, hipStream_t stream) {
+  const bool eight = s.kept < 4096;  // 16 units of each would leave compute units without work
+  auto with = [&](auto nb) {
+    constexpr int NB = decltype(nb)::value;
+    return eight ? launch_small_pairs<T, 8, NB>(d, s, X, W, bias, Z, H, stream)
+                 : launch_small_pairs<T, 16, NB>(d, s, X, W, bias, Z, H, stream);
+  };
+  using std::integral_constant;
+  if (s.B == 1) return with(integral_constant<int, 0>{});
+  if constexpr (sizeof(T) == 2) {
+    if (s.B > 32) return with(integral_constant<int, 4>{});
+    if (s.B > 16) return with(integral_constant<int, 2>{});
+  }
+  return with(integral_constant<int, 1>{});
+}
+
+template <class Cfg, int LD>
+hipError_t launch_tile(const GluTileArgs& g, hipStream_t stream) {
+  auto kern = glu_tile_kernel<Cfg, LD>;
+  constexpr int LDS = GluLds<Cfg, LD>::BYTES;
+  static const hipError_t attr =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  if (attr != hipSuccess) return attr;
+  const unsigned tiles = static_cast<unsigned>((g.s.kept + Cfg::BM / 2 - 1) / (Cfg::BM / 2)) *
+                         static_cast<unsigned>((g.s.B + Cfg::BN - 1) / Cfg::BN);
+  hipLaunchKernelGGL(kern, dim3(tiles), dim3(Cfg::NT), LDS, stream, g);
+  return hipGetLastError();
+}
+hipError_t run_tile(const GluTileArgs& g, hipStream_t stream) {
+  using C = FastCfgs<bf16>;
+  // rows off 16 bytes: register loads, of which a 256-wide tile has too few to spare
+  if (g.s.K % 8 || g.s.B % 8) return launch_tile<C::Big, LOAD_ANY>(g, stream);
+  switch (plan_tile(g.s)) {
+    case FAST_HUGE: return launch_tile<C::Huge, LOAD_DMA>(g, stream);
+    case FAST_WIDE: return launch_tile<C::Wide, LOAD_DMA>(g, stream);
+    case FAST_TALL: return launch_tile<C::Tall, LOAD_DMA>(g, stream);
+    default: return launch_tile<C::Big, LOAD_DMA>(g, stream);
+  }
+}
+
 template <typename T>
 int fwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const void* W, const float* bias, void* Zt,
              void* Ht, char* ws, hipStream_t stream) {
+  if (small_batch(s)) {
+    ARD_HIP_CHECK(launch_small_fwd<T>(d, s, Xt, W, bias, Zt, Ht, stream));
+    return ARD_OK;
+  }
+  if (one_product(s)) {
+    ARD_HIP_CHECK(run_tile(GluTileArgs{s, Xt, W, bias, Zt, Ht, d->act, d->scale}, stream));
+    if (s.zero && s.period > 1) {
+      hipLaunchKernelGGL(glu_clear_kernel<T>, dim3(s.N), dim3(256), 0, stream, s, static_cast<T*>(Ht));
+      ARD_LAUNCH_CHECK();
+    }
+    return ARD_OK;
+  }
   const Space sp = fwd_space<T>(s);
   float* zf = reinterpret_cast<float*>(ws);
   if (s.kept > 0) {
@@ -253,12 +728,14 @@ int bwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
   const Space sp = bwd_space<T>(s);
   float* part = reinterpret_cast<float*>(ws + sp.head);
   const int64_t half = static_cast<int64_t>(s.kept) * s.ldd;
+  const int vec = static_cast<int64_t>(s.B) * s.es % 16 == 0;
+  hipLaunchKernelGGL((glu_derive_kernel<T, G>), dim3(s.N), dim3(256), 0, stream, s, static_cast<const T*>(Zt),
+                     static_cast<const T*>(dHt), d->act, d->scale, vec, reinterpret_cast<T*>(ws), static_cast<G*>(dW),
+                     dbias);
+  ARD_LAUNCH_CHECK();
   if (s.kept == 0) {  // nothing is kept: nothing depends on the input
     if (dXt) ARD_HIP_CHECK(fill_zero(dXt, static_cast<size_t>(s.K) * s.B * s.es, stream));
   } else {
-    hipLaunchKernelGGL(glu_derive_kernel<T>, dim3(s.kept), dim3(256), 0, stream, s, static_cast<const T*>(Zt),
-                       static_cast<const T*>(dHt), d->act, d->scale, reinterpret_cast<T*>(ws), dbias);
-    ARD_LAUNCH_CHECK();
     GemmArgs g = {};
     if (dXt) {
       g.M = s.K, g.N = s.B, g.K = s.kept, g.kbatch = 2;
@@ -277,10 +754,6 @@ int bwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
       g.c.bstride = static_cast<int64_t>(s.N) * s.K;
       ARD_HIP_CHECK((product<T, false, false, G>(g, 2, stream, part, sp.part / 4)));
     }
-  }
-  if (s.zero && s.period > 1 && (dW || dbias)) {
-    hipLaunchKernelGGL(glu_clear_kernel<G>, dim3(2 * s.N), dim3(256), 0, stream, s, static_cast<G*>(dW), dbias);
-    ARD_LAUNCH_CHECK();
   }
   return ARD_OK;
 }
