@@ -76,20 +76,19 @@ struct Decay {
 };
 
 // ------------------------------------------------------------------ LDS tiles
-// [rows][COLS] of 16-byte chunks, chunk c of row r at position c ^ swz(r), so that
-// neither 16 rows at one chunk (operands contiguous along the contraction) nor
-// rows r .. r + 3 and r + 8 .. r + 11 at neighbouring chunks (transposed reads, and
-// fp32's element reads of four rows) meet in a bank. swz depends on r % 16 only.
+// [rows][COLS] of 16-byte chunks, chunk c of row r at position c ^ swz(r): free of bank
+// conflicts for 16 rows at one chunk (operands along the contraction; a pass of the
+// 16-byte reads takes rows 0-3 and 12-15 of one chunk with rows 4-11 of the next), for
+// rows {0, 1, 4, 5} + 8 g at two neighbouring chunks (transposed reads) and for four
+// neighbouring rows at four chunks (fp32 elements). swz depends on r % 16 only.
 template <int ES, int COLS>
 __device__ __forceinline__ int swz(int r) {
-  if constexpr (COLS * ES / 16 == 8) {
-    const int h = (r >> 1) & 7;
-    return ((h & 1) << 1) | (h & 4) | ((h >> 1) & 1);
-  } else if constexpr (ES == 4) {
-    return ((r & 3) << 2) | ((r >> 2) & 3);
-  } else {
-    return ((r & 3) << 1) | (r & 8);
-  }
+  if constexpr (COLS * ES / 16 == 8)
+    return (r >> 1) & 7;
+  else if constexpr (ES == 4)
+    return ((r & 3) << 2) | (((r >> 2) & 3) ^ ((r >> 1) & 2));
+  else
+    return ((r & 1) << 1) | (r & 12) | ((r >> 1) & 1);
 }
 template <int ES, int COLS>
 __device__ __forceinline__ int tile_off(int r, int c) {
@@ -122,20 +121,23 @@ struct Ops<bf16> {
     return *reinterpret_cast<const bf16x8*>(t + row * COLS * 2 + (base ^ (col * 2)));
   }
   struct Base {
-    int lo, hi;  // rows 8 g + 0 .. 3 and + 4 .. 7
+    int lo, hi;  // rows 8 g + {0, 1, 4, 5} and + {2, 3, 6, 7}
   };
   template <int COLS>
   static __device__ __forceinline__ Base base_across() {
-    const int lane = threadIdx.x & 63, s = lane & 15, r = 8 * (lane >> 4) + (s >> 2), c = 4 * (s & 3);
-    return {tile_off<2, COLS>(r, c >> 3) + (c & 7) * 2, tile_off<2, COLS>(r + 4, c >> 3) + (c & 7) * 2};
+    const int lane = threadIdx.x & 63, s = lane & 15, c = 4 * (s & 3);
+    const int r = 8 * (lane >> 4) + ((s >> 2) & 1) + 4 * (s >> 3);
+    return {tile_off<2, COLS>(r, c >> 3) + (c & 7) * 2, tile_off<2, COLS>(r + 2, c >> 3) + (c & 7) * 2};
   }
   template <int COLS>
   static __device__ __forceinline__ Across across(const char* t, Base base, int row, int col) {
     const char* p0 = t + row * COLS * 2 + (base.lo ^ (col * 2));
     const char* p1 = t + row * COLS * 2 + (base.hi ^ (col * 2));
-    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p0));
-    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p1));
-    return __builtin_shufflevector(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+    const bf16x4 lo = __builtin_bit_cast(
+        bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p0)));
+    const bf16x4 hi = __builtin_bit_cast(
+        bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p1)));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
   // The four columns 4 g .. of a row, 16 rows: how a lane holds a product's block.
   template <int COLS>
@@ -173,7 +175,7 @@ struct Ops<float> {
   }
   template <int COLS>
   static __device__ __forceinline__ Across across(const char* t, Base base, int row, int col) {
-    return *reinterpret_cast<const float*>(t + row * COLS * 4 + (base ^ (col * 4) ^ (((row >> 2) & 3) << 4)));
+    return *reinterpret_cast<const float*>(t + row * COLS * 4 + (base ^ (col * 4) ^ ((((row >> 2) & 3) ^ ((row >> 1) & 2)) << 4)));
   }
   template <int COLS>
   static __device__ __forceinline__ int base_block() {
@@ -592,6 +594,240 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   }
 }
 
+// dK and dV together (bf16). Both run backward from the same state G: with
+// R = G,  dV_i = sum a^{j-i} (k_i . q_j) dO_j + a^{n-1-i} k_i R
+// R^T:    dK_i = sum a^{j-i} (v_i . dO_j) q_j + a^{n-1-i} R v_i,   R <- a^L R + q'^T dO,
+// so that the four inputs are read and the state is carried once. Of eight waves four
+// compute 16 tokens of dV each and four the same of dK (the state in LDS is read across
+// its rows or along them); all share the state's update. Against one run for each: 4
+// sequences of 4096 tokens, 16 heads of 128, dK and dV 247 us one after the
+// other (states and outputs), together 171 us.
+struct PairArgs {
+  MixArgs m;  // y = q (ydim: key rows), w = dO (wdim: value rows), segments, states
+  const void* k;
+  const void* v;
+  void* dk;  // of the element type, or fp32 to be added over the heads of a group
+  void* dv;
+};
+
+template <int KD_, int VD_, bool PART_, int PARTS_>
+struct Pair {
+  using T = bf16;
+  static constexpr int YD = KD_, WD = VD_;
+  static constexpr bool PART = PART_;
+  static constexpr int PARTS = PARTS_, NW = 8, NT = 512, ES = 2, OS = PART ? 4 : 2;
+  // the state: a wave holds 16 rows of q by WBW blocks of 16 rows of dO
+  static constexpr int YW = YD / 16, WBW = WD / 16 / (NW / YW);
+  static constexpr int YT = YD * kChunk * ES, WT = WD * kChunk * ES, ST = YD * WD * ES;
+  static constexpr int LDS = 2 * YT + 2 * WT + ST + (YD + WD) * kChunk * OS;
+};
+
+template <class P>
+__global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
+  using T = bf16;
+  using O = Ops<bf16>;
+  using OutT = typename std::conditional<P::PART, float, bf16>::type;
+  using OutOps = Ops<OutT>;
+  const MixArgs& g = pa.m;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  char* Q = smem;
+  char* K = Q + P::YT;
+  char* D = K + P::YT;
+  char* V = D + P::WT;
+  char* S = V + P::WT;
+  char* OutV = S + P::ST;
+  char* OutK = OutV + P::WD * kChunk * P::OS;
+
+  int id = xcd_position(blockIdx.x, gridDim.x);
+  const int seg = id % g.nseg;
+  id /= g.nseg;
+  const int head = id % g.heads, seq = id / g.heads;
+  const Span sp = span_of(g, seq);
+  const int t0 = seg * g.seg_len, t1 = min(sp.len, t0 + g.seg_len);
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t hs = static_cast<int64_t>(seq) * g.heads + head;
+  const int64_t sdim = static_cast<int64_t>(g.ydim) * g.wdim;
+  float* segp = g.seg ? g.seg + (hs * g.nseg + seg) * P::YD * P::WD : nullptr;
+  if (g.nseg > 1 && t0 >= t1) return;  // whole workgroups
+
+  const Decay a(g.decay[head]);
+  const int yb = wv % P::YW, wb = wv / P::YW * P::WBW, grp = lane >> 4;
+  const int srow = yb * 16 + (lane & 15);  // the lane's row of the state
+  f32x4 st[P::WBW];
+#pragma unroll
+  for (int i = 0; i < P::WBW; ++i) st[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (g.nseg > 1) {
+#pragma unroll
+    for (int i = 0; i < P::WBW; ++i)
+      st[i] = reinterpret_cast<const f32x4*>(segp)[(yb * (P::WD / 16) + wb + i) * 64 + lane];
+  } else if (g.s0 && srow < g.ydim) {
+#pragma unroll
+    for (int i = 0; i < P::WBW; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int wr = (wb + i) * 16 + 4 * grp + r;
+        if (wr < g.wdim) st[i][r] = g.s0[hs * sdim + srow * g.wdim + wr];
+      }
+  }
+
+  const int64_t ld = g.tokens;
+  const int kv = head / g.group, nkv = g.heads / g.group;
+  auto start = [&](auto& regs, const void* p, int h, int heads, int dim) {
+    const T* b = static_cast<const T*>(p);
+    regs.init(b + static_cast<int64_t>(h) * dim * ld + sp.first, ld, dim, b, b + static_cast<int64_t>(heads) * dim * ld);
+  };
+  TileRegs<T, P::YD, P::NT> qr, kr;
+  TileRegs<T, P::WD, P::NT> dr, vr;
+  start(qr, g.y, head, g.heads, g.ydim);
+  start(kr, pa.k, kv, nkv, g.ydim);
+  start(dr, g.w, head, g.heads, g.wdim);
+  start(vr, pa.v, kv, nkv, g.wdim);
+
+  const int ib = wv & 3;
+  int at_along = O::base_along<kChunk>(), at_block = O::base_block<kChunk>();
+  int at_state = O::base_block<P::WD>() ^ (wb * 32), at_srow = O::base_along<P::WD>();
+  auto at_cols = O::base_across<kChunk>();
+  auto at_scols = O::base_across<P::WD>();
+  auto at_icols = at_cols;
+  at_icols.lo ^= ib * 32, at_icols.hi ^= ib * 32;
+  const int at_out = OutOps::template base_block<kChunk>() ^ (ib * 16 * P::OS);
+
+  const int nchunk = (t1 - t0 + kChunk - 1) / kChunk;
+  auto first_of = [&](int c) { return t0 + (nchunk - 1 - c) * kChunk; };
+  auto fetch = [&](int c) {
+    const int t = first_of(c);
+    if (t1 - t >= kChunk) {
+      qr.load(t), kr.load(t), dr.load(t), vr.load(t);
+    } else {
+      qr.load_part(t), kr.load_part(t), dr.load_part(t), vr.load_part(t);
+    }
+  };
+  // weights as in mix_kernel, running backward
+  f32x4 pw[4], wx;
+#pragma unroll
+  for (int jb = 0; jb < 4; ++jb)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int n = 16 * (jb - ib) + 4 * grp + r - (lane & 15);
+      pw[jb][r] = n >= 0 ? g.cp * a.pow(n) : 0.0f;
+    }
+  int weighed = -1;
+
+  if (nchunk > 0) fetch(0);
+  for (int c = 0; c < nchunk; ++c) {
+    const int t = first_of(c), L = min(kChunk, t1 - t);
+    // the addresses that follow from these are computed in each chunk: kept from one to
+    // the next, some 60 of them, they would push the accumulators into scratch memory
+    asm volatile("" : "+v"(at_along), "+v"(at_block), "+v"(at_state), "+v"(at_srow), "+v"(at_cols.lo), "+v"(at_cols.hi),
+                 "+v"(at_scols.lo), "+v"(at_scols.hi));
+    qr.store(Q, t, L);
+    kr.store(K, t, L);
+    dr.store(D, t, L);
+    vr.store(V, t, L);
+#pragma unroll
+    for (int i = 0; i < P::WBW; ++i)
+      *O::block<P::WD>(S + yb * 16 * P::WD * P::ES, at_state, 0, 16 * i) = O::round(st[i]);
+    lds_barrier();
+    if (c + 1 < nchunk) fetch(c + 1);
+    if (L != weighed) {
+      weighed = L;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) wx[r] = g.cx * a.pow(max(L - 1 - (16 * ib + 4 * grp + r), 0));
+    }
+    // 16 tokens of dV or dK: X and Y meet in the inner products, W follows them, OD rows out
+    auto outputs = [&](auto of_v, char* X, char* Y, char* W, char* Out) {
+      constexpr bool OFV = decltype(of_v)::value;
+      constexpr int XD = OFV ? P::YD : P::WD, OB = (OFV ? P::WD : P::YD) / 16;
+      f32x4 acc[OB], p[4];
+#pragma unroll
+      for (int b = 0; b < OB; ++b) acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int jb = 0; jb < 4; ++jb) p[jb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < XD; k += 32) {
+        const bf16x8 xf = O::across<kChunk>(X, at_icols, k, 0);
+        const bf16x8 xo = OFV ? xf : __builtin_shufflevector(xf, xf, 0, 1, 4, 5, 2, 3, 6, 7);  // its rows in order
+#pragma unroll
+        for (int b = 0; b < OB; ++b) {
+          const bf16x8 sf = OFV ? O::across<P::WD>(S, at_scols, k, 16 * b) : O::along<P::WD>(S, at_srow, 16 * b, k);
+          acc[b] = O::mma(xo, sf, acc[b]);
+        }
+#pragma unroll
+        for (int jb = 0; jb < 4; ++jb) p[jb] = O::mma(O::across<kChunk>(Y, at_cols, k, 16 * jb), xf, p[jb]);
+      }
+#pragma unroll
+      for (int b = 0; b < OB; ++b) acc[b] *= wx;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 pf = __builtin_shufflevector(O::round(p[2 * h] * pw[2 * h]), O::round(p[2 * h + 1] * pw[2 * h + 1]),
+                                                  0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int b = 0; b < OB; ++b) {
+          const bf16x4 lo = *O::block<kChunk>(W, at_block, 16 * b, 32 * h);
+          const bf16x4 hi = *O::block<kChunk>(W, at_block, 16 * b, 32 * h + 16);
+          acc[b] = O::mma(pf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), acc[b]);
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < OB; ++b) *OutOps::template block<kChunk>(Out, at_out, 16 * b, 0) = OutOps::round(acc[b]);
+    };
+    if (wv < 4) outputs(std::true_type{}, K, Q, D, OutV);
+    else outputs(std::false_type{}, V, D, Q, OutK);
+    // the state in front of this chunk
+    const float aL = a.pow(L);
+#pragma unroll
+    for (int i = 0; i < P::WBW; ++i) st[i] *= aL;
+#pragma unroll
+    for (int k = 0; k < kChunk; k += 32) {
+      const bf16x8 yf = O::along<kChunk>(Q + yb * 16 * kChunk * P::ES, at_along, 0, k);
+      Decay here = a;  // its weights, too, are computed in each chunk
+      asm volatile("" : "+v"(here.l2));
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(yf[e]) * (g.cy * here.pow(k + 8 * grp + e + 1));
+      bf16x8 ys[P::PARTS];
+      split(f, ys);
+#pragma unroll
+      for (int i = 0; i < P::WBW; ++i) {
+        const bf16x8 wf = O::along<kChunk>(D + wb * 16 * kChunk * P::ES, at_along, 16 * i, k);
+#pragma unroll
+        for (int q = P::PARTS - 1; q >= 0; --q) st[i] = O::mma(wf, ys[q], st[i]);
+      }
+    }
+    lds_barrier();  // the outputs are whole; no wave reads the tiles or the state any more
+    auto put = [&](char* Out, void* to, int dim, auto rows_c) {
+      constexpr int EPC = 16 / P::OS, CPR = kChunk * P::OS / 16, ROWS = decltype(rows_c)::value;
+      if (!to) return;
+      OutT* op = static_cast<OutT*>(to) + static_cast<int64_t>(head) * dim * ld + sp.first + t;
+      typedef u32x4 u32x4_any __attribute__((aligned(2), may_alias));
+#pragma unroll
+      for (int q = 0; q < ROWS * CPR / P::NT; ++q) {
+        const int at = q * P::NT + threadIdx.x, r = at / CPR, cc = at % CPR, n = L - cc * EPC;
+        if (r >= dim || n <= 0) continue;
+        const char* from = Out + tile_off<P::OS, kChunk>(r, cc);
+        OutT* o = op + r * ld + cc * EPC;
+        if (n >= EPC) {
+          *reinterpret_cast<u32x4_any*>(o) = *reinterpret_cast<const u32x4*>(from);
+        } else {
+#pragma unroll 1
+          for (int u = 0; u < n; ++u) o[u] = reinterpret_cast<const OutT*>(from)[u];
+        }
+      }
+    };
+    put(OutV, pa.dv, g.wdim, std::integral_constant<int, P::WD>{});
+    put(OutK, pa.dk, g.ydim, std::integral_constant<int, P::YD>{});
+  }
+  if (g.nseg == 1 && g.sT && srow < g.ydim) {
+#pragma unroll
+    for (int i = 0; i < P::WBW; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int wr = (wb + i) * 16 + 4 * grp + r;
+        if (wr < g.wdim) g.sT[hs * sdim + srow * g.wdim + wr] = st[i][r];
+      }
+  }
+}
+
 // Segment states -> the state in front of each segment, in running order, and the
 // last one. Four neighbouring accumulators of a thread.
 template <class M>
@@ -644,16 +880,17 @@ __global__ void __launch_bounds__(256) mix_scan_kernel(MixArgs g) {
 // out[head][row][token] = the sum over the heads of a group, for the tokens of the
 // sequences.
 template <typename T>
-__global__ void __launch_bounds__(256) mix_group_kernel(MixArgs g, T* __restrict__ out) {
-  const int64_t head = blockIdx.y / g.wdim, r = blockIdx.y % g.wdim, row = blockIdx.y;
+__global__ void __launch_bounds__(256) mix_group_kernel(MixArgs g, const float* __restrict__ part, int32_t dim,
+                                                        T* __restrict__ out) {
+  const int64_t head = blockIdx.y / dim, r = blockIdx.y % dim, row = blockIdx.y;
   const int per = (g.max_len - 1) / 256 + 1;  // blocks of a sequence
   for (int64_t id = blockIdx.x; id < static_cast<int64_t>(per) * g.n_seqs; id += gridDim.x) {
     const Span sp = span_of(g, static_cast<int>(id / per));
     const int t = static_cast<int>(id % per) * 256 + threadIdx.x;
     if (t >= sp.len) continue;
-    const float* p = static_cast<const float*>(g.out) + (head * g.group * g.wdim + r) * g.tokens + sp.first + t;
+    const float* p = part + (head * g.group * dim + r) * g.tokens + sp.first + t;
     float s = 0.0f;
-    for (int q = 0; q < g.group; ++q) s += p[static_cast<int64_t>(q) * g.wdim * g.tokens];
+    for (int q = 0; q < g.group; ++q) s += p[static_cast<int64_t>(q) * dim * g.tokens];
     out[row * g.tokens + sp.first + t] = from_f32<T>(s);
   }
 }
@@ -782,9 +1019,11 @@ size_t seg_bytes(const ard_linattn_desc* d, int ydim, int wdim) {
   if (p.nseg == 1) return 0;
   return al256(static_cast<size_t>(d->n_seqs) * d->q_heads * p.wtiles * p.nseg * p.yd * p.wd * 4);
 }
+// Gradients of shared heads before they are added: bf16 both at once, fp32 one after the other.
 size_t part_bytes(const ard_linattn_desc* d) {
   if (d->q_heads == d->kv_heads) return 0;
-  return al256(static_cast<size_t>(d->q_heads) * std::max(d->key_dim, d->value_dim) * d->tokens * 4);
+  const int rows = d->dtype == ARD_BF16 ? d->key_dim + d->value_dim : std::max(d->key_dim, d->value_dim);
+  return al256(static_cast<size_t>(d->q_heads) * rows * d->tokens * 4);
 }
 size_t fwd_bytes(const ard_linattn_desc* d) { return seg_bytes(d, d->key_dim, d->value_dim); }
 size_t bwd_bytes(const ard_linattn_desc* d) {
@@ -802,54 +1041,97 @@ hipError_t launch_mix(const MixArgs& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// The states of the segments, and what lies in front of each.
 template <typename T, int YD, int WD, bool REV>
-hipError_t run_mix(const MixArgs& g, bool part, hipStream_t stream) {
-  hipError_t e;
-  if (g.nseg > 1) {
-    using U = Mix<T, YD, WD, REV, false, false>;
-    if ((e = launch_mix<U>(g, stream)) != hipSuccess) return e;
-    hipLaunchKernelGGL(mix_scan_kernel<U>, dim3(g.n_seqs * g.heads * g.wtiles, YD * WD / 1024), dim3(256), 0, stream, g);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  // the segments' states came from the pass above; within one the state ends in outputs only
-  if (g.nseg > 1)
-    return part ? launch_mix<Mix<T, YD, WD, REV, true, true, 2>>(g, stream)
-                : launch_mix<Mix<T, YD, WD, REV, true, false, 2>>(g, stream);
-  return part ? launch_mix<Mix<T, YD, WD, REV, true, true, 3>>(g, stream)
-              : launch_mix<Mix<T, YD, WD, REV, true, false, 3>>(g, stream);
+hipError_t run_states(const MixArgs& g, hipStream_t stream) {
+  using U = Mix<T, YD, WD, REV, false, false>;
+  const hipError_t e = launch_mix<U>(g, stream);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(mix_scan_kernel<U>, dim3(g.n_seqs * g.heads * g.wtiles, YD * WD / 1024), dim3(256), 0, stream, g);
+  return hipGetLastError();
 }
 
+template <typename T, int YD, int WD, bool REV>
+hipError_t run_mix(const MixArgs& g, bool part, hipStream_t stream) {
+  if (g.nseg > 1) {
+    const hipError_t e = run_states<T, YD, WD, REV>(g, stream);
+    if (e != hipSuccess) return e;
+  }
+  // with more than one segment the last state came from the pass above, and a chunk's
+  // own ends in outputs only
+  if constexpr (sizeof(T) == 2) {
+    return g.nseg > 1 ? launch_mix<Mix<T, YD, WD, REV, true, false, 2>>(g, stream)
+                      : launch_mix<Mix<T, YD, WD, REV, true, false, 3>>(g, stream);
+  } else {
+    return part ? launch_mix<Mix<T, YD, WD, REV, true, true>>(g, stream)
+                : launch_mix<Mix<T, YD, WD, REV, true, false>>(g, stream);
+  }
+}
+
+void fill_args(const ard_linattn_desc* d, const MixPlan& p, MixArgs* g) {
+  g->offsets = d->d_offsets;
+  g->n_seqs = d->n_seqs;
+  g->max_len = d->max_len;
+  g->tokens = d->tokens;
+  g->heads = d->q_heads;
+  g->group = d->q_heads / d->kv_heads;
+  g->nseg = p.nseg;
+  g->seg_len = p.seg_len;
+  g->wtiles = p.wtiles;
+  if (p.nseg == 1) g->seg = nullptr;
+}
+
+// Adds the fp32 gradients part[q_heads * dim][tokens] over the heads of a group.
+template <typename T>
+hipError_t add_group(const ard_linattn_desc* d, const MixArgs& g, const float* part, int dim, void* out,
+                     hipStream_t stream) {
+  const int64_t blocks = ((g.max_len - 1) / 256 + 1) * static_cast<int64_t>(g.n_seqs);
+  hipLaunchKernelGGL(mix_group_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 1 << 16)),
+                                               d->kv_heads * dim),
+                     dim3(256), 0, stream, g, part, dim, static_cast<T*>(out));
+  return hipGetLastError();
+}
+
+// part: where a group's gradients go before they are added, or NULL (fp32 only).
 template <typename T, bool REV>
 hipError_t run_mix(const ard_linattn_desc* d, MixArgs g, void* out, float* part, hipStream_t stream) {
   const MixPlan p = plan_mix(d, g.ydim, g.wdim);
-  g.offsets = d->d_offsets;
-  g.n_seqs = d->n_seqs;
-  g.max_len = d->max_len;
-  g.tokens = d->tokens;
-  g.heads = d->q_heads;
-  g.group = d->q_heads / d->kv_heads;
-  g.nseg = p.nseg;
-  g.seg_len = p.seg_len;
-  g.wtiles = p.wtiles;
-  if (p.nseg == 1) g.seg = nullptr;
+  fill_args(d, p, &g);
   if (!out) part = nullptr;  // the last state alone is asked for
   g.out = part ? part : out;
   hipError_t e;
-  const bool pt = part != nullptr;
   if constexpr (sizeof(T) == 2) {
-    if (p.yd == 64 && p.wd == 64) e = run_mix<T, 64, 64, REV>(g, pt, stream);
-    else if (p.yd == 64) e = run_mix<T, 64, 128, REV>(g, pt, stream);
-    else if (p.wd == 64) e = run_mix<T, 128, 64, REV>(g, pt, stream);
-    else e = run_mix<T, 128, 128, REV>(g, pt, stream);
+    static_assert(!REV, "dK and dV are pair_kernel's");
+    if (p.yd == 64 && p.wd == 64) e = run_mix<T, 64, 64, REV>(g, false, stream);
+    else if (p.yd == 64) e = run_mix<T, 64, 128, REV>(g, false, stream);
+    else if (p.wd == 64) e = run_mix<T, 128, 64, REV>(g, false, stream);
+    else e = run_mix<T, 128, 128, REV>(g, false, stream);
   } else {
+    const bool pt = part != nullptr;
     e = p.yd == 64 ? run_mix<T, 64, 64, REV>(g, pt, stream) : run_mix<T, 128, 64, REV>(g, pt, stream);
   }
   if (e != hipSuccess || !part) return e;
-  const int64_t blocks = ((g.max_len - 1) / 256 + 1) * static_cast<int64_t>(g.n_seqs);
-  hipLaunchKernelGGL(mix_group_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 1 << 16)),
-                                               d->kv_heads * g.wdim),
-                     dim3(256), 0, stream, g, static_cast<T*>(out));
-  return hipGetLastError();
+  return add_group<T>(d, g, part, g.wdim, out, stream);
+}
+
+template <int KD, int VD>
+hipError_t run_pair(const PairArgs& a, bool part, hipStream_t stream) {
+  auto go = [&](auto cfg) {
+    using P = decltype(cfg);
+    auto kern = pair_kernel<P>;
+    static const hipError_t attr =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
+    if (attr != hipSuccess) return attr;
+    const unsigned blocks = static_cast<unsigned>(a.m.n_seqs) * a.m.heads * a.m.nseg;
+    hipLaunchKernelGGL(kern, dim3(blocks), dim3(P::NT), P::LDS, stream, a);
+    return hipGetLastError();
+  };
+  if (a.m.nseg > 1) {
+    const hipError_t e = run_states<bf16, KD, VD, true>(a.m, stream);
+    if (e != hipSuccess) return e;
+    return part ? go(Pair<KD, VD, true, 2>{}) : go(Pair<KD, VD, false, 2>{});
+  }
+  return part ? go(Pair<KD, VD, true, 3>{}) : go(Pair<KD, VD, false, 3>{});
 }
 
 template <typename T>
@@ -883,23 +1165,42 @@ int bwd_impl(const ard_linattn_desc* d, const void* Q, const void* K, const void
     r.cy = 1.0f, r.cx = d->scale;
     ARD_HIP_CHECK((run_mix<T, false>(d, r, dQ, nullptr, stream)));
   }
-  if (dK) {
-    MixArgs r = g;
-    r.x = V, r.y = dO, r.w = Q;
-    r.x_shared = 1;
-    r.ydim = d->value_dim, r.wdim = d->key_dim;
-    r.s0 = dST, r.s_trans = 1;
-    r.cy = d->scale, r.cx = 1.0f;
-    ARD_HIP_CHECK((run_mix<T, true>(d, r, dK, part, stream)));
-  }
-  if (dV || dS0) {
-    MixArgs r = g;
-    r.x = K, r.y = Q, r.w = dO;
-    r.x_shared = 1;
+  MixArgs r = g;
+  if constexpr (sizeof(T) == 2) {
+    if (!dK && !dV && !dS0) return ARD_OK;
+    r.y = Q, r.w = dO;
     r.ydim = d->key_dim, r.wdim = d->value_dim;
     r.s0 = dST, r.sT = dS0;
     r.cy = d->scale, r.cx = 1.0f;
-    ARD_HIP_CHECK((run_mix<T, true>(d, r, dV, part, stream)));
+    const MixPlan p = plan_mix(d, r.ydim, r.wdim);
+    fill_args(d, p, &r);
+    float* kp = part && dK ? part : nullptr;
+    float* vp = part && dV ? part + static_cast<size_t>(d->q_heads) * d->key_dim * d->tokens : nullptr;
+    const PairArgs a = {r, K, V, part ? kp : dK, part ? vp : dV};
+    if (p.yd == 64 && p.wd == 64) ARD_HIP_CHECK((run_pair<64, 64>(a, part != nullptr, stream)));
+    else if (p.yd == 64) ARD_HIP_CHECK((run_pair<64, 128>(a, part != nullptr, stream)));
+    else if (p.wd == 64) ARD_HIP_CHECK((run_pair<128, 64>(a, part != nullptr, stream)));
+    else ARD_HIP_CHECK((run_pair<128, 128>(a, part != nullptr, stream)));
+    if (kp) ARD_HIP_CHECK(add_group<T>(d, r, kp, d->key_dim, dK, stream));
+    if (vp) ARD_HIP_CHECK(add_group<T>(d, r, vp, d->value_dim, dV, stream));
+  } else {
+    if (dK) {
+      r.x = V, r.y = dO, r.w = Q;
+      r.x_shared = 1;
+      r.ydim = d->value_dim, r.wdim = d->key_dim;
+      r.s0 = dST, r.s_trans = 1;
+      r.cy = d->scale, r.cx = 1.0f;
+      ARD_HIP_CHECK((run_mix<T, true>(d, r, dK, part, stream)));
+    }
+    if (dV || dS0) {
+      r = g;
+      r.x = K, r.y = Q, r.w = dO;
+      r.x_shared = 1;
+      r.ydim = d->key_dim, r.wdim = d->value_dim;
+      r.s0 = dST, r.sT = dS0;
+      r.cy = d->scale, r.cx = 1.0f;
+      ARD_HIP_CHECK((run_mix<T, true>(d, r, dV, part, stream)));
+    }
   }
   return ARD_OK;
 }
