@@ -179,3 +179,59 @@ def test_runs_alike():
     idx[4] = idx[2]
     a, b = (_run("bf16", Z, idx, t, labels, 2.0, 0.5, dloss) for _ in range(2))
     assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+@pytest.mark.gpu
+def test_logits_past_two_to_the_31():
+    """More than 2^31 logits: zero everywhere but in the last class, whose softmax is known."""
+    from gpu_util import device, workspace
+    dev, V, B = device(), 65600, 32776
+    assert V * B > 2 ** 31
+    Z = torch.zeros(V, B, dtype=torch.bfloat16, device=dev)
+    Z[V - 1] = 8.0
+    idx = torch.full((1, B), V - 1, dtype=torch.int32, device=dev)
+    tl, labels = torch.ones(1, B, device=dev), torch.full((B,), V - 1, dtype=torch.int32, device=dev)
+    desc = api.distill_desc(api.ARD_BF16, B, V, 1, 1.0, 0.5)
+    loss, stats, dZ = torch.empty(B, device=dev), torch.empty(5, B, device=dev), torch.empty_like(Z)
+    ws = workspace(api.ard_distill_workspace_bytes(desc))
+    api.ard_distill_fwd(desc, Z, idx, tl, labels, loss, stats, ws)
+    api.ard_distill_bwd(desc, Z, idx, tl, labels, stats, None, dZ)
+    torch.cuda.synchronize()
+    total = np.exp(8.0) + V - 1
+    want = np.log(total) - 8.0  # both terms are -log q of the last class
+    assert (loss.double() - want).abs().max() < 64 * U32 * (8 + want)
+    q = np.exp(8.0) / total
+    assert (dZ[V - 1].double() - (q - 1)).abs().max() < UBF
+    assert (dZ[V - 2].double() - 1 / total).abs().max() < UBF / total + 64 * U32 / total
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V,B", [(40, 20), (3000, 70)])
+def test_in_a_graph(V, B):
+    from gpu_util import device, workspace
+    dev = device()
+    Z, idx, t, labels, dloss = (x.contiguous().to(dev) for x in _inputs("bf16", V, B, 5, 21))
+    desc = api.distill_desc(api.ARD_BF16, B, V, 5, 2.0, 0.5)
+    ws = workspace(api.ard_distill_workspace_bytes(desc))
+    loss, stats, dZ = torch.empty(B, device=dev), torch.empty(5, B, device=dev), torch.empty_like(Z)
+
+    def step():
+        api.ard_distill_fwd(desc, Z, idx, t, labels, loss, stats, ws)
+        api.ard_distill_bwd(desc, Z, idx, t, labels, stats, dloss, dZ)
+    step()
+    torch.cuda.synchronize()
+    eager = loss.clone(), dZ.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        loss.fill_(3.0)
+        dZ.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, eager[0]) and torch.equal(dZ, eager[1])

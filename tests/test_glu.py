@@ -110,6 +110,13 @@ SIZES = [  # dtype, B, K, N, period, offset, act
     ("bf16", 100, 1023, 153, 3, 1, "gelu"), ("f32", 100, 103, 153, 3, 1, "gelu"), ("bf16", 128, 256, 512, 2, 1, "silu"),
     ("f32", 96, 256, 512, 2, 1, "silu"), ("bf16", 200, 512, 1100, 5, 4, "silu"), ("bf16", 640, 320, 2100, 1, 0, "relu"),
     ("f32", 640, 320, 1300, 1, 0, "relu"), ("bf16", 33, 40, 5, 7, 6, "silu"), ("f32", 33, 40, 9, 2, 1, "silu"),
+    # grids large enough for each tile of the one-product forward, rows on 16 bytes and off them
+    ("bf16", 1280, 72, 4096, 1, 0, "silu"), ("bf16", 256, 40, 11000, 1, 0, "gelu"), ("bf16", 128, 72, 20600, 1, 0, "silu"),
+    ("bf16", 643, 63, 4200, 2, 1, "sigmoid"), ("bf16", 1100, 33, 4999, 3, 2, "silu"), ("bf16", 65, 24, 300, 1, 0, "silu"),
+    # the few-column kernel: blocks of 16 columns, 8 or 16 units of a workgroup, inputs that end inside a step
+    ("bf16", 31, 95, 4200, 1, 0, "silu"), ("bf16", 64, 33, 9000, 2, 1, "gelu"), ("bf16", 3, 31, 4500, 1, 0, "relu"),
+    ("f32", 2, 17, 4500, 1, 0, "silu"), ("bf16", 1, 31, 17, 1, 0, "silu"), ("bf16", 64, 1, 3, 1, 0, "silu"),
+    ("bf16", 33, 2, 40, 1, 0, "silu"), ("bf16", 49, 700, 33, 2, 0, "gelu"), ("f32", 16, 15, 5, 2, 0, "gelu"),
 ]
 
 
@@ -252,3 +259,41 @@ def test_on_another_stream():
         api.ard_glu_fwd(desc, x, w, bb, None, other, ws)
     side.synchronize()
     assert torch.equal(Ht, other)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [("bf16", 4, 200, 96, 2, 1, "silu"), ("bf16", 200, 512, 1100, 2, 1, "silu"),
+                                  ("f32", 100, 96, 64, 2, 0, "gelu")])
+def test_in_a_graph(size):
+    from gpu_util import ard_dtype, device, workspace
+    dtype, B, K, N, period, offset, name = size
+    X, W, b, dH, Z, _ = _case(dtype, B, K, N, period, offset, name, seed=5)
+    dev, st = device(), synth.storage_dtype(dtype)
+    desc = api.glu_desc(ard_dtype(dtype), B, K, N, api.ard_plan_rows(N, period, offset, None), 1.5, ACTS[name])
+    ws = workspace(api.ard_glu_workspace_bytes(desc))
+    x, w, bb, dh = X.T.contiguous().to(dev), W.to(dev), b.to(dev), dH.T.contiguous().to(dev)
+    H, z = torch.empty(N, B, dtype=st, device=dev), torch.zeros(2, N, B, dtype=st, device=dev)
+    dX, dW, db = torch.empty(K, B, dtype=st, device=dev), torch.empty(2, N, K, device=dev), torch.empty(2, N, device=dev)
+
+    def step():
+        api.ard_glu_fwd(desc, x, w, bb, z, H, ws)
+        api.ard_glu_bwd(desc, x, w, z, dh, dX, dW, db, ws)
+    outs = (H, z, dX, dW, db)
+    step()
+    torch.cuda.synchronize()
+    eager = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for o in outs:
+            o.fill_(3.0)
+        z.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, o) for a, o in zip(eager, outs))

@@ -351,3 +351,64 @@ def test_prompt_then_steps_are_one_sequence():
     c.inside(got, want[0], size[0], "O")
     c.inside(S, want[1], size[1], "ST", state=True)
     c.inside(whole, want[0], size[0], "O")
+
+
+@pytest.mark.gpu
+def test_offsets_past_two_to_the_31():
+    """A sequence at the end of rows whose last head lies past 2^31 elements, against the same columns on their own."""
+    from gpu_util import device, workspace
+    dev, heads, dk, n, length = device(), 8, 128, (1 << 21) + 12, 130
+    assert heads * dk * n > 2 ** 31
+    c = Case("bf16", [length], heads, heads, dk, dk, True, seed=11)
+    small = _fwd(c) + tuple(_bwd(c))
+
+    def wide(x):
+        t = torch.empty(heads * dk, n, dtype=torch.bfloat16, device=dev)
+        t[:, n - length:] = x.to(dev)
+        return t
+    Q, K, V, dO = (wide(x) for x in (c.Q, c.K, c.V, c.dO))
+    off = torch.tensor([n - length, n], dtype=torch.int32, device=dev)
+    d = api.linattn_desc(api.ARD_BF16, 1, length, n, heads, heads, dk, dk, c.scale, off)
+    ws = workspace(api.ard_linattn_workspace_bytes(d))
+    O, ST, dS0 = torch.empty_like(Q), torch.empty(1, heads, dk, dk, device=dev), torch.empty(1, heads, dk, dk, device=dev)
+    api.ard_linattn_fwd(d, Q, K, V, _put(c.g), _put(c.S0), O, ST, ws)
+    grads = [torch.empty_like(Q) for _ in range(3)]
+    api.ard_linattn_bwd(d, Q, K, V, _put(c.g), _put(c.S0), dO, _put(c.dST), *grads, dS0, ws)
+    torch.cuda.synchronize()
+    got = [O[:, n - length:], ST] + [x[:, n - length:] for x in grads] + [dS0]
+    for a, b in zip(small, got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,lens,heads,kv", [("bf16", [700, 90], 2, 1), ("f32", [300, 1], 2, 2)])
+def test_in_a_graph(dtype, lens, heads, kv):
+    from gpu_util import device, workspace
+    dev = device()
+    c = Case(dtype, lens, heads, kv, 64, 48, True, seed=12)
+    d = c.desc()
+    put = [_put(x) for x in (c.Q, c.K, c.V, c.g, c.S0, c.dO, c.dST)]
+    ws = workspace(api.ard_linattn_workspace_bytes(d))
+    outs = [torch.empty_like(put[5]), torch.empty_like(put[4])] + [torch.empty_like(x) for x in put[:3]] + [
+        torch.empty_like(put[4])]
+
+    def step():
+        api.ard_linattn_fwd(d, *put[:5], outs[0], outs[1], ws)
+        api.ard_linattn_bwd(d, *put[:5], put[5], put[6], *outs[2:], ws)
+    step()
+    torch.cuda.synchronize()
+    eager = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for o in outs:
+            o.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, o) for a, o in zip(eager, outs))
