@@ -38,9 +38,10 @@ def _compile(src, obj, verbose):
 
 
 def build_library(verbose=False, jobs=None):
-    """Compiles every source under csrc/ and links libard.so. Always rebuilds."""
+    """Compiles every source under csrc/ and csrc/lm/ and links libard.so. Always rebuilds."""
     os.makedirs(BUILD_DIR, exist_ok=True)
-    sources = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")))
+    sources = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "lm", "*.hip")) +
+                     glob.glob(os.path.join(CSRC, "*.cpp")))
     objs = [os.path.join(BUILD_DIR, os.path.basename(s) + ".o") for s in sources]
     jobs = jobs or min(len(sources), max(1, min(8, os.cpu_count() or 1)))
     with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as ex:

@@ -23,8 +23,8 @@
 
 #include <cmath>
 
-#include "ard_gemm_fast.hpp"
-#include "ard_internal.hpp"
+#include "../ard_gemm_fast.hpp"
+#include "../ard_internal.hpp"
 
 namespace ard {
 namespace {

@@ -15,8 +15,8 @@
 #include <algorithm>
 #include <cmath>
 
-#include "ard_gemm_fast.hpp"
-#include "ard_internal.hpp"
+#include "../ard_gemm_fast.hpp"
+#include "../ard_internal.hpp"
 
 namespace ard {
 namespace {

@@ -30,8 +30,8 @@
 #include <algorithm>
 #include <cmath>
 
-#include "ard_gemm_fast.hpp"
-#include "ard_internal.hpp"
+#include "../ard_gemm_fast.hpp"
+#include "../ard_internal.hpp"
 
 namespace ard {
 namespace {
@@ -201,36 +201,36 @@ struct TileRegs {
   static constexpr int ES = sizeof(T), EPC = 16 / ES, CPR = kChunk * ES / 16, PER = D * CPR / NT, RPI = NT / CPR;
   static_assert(D * CPR % NT == 0, "whole rounds");
   u32x4 v[PER];
-  const char* p[PER];  // the thread's bytes at the sequence's first token
-  const char* last;    // where 16 bytes of the tensor may start at the latest
-  const T* base;       // row 0 at the sequence's first token
+  const char* last;  // where 16 bytes of the tensor may start at the latest
+  const T* base;     // row 0 at the sequence's first token
   const T* end;
   int64_t ld;
   int rows;
+  int tid;  // threadIdx.x, by name: a kernel may keep what follows from it out of its registers
 
   // base: row 0 at the sequence's first token; first, end: the tensor (of a tensor
   // below 16 bytes, which starts on 16, the 16 that it starts are read)
   __device__ __forceinline__ void init(const T* base_, int64_t ld_, int rows_, const T* first, const T* end_) {
-    base = base_, ld = ld_, rows = rows_, end = end_;
+    base = base_, ld = ld_, rows = rows_, end = end_, tid = threadIdx.x;
     last = reinterpret_cast<const char*>(end - first < EPC ? first : end - EPC);
-    const int r = threadIdx.x / CPR, c = threadIdx.x % CPR;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      p[i] = reinterpret_cast<const char*>(base + static_cast<int64_t>(min(r + i * RPI, rows - 1)) * ld + c * EPC);
+  }
+  __device__ __forceinline__ const char* at(int i, int t) const {  // the thread's bytes i of the chunk at t
+    const int r = tid / CPR, c = tid % CPR;
+    return reinterpret_cast<const char*>(base + t + static_cast<int64_t>(min(r + i * RPI, rows - 1)) * ld + c * EPC);
   }
   __device__ __forceinline__ void load(int t) {  // a whole chunk
 #pragma unroll
-    for (int i = 0; i < PER; ++i) v[i] = load16_any<ES>(p[i] + static_cast<int64_t>(t) * ES);
+    for (int i = 0; i < PER; ++i) v[i] = load16_any<ES>(at(i, t));
   }
   __device__ __forceinline__ void load_part(int t) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const char* q = p[i] + static_cast<int64_t>(t) * ES;
+      const char* q = at(i, t);
       v[i] = load16_any<ES>(q < last ? q : last);
     }
   }
   __device__ __forceinline__ void store(char* lds, int t, int L) {
-    const int r = threadIdx.x / CPR, c = threadIdx.x % CPR, n = L - c * EPC;
+    const int r = tid / CPR, c = tid % CPR, n = L - c * EPC;
     if (L < kChunk || rows < D) {  // uniform
       u32x4 keep;
 #pragma unroll
@@ -243,7 +243,7 @@ struct TileRegs {
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = i * NT + threadIdx.x;
+      const int at = i * NT + tid;
       *reinterpret_cast<u32x4*>(lds + tile_off<ES, kChunk>(at / CPR, at % CPR)) = v[i];
     }
     if (L < kChunk && base + t + (rows - 1) * ld + (L + EPC - 1) / EPC * EPC > end) {  // uniform
@@ -398,9 +398,9 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   yr.init(rows(g.y, g.y_shared, g.ydim), ld, g.ydim, static_cast<const T*>(g.y), end(g.y, g.y_shared, g.ydim));
   wr.init(rows(g.w, g.w_shared, g.wdim) + w0 * ld, ld, wrows, static_cast<const T*>(g.w),
           end(g.w, g.w_shared, g.wdim));
-  const int at_along = O::template base_along<kChunk>(), at_block = O::template base_block<kChunk>();
+  int at_along = O::template base_along<kChunk>(), at_block = O::template base_block<kChunk>();
   const int at_state = O::template base_block<M::WD>();
-  const auto at_cols = O::template base_across<kChunk>();
+  auto at_cols = O::template base_across<kChunk>();
   auto at_scols = O::template base_across<M::WD>();
   // the wave's 16 columns: part of the lane's address, since they differ by wave
   using OutOps = Ops<typename std::conditional<M::PART, float, T>::type>;
@@ -460,6 +460,10 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   if (nchunk > 0) fetch(0);
   for (int c = 0; c < nchunk; ++c) {
     const int t = first_of(c), L = min(kChunk, t1 - t);
+    // fp32 reads across rows have 16 addresses for each base (bf16: 4): computed in each
+    // chunk, as they do not fit the registers if they are kept from one to the next
+    if constexpr (M::OUT && M::ES == 4)
+      asm volatile("" : "+v"(at_along), "+v"(at_block), "+v"(at_cols), "+v"(at_icols), "+v"(at_scols));
     yr.store(Y, t, L);
     wr.store(W, t, L);
     if constexpr (M::OUT) {
@@ -620,6 +624,11 @@ struct Pair {
   static constexpr int YW = YD / 16, WBW = WD / 16 / (NW / YW);
   static constexpr int YT = YD * kChunk * ES, WT = WD * kChunk * ES, ST = YD * WD * ES;
   static constexpr int LDS = 2 * YT + 2 * WT + ST + (YD + WD) * kChunk * OS;
+  // Addresses and weights computed in each chunk, where they are used: kept from one chunk
+  // to the next, some 60 registers, they would push the accumulators of the larger tiles
+  // into scratch memory. 64 by 64 has room for them (backward of 8 x 2048 tokens, 16 heads:
+  // 154 us; computed in each chunk 163 us).
+  static constexpr bool LEAN = KD_ + VD_ > 128;
 };
 
 template <class P>
@@ -702,24 +711,16 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
       qr.load_part(t), kr.load_part(t), dr.load_part(t), vr.load_part(t);
     }
   };
-  // weights as in mix_kernel, running backward
-  f32x4 pw[4], wx;
-#pragma unroll
-  for (int jb = 0; jb < 4; ++jb)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int n = 16 * (jb - ib) + 4 * grp + r - (lane & 15);
-      pw[jb][r] = n >= 0 ? g.cp * a.pow(n) : 0.0f;
-    }
-  int weighed = -1;
-
   if (nchunk > 0) fetch(0);
   for (int c = 0; c < nchunk; ++c) {
     const int t = first_of(c), L = min(kChunk, t1 - t);
-    // the addresses that follow from these are computed in each chunk: kept from one to
-    // the next, some 60 of them, they would push the accumulators into scratch memory
-    asm volatile("" : "+v"(at_along), "+v"(at_block), "+v"(at_state), "+v"(at_srow), "+v"(at_cols.lo), "+v"(at_cols.hi),
-                 "+v"(at_scols.lo), "+v"(at_scols.hi));
+    int tid = threadIdx.x;
+    if constexpr (P::LEAN) {
+      asm volatile("" : "+v"(tid));
+      qr.tid = kr.tid = dr.tid = vr.tid = tid;
+      asm volatile("" : "+v"(at_along), "+v"(at_block), "+v"(at_state), "+v"(at_srow), "+v"(at_cols.lo),
+                   "+v"(at_cols.hi), "+v"(at_scols.lo), "+v"(at_scols.hi));
+    }
     qr.store(Q, t, L);
     kr.store(K, t, L);
     dr.store(D, t, L);
@@ -729,11 +730,8 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
       *O::block<P::WD>(S + yb * 16 * P::WD * P::ES, at_state, 0, 16 * i) = O::round(st[i]);
     lds_barrier();
     if (c + 1 < nchunk) fetch(c + 1);
-    if (L != weighed) {
-      weighed = L;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) wx[r] = g.cx * a.pow(max(L - 1 - (16 * ib + 4 * grp + r), 0));
-    }
+    Decay here = a;
+    if constexpr (P::LEAN) asm volatile("" : "+v"(here.l2));
     // 16 tokens of dV or dK: X and Y meet in the inner products, W follows them, OD rows out
     auto outputs = [&](auto of_v, char* X, char* Y, char* W, char* Out) {
       constexpr bool OFV = decltype(of_v)::value;
@@ -754,19 +752,31 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
         }
 #pragma unroll
         for (int jb = 0; jb < 4; ++jb) p[jb] = O::mma(O::across<kChunk>(Y, at_cols, k, 16 * jb), xf, p[jb]);
+        if constexpr (P::LEAN) __builtin_amdgcn_sched_barrier(0);  // later reads would take the sums' registers
       }
+      // weights as in mix_kernel, running backward
+      f32x4 wx;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) wx[r] = g.cx * here.pow(max(L - 1 - (16 * ib + 4 * grp + r), 0));
 #pragma unroll
       for (int b = 0; b < OB; ++b) acc[b] *= wx;
 #pragma unroll
+      for (int jb = 0; jb < 4; ++jb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int n = 16 * (jb - ib) + 4 * grp + r - (lane & 15);
+          p[jb][r] *= n >= 0 ? g.cp * here.pow(max(n, 0)) : 0.0f;
+        }
+#pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bf16x8 pf = __builtin_shufflevector(O::round(p[2 * h] * pw[2 * h]), O::round(p[2 * h + 1] * pw[2 * h + 1]),
-                                                  0, 1, 2, 3, 4, 5, 6, 7);
+        const bf16x8 pf = __builtin_shufflevector(O::round(p[2 * h]), O::round(p[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
         for (int b = 0; b < OB; ++b) {
           const bf16x4 lo = *O::block<kChunk>(W, at_block, 16 * b, 32 * h);
           const bf16x4 hi = *O::block<kChunk>(W, at_block, 16 * b, 32 * h + 16);
           acc[b] = O::mma(pf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), acc[b]);
         }
+        if constexpr (P::LEAN) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int b = 0; b < OB; ++b) *OutOps::template block<kChunk>(Out, at_out, 16 * b, 0) = OutOps::round(acc[b]);
@@ -780,8 +790,6 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
 #pragma unroll
     for (int k = 0; k < kChunk; k += 32) {
       const bf16x8 yf = O::along<kChunk>(Q + yb * 16 * kChunk * P::ES, at_along, 0, k);
-      Decay here = a;  // its weights, too, are computed in each chunk
-      asm volatile("" : "+v"(here.l2));
       float f[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(yf[e]) * (g.cy * here.pow(k + 8 * grp + e + 1));
@@ -802,7 +810,7 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
       typedef u32x4 u32x4_any __attribute__((aligned(2), may_alias));
 #pragma unroll
       for (int q = 0; q < ROWS * CPR / P::NT; ++q) {
-        const int at = q * P::NT + threadIdx.x, r = at / CPR, cc = at % CPR, n = L - cc * EPC;
+        const int at = q * P::NT + tid, r = at / CPR, cc = at % CPR, n = L - cc * EPC;
         if (r >= dim || n <= 0) continue;
         const char* from = Out + tile_off<P::OS, kChunk>(r, cc);
         OutT* o = op + r * ld + cc * EPC;

@@ -67,8 +67,12 @@ def test_refuses_bad_calls():
         refused(1, api.ard_distill_fwd, d, *args, (a, 1 << 30))
         args[i] = a + 4
         refused(1, api.ard_distill_fwd, d, *args, (a, 1 << 30))
-    refused(5, api.ard_distill_fwd, d, a, a, a, a, a, a, None)
-    refused(5, api.ard_distill_fwd, d, a, a, a, a, a, a, (a, 4))
+    refused(1, api.ard_distill_fwd, d, a, a, a, a, a, a, (a + 4, 1 << 30))
+    assert api.ard_distill_workspace_bytes(d) == 0  # few classes: one launch, no sums to keep
+    many = api.distill_desc(**{**good, "classes": 3000})
+    assert api.ard_distill_workspace_bytes(many) > 0
+    refused(5, api.ard_distill_fwd, many, a, a, a, a, a, a, None)
+    refused(5, api.ard_distill_fwd, many, a, a, a, a, a, a, (a, 4))
     refused(1, api.ard_distill_bwd, d, a, a, a, a, a, None, a)  # in place
     refused(1, api.ard_distill_bwd, d, a, a, a, a, None, None, 2 * a)
     refused(1, api.ard_distill_bwd, d, a, a, a, a, a, None, None)
