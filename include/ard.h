@@ -615,7 +615,8 @@ int ard_distill_bwd(const ard_distill_desc* desc, const void* Zt, const int32_t*
  * d_offsets[s] .. d_offsets[s + 1] - 1 (device memory; at most max_len of
  * them, none is allowed; entries are clamped to 0 .. tokens), or, with
  * d_offsets NULL, the columns s * max_len .. (s + 1) * max_len - 1. Columns of
- * no sequence are not touched.
+ * no sequence are not touched. A token that is not finite reaches only what the
+ * formulas have it in, not the tokens in front of it.
  * fwd: S0 (NULL = 0) is the state before the first token; ST (may be NULL)
  * receives the one after the last; of an empty sequence it is S0.
  * bwd: dOt and dST (NULL = 0) -> dQt, dKt, dVt (of a shared head the sum over

@@ -278,6 +278,52 @@ __device__ __forceinline__ void split(const float (&f)[8], bf16x8 (&s)[N]) {
   }
 }
 
+// Tokens behind the mask that are not finite. As an operand y they are kept from the
+// inner products by mul_masked (0 times anything is 0). As an operand w they make NaN of
+// the outputs in front of them, 0 times not finite in the matrix product: a lane that has
+// such an output computes it again from the tiles, where its row of w is finite up to it.
+extern "C" __device__ __attribute__((const)) float mul_masked(float p, float weight) __asm("llvm.amdgcn.fmul.legacy");
+
+__device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= 3.4028234663852886e38f; }
+
+template <typename T, int COLS>
+__device__ __forceinline__ float tile_at(const char* t, int row, int col) {
+  constexpr int EPC = 16 / static_cast<int>(sizeof(T));
+  return static_cast<float>(reinterpret_cast<const T*>(t + tile_off<sizeof(T), COLS>(row, col / EPC))[col % EPC]);
+}
+
+// Outputs (tokens i0 .. i0 + 3, row) of a chunk, in Out: out = p w + x R, computed in order
+// for the tokens in front of the first of w that is not finite. S[SROW ? row : k][...]. One
+// lane a token: some 10 ms for a chunk whose rows all end in NaN, and one such chunk is all
+// that a sequence has, as the state is not finite from there on.
+template <typename T, typename OutT, int XD, int SCOLS, bool SROW, bool REV>
+__device__ __forceinline__ void mend_outputs(const char* X, const char* Y, const char* W, const char* S, char* Out,
+                                             int i0, int row, int L, const Decay& a, float cp, float cx) {
+  int stop = REV ? L - 1 : 0;  // the first token that is not finite
+#pragma unroll 1
+  for (; REV ? stop >= 0 : stop < L; stop += REV ? -1 : 1)
+    if (!is_finite(tile_at<T, kChunk>(W, row, stop))) break;
+  if (REV ? stop < 0 : stop >= L) return;
+#pragma unroll 1
+  for (int i = max(i0, REV ? stop + 1 : 0); i < min(i0 + 4, REV ? L : stop); ++i) {
+    float s = 0.0f;
+#pragma unroll 1
+    for (int k = 0; k < XD; ++k)
+      s = fmaf(tile_at<T, kChunk>(X, k, i), tile_at<T, SCOLS>(S, SROW ? row : k, SROW ? k : row), s);
+    s *= cx * a.pow(REV ? L - 1 - i : i + 1);
+#pragma unroll 1
+    for (int j = REV ? i : 0; j < (REV ? L : i + 1); ++j) {
+      float p = 0.0f;
+#pragma unroll 1
+      for (int k = 0; k < XD; ++k) p = fmaf(tile_at<T, kChunk>(X, k, i), tile_at<T, kChunk>(Y, k, j), p);
+      p *= cp * a.pow(REV ? j - i : i - j);
+      s = fmaf(static_cast<float>(from_f32<T>(p)), tile_at<T, kChunk>(W, row, j), s);
+    }
+    constexpr int EPC = 16 / static_cast<int>(sizeof(OutT));
+    reinterpret_cast<OutT*>(Out + tile_off<sizeof(OutT), kChunk>(row, i / EPC))[i % EPC] = from_f32<OutT>(s);
+  }
+}
+
 template <typename T_, int YD_, int WD_, bool REV_, bool OUT_, bool PART_, int PARTS_ = 3>
 struct Mix {
   using T = T_;
@@ -403,7 +449,8 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   auto at_cols = O::template base_across<kChunk>();
   auto at_scols = O::template base_across<M::WD>();
   // the wave's 16 columns: part of the lane's address, since they differ by wave
-  using OutOps = Ops<typename std::conditional<M::PART, float, T>::type>;
+  using OutT = typename std::conditional<M::PART, float, T>::type;
+  using OutOps = Ops<OutT>;
   auto at_icols = at_cols;
   const int ic = (wv & 3) * 16 * M::ES, sc = M::HALVES > 1 ? (wv >> 2) * (M::WD / 2) * M::ES : 0;
   if constexpr (M::ES == 2) at_icols.lo ^= ic, at_icols.hi ^= ic, at_scols.lo ^= sc, at_scols.hi ^= sc;
@@ -464,6 +511,8 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
     // chunk, as they do not fit the registers if they are kept from one to the next
     if constexpr (M::OUT && M::ES == 4)
       asm volatile("" : "+v"(at_along), "+v"(at_block), "+v"(at_cols), "+v"(at_icols), "+v"(at_scols));
+    if constexpr (M::OUT && M::ES == 2 && M::YD < M::WD)  // four waves hold the state that elsewhere eight do
+      asm volatile("" : "+v"(at_along), "+v"(at_block), "+v"(at_cols.lo), "+v"(at_cols.hi));
     yr.store(Y, t, L);
     wr.store(W, t, L);
     if constexpr (M::OUT) {
@@ -477,12 +526,12 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
     if (L != weighed) weigh(weighed = L);
     // The outputs read the state in LDS, the state's update the one in registers: neither
     // waits for the other.
+    const int b0 = M::HALVES > 1 ? (wv >> 2) * M::OB : 0;
+    float bad = 0.0f;  // NaN if an output of the lane is not finite
     auto outputs = [&]() {
       // outputs of 16 tokens i: out[i][w] = sum_y x[y][i] R[y][w], weighted, plus the chunk's own.
       // A lane of p holds token i = 16 ib + lane % 16 and tokens j = 16 jb + 4 grp + r; one of acc
-      // tokens i = 16 ib + 4 grp + r and row w = 16 b + lane % 16. A token that is not finite
-      // spoils its chunk's other outputs: weights of 0 do not keep it from them.
-      const int b0 = M::HALVES > 1 ? (wv >> 2) * M::OB : 0;
+      // tokens i = 16 ib + 4 grp + r and row w = 16 b + lane % 16.
       char* Wo = W + b0 * 16 * kChunk * M::ES;
       f32x4 acc[M::OB];
 #pragma unroll
@@ -502,12 +551,17 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
       }
 #pragma unroll
       for (int b = 0; b < M::OB; ++b) acc[b] *= wx;
+      auto weighed_p = [&](int jb) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = mul_masked(p[jb][r], pw[jb][r]);
+        return v;
+      };
       if constexpr (M::ES == 2) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // 32 tokens j
           const bf16x8 pf =
-              __builtin_shufflevector(O::round(p[2 * h] * pw[2 * h]), O::round(p[2 * h + 1] * pw[2 * h + 1]), 0, 1, 2, 3,
-                                      4, 5, 6, 7);
+              __builtin_shufflevector(O::round(weighed_p(2 * h)), O::round(weighed_p(2 * h + 1)), 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
           for (int b = 0; b < M::OB; ++b) {
             const bf16x4 lo = *O::template block<kChunk>(Wo, at_block, 16 * b, 32 * h);
@@ -523,7 +577,7 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
           for (int k = 0; k < M::YD; k += O::ACROSS)
             p[jb] = O::mma(O::template across<kChunk>(Y, at_cols, k, 16 * jb),
                            O::template across<kChunk>(X, at_icols, k, 0), p[jb]);
-          p[jb] *= pw[jb];
+          p[jb] = weighed_p(jb);
 #pragma unroll
           for (int b = 0; b < M::OB; ++b) {
             const auto wf = O::template along<kChunk>(Wo, at_along, 16 * b, 16 * jb);
@@ -535,6 +589,10 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
 #pragma unroll
       for (int b = 0; b < M::OB; ++b)
         *OutOps::template block<kChunk>(Out + b0 * 16 * kChunk * M::OS, at_out, 16 * b, 0) = OutOps::round(acc[b]);
+#pragma unroll
+      for (int b = 0; b < M::OB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) bad = fmaf(acc[b][r], 0.0f, bad);
     };
     auto update = [&]() {  // the state past this chunk
       const float aL = a.pow(L);
@@ -568,10 +626,17 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
     };
     if constexpr (M::OUT) outputs();
     update();
+    if constexpr (M::OUT) {
+      if (bad != bad) {
+#pragma unroll 1
+        for (int b = b0; b < b0 + M::OB; ++b)
+          mend_outputs<T, OutT, M::YD, M::WD, false, M::REV>(X, Y, W, S, Out, 16 * ib + 4 * grp, 16 * b + (lane & 15), L,
+                                                              a, g.cp, g.cx);
+      }
+    }
     lds_barrier();  // the outputs are whole; no wave reads the tiles or the state any more
     if (M::OUT && g.out) {
       constexpr int EPC = 16 / M::OS, CPR = kChunk * M::OS / 16;
-      using OutT = typename std::conditional<M::PART, float, T>::type;
       OutT* op = static_cast<OutT*>(g.out) + (static_cast<int64_t>(head) * g.wdim + w0) * ld + sp.first + t;
       typedef u32x4 u32x4_any __attribute__((aligned(2), may_alias));
 #pragma unroll
@@ -732,6 +797,7 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
     if (c + 1 < nchunk) fetch(c + 1);
     Decay here = a;
     if constexpr (P::LEAN) asm volatile("" : "+v"(here.l2));
+    float bad = 0.0f;  // NaN if an output of the lane is not finite
     // 16 tokens of dV or dK: X and Y meet in the inner products, W follows them, OD rows out
     auto outputs = [&](auto of_v, char* X, char* Y, char* W, char* Out) {
       constexpr bool OFV = decltype(of_v)::value;
@@ -765,7 +831,7 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int n = 16 * (jb - ib) + 4 * grp + r - (lane & 15);
-          p[jb][r] *= n >= 0 ? g.cp * here.pow(max(n, 0)) : 0.0f;
+          p[jb][r] = mul_masked(p[jb][r], n >= 0 ? g.cp * here.pow(max(n, 0)) : 0.0f);
         }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -780,6 +846,10 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
       }
 #pragma unroll
       for (int b = 0; b < OB; ++b) *OutOps::template block<kChunk>(Out, at_out, 16 * b, 0) = OutOps::round(acc[b]);
+#pragma unroll
+      for (int b = 0; b < OB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) bad = fmaf(acc[b][r], 0.0f, bad);
     };
     if (wv < 4) outputs(std::true_type{}, K, Q, D, OutV);
     else outputs(std::false_type{}, V, D, Q, OutK);
@@ -800,6 +870,18 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
         const bf16x8 wf = O::along<kChunk>(D + wb * 16 * kChunk * P::ES, at_along, 16 * i, k);
 #pragma unroll
         for (int q = P::PARTS - 1; q >= 0; --q) st[i] = O::mma(wf, ys[q], st[i]);
+      }
+    }
+    if (bad != bad) {
+      const int i0 = 16 * ib + 4 * grp, row = lane & 15;
+      if (wv < 4) {
+#pragma unroll 1
+        for (int b = 0; b < P::WD; b += 16)
+          mend_outputs<T, OutT, P::YD, P::WD, false, true>(K, Q, D, S, OutV, i0, b + row, L, a, g.cp, g.cx);
+      } else {
+#pragma unroll 1
+        for (int b = 0; b < P::YD; b += 16)
+          mend_outputs<T, OutT, P::WD, P::WD, true, true>(V, D, Q, S, OutK, i0, b + row, L, a, g.cp, g.cx);
       }
     }
     lds_barrier();  // the outputs are whole; no wave reads the tiles or the state any more

@@ -381,6 +381,40 @@ def test_offsets_past_two_to_the_31():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ["Q", "K", "V", "dO"])
+@pytest.mark.parametrize("lens,heads,kv,dk,dv", [([150], 2, 1, 64, 64), ([110, 128], 1, 1, 128, 128), ([120], 2, 2, 64, 128),
+                                                 ([128], 1, 1, 128, 40), ([700], 2, 1, 40, 64)])
+def test_a_token_that_is_not_finite_spoils_nothing_that_does_not_read_it(dtype, name, lens, heads, kv, dk, dv):
+    """An infinity in one row of a token and NaN in all rows of a later one, in each sequence: what is finite by the
+    formula, token after token, is right, and nothing else is finite."""
+    c = Case(dtype, lens, heads, kv, dk, dv, True, seed=15)
+    x = getattr(c, name)
+    for b, _ in c.spans:
+        x[3, b + 37] = float("inf")
+        x[:, b + 100] = float("nan")
+
+    def right(got, want, size, what, state):
+        got = got.double().cpu().numpy()
+        on = np.isfinite(want)
+        assert (np.isfinite(got) == on).all(), f"{what}: {np.argwhere(np.isfinite(got) != on)[:5]}"
+        if not on.any():
+            return
+        got, want, size = got[on], want[on], size[on]
+        bound = 2 * (max(lens) + 200) * U32 * size + (U32 if state or dtype == "f32" else UBF) * np.abs(want) + 1e-30
+        if dtype == "bf16" and not state:
+            bound = bound + 2 * UBF * size
+        assert (np.abs(got - want) <= bound).all(), what
+    with np.errstate(invalid="ignore"):
+        forward, backward = (c.forward(), c.forward(size=True)), (c.backward(), c.backward(size=True))
+    if name != "dO":
+        for i, (g, what) in enumerate(zip(_fwd(c), ("O", "ST"))):
+            right(g, forward[0][i], forward[1][i], what, i == 1)
+    for i, (g, what) in enumerate(zip(_bwd(c), ("dQ", "dK", "dV", "dS0"))):
+        right(g, backward[0][i], backward[1][i], what, i == 3)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,lens,heads,kv", [("bf16", [700, 90], 2, 1), ("f32", [300, 1], 2, 2)])
 def test_in_a_graph(dtype, lens, heads, kv):
     from gpu_util import device, workspace
