@@ -191,7 +191,10 @@ __device__ __forceinline__ void finish_column(Run a, int64_t col, bool on, int t
   stats[4 * b + col] = es;
 }
 
-// The running sums of a range of rows; ONE: of all rows, and with them the loss.
+// The running sums of a range of rows; ONE: of all rows, and with them the loss. Bound by
+// reading the logits: 32000 x 4096 bf16 (262 MB) 75 us, 3.5 TB/s; large reductions read at
+// 4.0 to 4.5 TB/s here. Without its exponentials the kernel took 71 us; eight rows in
+// flight, more workgroups or another order of them changed nothing.
 template <typename T, int VE, bool TWO, bool ONE>
 __global__ void __launch_bounds__(256) distill_sums_kernel(const T* __restrict__ Z, int32_t V, int32_t B, Grid g,
                                                            int32_t top, const int32_t* __restrict__ idx,
@@ -280,7 +283,8 @@ __global__ void __launch_bounds__(256) distill_sums_kernel(const T* __restrict__
 }
 
 // Joins a column's ranges, then the teacher's entries and the label: 16 columns
-// of a workgroup, sixteen threads each.
+// of a workgroup, sixteen threads each. Bound by the latency of entry, then logit: 64
+// entries of 4096 columns 10 us.
 template <typename T, bool TWO>
 __global__ void __launch_bounds__(256) distill_loss_kernel(const T* __restrict__ Z, int32_t V, int32_t B, int32_t top,
                                                            const int32_t* __restrict__ idx,
@@ -385,7 +389,9 @@ __device__ __forceinline__ void sparse_entry(int64_t j, int64_t col, const Facto
   dZ[at] = from_f32<T>(g);
 }
 
-// The dense part of a range of rows; ONE: of all rows, and the entries after it.
+// The dense part of a range of rows; ONE: of all rows, and the entries after it. Bound by
+// reading the logits and writing as much: 32000 x 4096 bf16 (524 MB) 93 us, 5.6 TB/s,
+// which is what a copy reaches.
 template <typename T, int VE, bool TWO, bool ONE>
 __global__ void __launch_bounds__(256) distill_dense_kernel(const T* __restrict__ Z, int32_t V, int32_t B, Grid g,
                                                             int32_t top, const int32_t* __restrict__ idx,
@@ -439,7 +445,13 @@ __global__ void __launch_bounds__(256) distill_dense_kernel(const T* __restrict_
   }
 }
 
-template <typename T, bool TWO>
+// The entries after a dense launch: 16 columns of a workgroup, 16 threads of each, OWN
+// entries in a thread's registers. The column's entries pass through LDS, 16 OWN at a time,
+// so that each is read and raised to its power once for all that compare with it. Bound by
+// scattered reads and writes of single logits: 64 entries of 4096 columns (262144 of them)
+// of 32000 bf16 classes 18.6 us, and the whole backward of 1024 entries of 1024 columns
+// 170 us (each entry read again from memory for every other: 22.3 and 540).
+template <typename T, bool TWO, int OWN>
 __global__ void __launch_bounds__(256) distill_sparse_kernel(const T* __restrict__ Z, int32_t V, int32_t B,
                                                              int32_t top, const int32_t* __restrict__ idx,
                                                              const float* __restrict__ tl,
@@ -447,12 +459,62 @@ __global__ void __launch_bounds__(256) distill_sparse_kernel(const T* __restrict
                                                              const float* __restrict__ stats,
                                                              const float* __restrict__ dloss, float temp,
                                                              float weight, T* dZ) {
-  const int64_t col = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63), b = B;
-  const int64_t j = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 6);
-  if (col >= B || j > top) return;
+  constexpr int NX = 16, NY = 16, PASSED = NY * OWN;  // entries in LDS at a time
+  __shared__ int32_t si[PASSED][NX];
+  __shared__ float se[PASSED][NX];
+  const int tx = threadIdx.x % NX, ty = threadIdx.x / NX;
+  const int64_t b = B, at = static_cast<int64_t>(blockIdx.x) * NX + tx;
+  const bool on = at < b;
+  const int64_t col = on ? at : b - 1;  // past the last: read again, nothing written
+  const int64_t j0 = static_cast<int64_t>(blockIdx.y) * NY * OWN + ty;
+  const float inv_t = 1.0f / temp;
+  const int32_t passed = weight > 0.0f ? top : 0;
+  int32_t ci[OWN];
+  float ct[OWN];
+  auto fetch = [&](int64_t i0) {
+#pragma unroll
+    for (int u = 0; u < OWN; ++u) {
+      const int64_t i = i0 + ty + u * NY < passed ? i0 + ty + u * NY : i0;
+      ci[u] = idx[i * b + col], ct[u] = tl[i * b + col];
+    }
+  };
+  if (passed > 0) fetch(0);
+  const int32_t label = labels ? labels[col] : -1;
+  int32_t v[OWN];
+  float z[OWN], p[OWN];
+#pragma unroll
+  for (int q = 0; q < OWN; ++q) {  // entry `top` is the label
+    const int64_t j = j0 + q * NY;
+    const int32_t w = j < top ? idx[j * b + col] : j == top ? label : -1;
+    v[q] = on && w >= 0 && w < V ? w : -1;
+    p[q] = 0.0f;
+  }
+#pragma unroll
+  for (int q = 0; q < OWN; ++q) z[q] = to_f32(Z[(v[q] < 0 ? 0 : v[q]) * b + col]);
   const Factors f = factors_of(col, V, B, stats, labels, dloss, temp, weight);
-  sparse_entry<T, TWO>(j, col, f, Z, V, B, top, idx, tl, labels ? labels[col] : -1, stats[3 * b + col],
-                       stats[4 * b + col], 1.0f / temp, dZ);
+  const float tref = stats[3 * b + col], es = stats[4 * b + col];
+  for (int64_t i0 = 0; i0 < passed; i0 += PASSED) {
+    const int n = static_cast<int>(passed - i0 < PASSED ? passed - i0 : PASSED);
+    if (i0 > 0) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < OWN; ++u) si[ty + u * NY][tx] = ci[u], se[ty + u * NY][tx] = expf((ct[u] - tref) * inv_t);
+    __syncthreads();
+    if (i0 + PASSED < passed) fetch(i0 + PASSED);
+    for (int i = 0; i < n; ++i) {
+      const int32_t w = si[i][tx];
+      const float e = se[i][tx];
+#pragma unroll
+      for (int q = 0; q < OWN; ++q) p[q] = w == v[q] ? p[q] + e : p[q];
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < OWN; ++q) {
+    if (v[q] < 0) continue;
+    float g = dense_grad<T, TWO>(z[q], f.m, f.fT, f.f1, inv_t);
+    if (!(f.cs == 0.0f)) g -= f.cs * (p[q] / es);
+    if (v[q] == label) g -= f.ch;
+    dZ[v[q] * b + col] = from_f32<T>(g);
+  }
 }
 
 int need_ptr(const void* p, const char* name) {
@@ -482,7 +544,7 @@ constexpr int kBlocks = 512;  // workgroups that fill the chip: two on a compute
 
 // Few classes: one column per thread and 16 threads down its rows, the whole pass in
 // one launch. A launch costs what the reading of some hundred rows does (10 classes,
-// 128 columns, fp32, forward and backward: 18.5 us in four launches of wide rows).
+// 128 columns, fp32, forward and backward: 11.6 us, in four launches of wide rows 18.5).
 constexpr int kOneLaunch = 256;
 bool one_launch(const ard_distill_desc* d) { return d->classes <= kOneLaunch; }
 
@@ -544,9 +606,15 @@ int bwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, cons
                      dZ);
   ARD_LAUNCH_CHECK();
   if (!ONE && (d->top > 0 || labels)) {
-    hipLaunchKernelGGL((distill_sparse_kernel<T, TWO>), dim3((d->batch - 1) / 64 + 1, d->top / 4 + 1), dim3(256), 0,
-                       stream, Z, d->classes, d->batch, d->top, idx, tl, labels, stats, dloss, d->temperature,
-                       d->soft_weight, dZ);
+    // few entries: fewer for each thread (20 of 700 columns, 8800 classes: backward 22.7 us, with 8 24.5)
+    auto entries = [&](auto own) {
+      constexpr int OWN = decltype(own)::value;
+      hipLaunchKernelGGL((distill_sparse_kernel<T, TWO, OWN>), dim3((d->batch - 1) / 16 + 1, d->top / (16 * OWN) + 1),
+                         dim3(256), 0, stream, Z, d->classes, d->batch, d->top, idx, tl, labels, stats, dloss,
+                         d->temperature, d->soft_weight, dZ);
+    };
+    if (d->top < 32) entries(std::integral_constant<int, 2>{});
+    else entries(std::integral_constant<int, 8>{});
     ARD_LAUNCH_CHECK();
   }
   return ARD_OK;

@@ -293,9 +293,10 @@ __device__ __forceinline__ float tile_at(const char* t, int row, int col) {
 }
 
 // Outputs (tokens i0 .. i0 + 3, row) of a chunk, in Out: out = p w + x R, computed in order
-// for the tokens in front of the first of w that is not finite. S[SROW ? row : k][...]. One
-// lane a token: some 10 ms for a chunk whose rows all end in NaN, and one such chunk is all
-// that a sequence has, as the state is not finite from there on.
+// for the tokens in front of the first of w that is not finite. S[SROW ? row : k][...]. Slow,
+// 8 ms for a chunk of 128 rows that all end in NaN, but a sequence has one such chunk: the
+// state that the next ones read is not finite then. Finite inputs pay for the check of the
+// outputs: 128 x 128 3 to 4% (4 x 4096 tokens, 16 heads: 123 us in place of 119), 64 x 64 1%.
 template <typename T, typename OutT, int XD, int SCOLS, bool SROW, bool REV>
 __device__ __forceinline__ void mend_outputs(const char* X, const char* Y, const char* W, const char* S, char* Out,
                                              int i0, int row, int L, const Decay& a, float cp, float cx) {

@@ -138,6 +138,15 @@ def test_loss_and_gradient(dtype, V, B, top, T, a):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("top", [15, 16, 31, 32, 127, 128, 129])
+def test_entries_in_blocks_of_threads(top):
+    """Entry counts on both sides of what a workgroup holds, classes named more than once."""
+    Z, idx, t, labels, dloss = _inputs("bf16", 400, 19, top, top)
+    idx[: top // 3] = idx[top - top // 3:]
+    _check("bf16", Z, idx, t, labels, 2.0, 0.5, dloss)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [1.0, 2.0])
 def test_masked_and_empty_columns(dtype, T):
