@@ -46,10 +46,57 @@ __device__ __forceinline__ Act act_of(int act, float g) {
 
 struct GluShape {
   int32_t B, K, N, kept, period, offset;
-  int64_t ldd;   // row length of the derivatives in the workspace
+  int64_t ldd;   // row length of the derivatives in the workspace, and of X's copy
+  int64_t ldk;   // row length of the kept weights' copy
   size_t es;
   bool zero;     // dropped rows are written 0
 };
+
+// ------------------------------------------------------------------ rows off 16 bytes
+// Products of rows that do not start on 16 bytes run at a third to a half of the rate of
+// those that do (register loads in place of direct ones, smaller tiles), while a copy whose
+// rows are a multiple of 16 bytes costs its bytes once: kept weights [2][kept][ldk], X
+// [K][ldd]. bf16, every other of 8191 units kept, batch 2047: forward 945 to 311 us,
+// backward (where the derivatives' launch makes the copies) 2866 to 679; 407 x 5687 -> 517
+// forward 142 to 36.
+
+// A row of n elements to one that starts on 16 bytes, 0 in the rest of its last 16; a wave.
+template <typename T>
+__device__ __forceinline__ void copy_row(const T* __restrict__ from, T* __restrict__ to, int32_t n) {
+  constexpr int E = 16 / static_cast<int>(sizeof(T)), U = 4;
+  const int lane = threadIdx.x & 63, whole = n / E;
+  int c = lane;
+  for (; c + (U - 1) * 64 < whole; c += U * 64) {
+    u32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load16_any<sizeof(T)>(reinterpret_cast<const char*>(from + (c + u * 64) * E));
+#pragma unroll
+    for (int u = 0; u < U; ++u) reinterpret_cast<u32x4*>(to)[c + u * 64] = v[u];
+  }
+  for (; c < whole; c += 64)
+    reinterpret_cast<u32x4*>(to)[c] = load16_any<sizeof(T)>(reinterpret_cast<const char*>(from + c * E));
+  if (c == whole && n % E) {
+    T e[E];
+#pragma unroll
+    for (int q = 0; q < E; ++q) e[q] = whole * E + q < n ? from[whole * E + q] : from_f32<T>(0.0f);
+    reinterpret_cast<u32x4*>(to)[whole] = *reinterpret_cast<const u32x4*>(e);
+  }
+}
+
+// The forward's copies (Wc, Xc: NULL = not wanted), a row a wave.
+template <typename T>
+__global__ void __launch_bounds__(256) glu_copy_kernel(GluShape s, const T* __restrict__ X, const T* __restrict__ W,
+                                                       T* __restrict__ Xc, T* __restrict__ Wc) {
+  const int64_t rw = Wc ? 2 * static_cast<int64_t>(s.kept) : 0, rows = rw + (Xc ? s.K : 0);
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4ll) {
+    if (r < rw) {
+      const int64_t h = r >= s.kept, i = r - h * s.kept;
+      copy_row(W + (h * s.N + s.offset + i * s.period) * s.K, Wc + r * s.ldk, s.K);
+    } else {
+      copy_row(X + (r - rw) * s.B, Xc + (r - rw) * s.ldd, s.B);
+    }
+  }
+}
 
 // Joins the projections zf[2][kept][B] (fp32): a workgroup per hidden unit, a
 // dropped one's row cleared if asked. 2000 units of 700 columns, fp32: 10 us.
@@ -274,8 +321,10 @@ __global__ void __launch_bounds__(64 * kSmallWaves) glu_small_kernel(GluShape s,
 // 242 us, 1136 TFLOP/s; a square product of 8192 by the library runs at 1111.
 struct GluTileArgs {
   GluShape s;
-  const void* X;
-  const void* W;
+  const void* X;     // rows of ldx
+  const void* W;     // a projection's first kept row; rows of ldw, those kept w_step apart
+  int64_t ldx, ldw;
+  int32_t w_step, w_half;  // rows between kept ones, and between the projections
   const float* bias;
   void* Z;
   void* H;
@@ -285,15 +334,14 @@ struct GluTileArgs {
 
 // LDS: the stages, then the outputs of each wave on their way out (g, u, h: 32 rows
 // each, and the biases of its units).
-template <class Cfg, int LD>
+template <class Cfg>
 struct GluLds {
   static constexpr int ROW = Cfg::TN * 2 + 16, PART = 32 * ROW, PAIRS = Cfg::TM / 2;
   static constexpr int WAVE = 3 * PART + 2 * PAIRS * 4;
-  static constexpr int STAGES = LD == LOAD_ANY ? Cfg::LDS_REG : Cfg::LDS;
-  static constexpr int BYTES = Cfg::NW * WAVE > STAGES ? Cfg::NW * WAVE : STAGES;
+  static constexpr int BYTES = Cfg::NW * WAVE > Cfg::LDS ? Cfg::NW * WAVE : Cfg::LDS;
 };
 
-template <class Cfg, int LD>
+template <class Cfg>
 __global__ void __launch_bounds__(Cfg::NT) glu_tile_kernel(GluTileArgs g) {
   static_assert(Cfg::TM % 64 == 0 && Cfg::KSPLIT == 1 && Cfg::ES == 2, "whole pairs of 32 rows in a wave");
   constexpr int ES = Cfg::ES;
@@ -313,35 +361,29 @@ __global__ void __launch_bounds__(Cfg::NT) glu_tile_kernel(GluTileArgs g) {
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
   const int nslab = (s.K + Cfg::BK - 1) / Cfg::BK;
-  auto row_of = [&](int r) {  // tile row -> row of W[2 N][K]; past the last pair: the last one, discarded
-    const int p = min(p0 + (r >> 6) * 32 + (r & 31), s.kept - 1);
-    return ((r >> 5) & 1) * s.N + s.offset + p * s.period;
+  auto row_of = [&](int r) {  // tile row -> row of W; past the last pair: the last one, discarded
+    return ((r >> 5) & 1) * g.w_half + min(p0 + (r >> 6) * 32 + (r & 31), s.kept - 1) * g.w_step;
   };
-  using Loader = typename std::conditional<LD == LOAD_ANY, RegLoader<Cfg, false, true>, SlabLoader<Cfg, false, true>>::type;
-  Loader ld;
+  SlabLoader<Cfg, false, true> ld;
   ld.wv = wv;
-  ld.da.init_rows(s.K, row_of, wv);
-  ld.db.init(s.B, n0, s.B, wv);
+  ld.da.init_rows(g.ldw, row_of, wv);
+  ld.db.init(g.ldx, n0, s.B, wv);
   ld.K = s.K;
   ld.ik = 0;
   ld.a_step = static_cast<int64_t>(Cfg::BK) * ES;
-  ld.b_step = static_cast<int64_t>(s.B) * Cfg::BK * ES;
+  ld.b_step = g.ldx * Cfg::BK * ES;
   ld.a_wrap = ld.b_wrap = 0;
   ld.na = uniform_ptr(static_cast<const char*>(g.W));
   ld.nb = uniform_ptr(static_cast<const char*>(g.X));
-  if constexpr (LD == LOAD_ANY) {
-    run_slabs_reg<Cfg, false, true, false>(ld, nslab, acc, wm, wn, 0, smem, nullptr);
-  } else {
-    ld.lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-    ld.is = 0;
-    ld.left = nslab - 1;
-    run_slabs<Cfg, false, true, true, false>(ld, nslab, s.K, 0, acc, wm, wn, 0, smem);
-  }
+  ld.lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+  ld.is = 0;
+  ld.left = nslab - 1;
+  run_slabs<Cfg, false, true, true, false>(ld, nslab, s.K, 0, acc, wm, wn, 0, smem);
 
   // Each block of 32 units passes through the wave's own LDS, g, u and h side by side,
   // and is written 16 bytes of a row at a time. The units' biases come first, every
   // load in flight together.
-  using L = GluLds<Cfg, LD>;
+  using L = GluLds<Cfg>;
   constexpr int ROW = L::ROW, PART = L::PART, CPRW = Cfg::TN / 8, RPI = 64 / CPRW, PAIRS = L::PAIRS;
   lds_barrier();  // every wave is done with the stages
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
@@ -415,9 +457,11 @@ __global__ void __launch_bounds__(256) glu_clear_kernel(GluShape s, T* __restric
 // and 134 MB cleared) 35.6 us, 6.1 TB/s.
 template <typename T, typename G>
 __global__ void __launch_bounds__(256) glu_derive_kernel(GluShape s, const T* __restrict__ Z,
-                                                         const T* __restrict__ dH, int act, float scale, int vec,
+                                                         const T* __restrict__ dH, const T* __restrict__ X,
+                                                         const T* __restrict__ W, int act, float scale,
                                                          T* __restrict__ D, G* __restrict__ dW,
-                                                         float* __restrict__ dbias) {
+                                                         float* __restrict__ dbias, T* __restrict__ Xc,
+                                                         T* __restrict__ Wc) {
   const int64_t n = blockIdx.x;
   if (static_cast<int32_t>(n % s.period) != s.offset) {
     if (!s.zero) return;
@@ -449,31 +493,36 @@ __global__ void __launch_bounds__(256) glu_derive_kernel(GluShape s, const T* __
     sg += og;
     su += ou;
   };
-  if (vec) {
-    constexpr int E = 16 / static_cast<int>(sizeof(T));
-    for (int b = threadIdx.x * E; b < s.B; b += 256 * E) {
-      const u32x4 rg = *reinterpret_cast<const u32x4*>(gp + b), ru = *reinterpret_cast<const u32x4*>(up + b);
-      const u32x4 rh = *reinterpret_cast<const u32x4*>(hp + b);
-      u32x4 og, ou;
+  constexpr int E = 16 / static_cast<int>(sizeof(T));
+  for (int b = threadIdx.x * E; b < s.B; b += 256 * E) {
+    u32x4 r[3], og, ou;  // g, u and dH
+    const T* from[3] = {gp + b, up + b, hp + b};
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        float x, y;
-        one(to_f32(reinterpret_cast<const T*>(&rg)[e]), to_f32(reinterpret_cast<const T*>(&ru)[e]),
-            to_f32(reinterpret_cast<const T*>(&rh)[e]), x, y);
-        reinterpret_cast<T*>(&og)[e] = from_f32<T>(x);
-        reinterpret_cast<T*>(&ou)[e] = from_f32<T>(y);
+    for (int q = 0; q < 3; ++q) {
+      if (b + E <= s.B) {
+        r[q] = load16_any<sizeof(T)>(reinterpret_cast<const char*>(from[q]));
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) reinterpret_cast<T*>(&r[q])[e] = b + e < s.B ? from[q][e] : from_f32<T>(0.0f);
       }
-      *reinterpret_cast<u32x4*>(dg + b) = og;
-      *reinterpret_cast<u32x4*>(du + b) = ou;
     }
-  } else {
-    for (int b = threadIdx.x; b < s.B; b += 256) {
-      float x, y;
-      one(to_f32(gp[b]), to_f32(up[b]), to_f32(hp[b]), x, y);
-      dg[b] = from_f32<T>(x);
-      du[b] = from_f32<T>(y);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float x = 0.0f, y = 0.0f;
+      if (b + e < s.B)
+        one(to_f32(reinterpret_cast<const T*>(&r[0])[e]), to_f32(reinterpret_cast<const T*>(&r[1])[e]),
+            to_f32(reinterpret_cast<const T*>(&r[2])[e]), x, y);
+      reinterpret_cast<T*>(&og)[e] = from_f32<T>(x);
+      reinterpret_cast<T*>(&ou)[e] = from_f32<T>(y);
     }
+    *reinterpret_cast<u32x4*>(dg + b) = og;
+    *reinterpret_cast<u32x4*>(du + b) = ou;
   }
+  // the products' copies, a row a wave: this unit's weights, and X's rows i, i + kept, ...
+  for (int64_t r = threadIdx.x >> 6; Wc && r < 2; r += 4)
+    copy_row(W + (r * s.N + n) * s.K, Wc + (r * s.kept + i) * s.ldk, s.K);
+  for (int64_t r = i + (threadIdx.x >> 6) * static_cast<int64_t>(s.kept); Xc && r < s.K; r += 4 * static_cast<int64_t>(s.kept))
+    copy_row(X + r * s.B, Xc + r * s.ldd, s.B);
   if (!dbias) return;
   __shared__ float red[8];
 #pragma unroll
@@ -534,6 +583,7 @@ int check_desc(const ard_glu_desc* d, GluShape* s) {
   s->period = all ? 1 : d->hidden_plan->period;
   s->offset = all ? 0 : d->hidden_plan->offset;
   s->ldd = (static_cast<int64_t>(s->B) + 7) / 8 * 8;
+  s->ldk = (static_cast<int64_t>(s->K) + 7) / 8 * 8;
   s->es = d->dtype == ARD_BF16 ? 2 : 4;
   s->zero = d->dropped == ARD_DROPPED_ZERO;
   return ARD_OK;
@@ -567,8 +617,7 @@ bool small_batch(const GluShape& s) { return s.B <= (s.es == 2 ? 64 : 16) && s.k
 // 64 x 64 tiles included, and what a fused epilogue saved there (1 to 5 us) the tiles
 // with 64 rows in a wave lost several times over (700 x 1500 -> 2000 units 113 to 94 us).
 int plan_tile(const GluShape& s) {
-  if (s.es != 2 || 4 * static_cast<int64_t>(s.N) * s.K + 4096 >= int64_t{1} << 31 ||
-      514 * static_cast<int64_t>(s.B) >= int64_t{1} << 31)
+  if (s.es != 2 || 4 * s.N * s.ldk + 4096 >= int64_t{1} << 31 || 514 * s.ldd >= int64_t{1} << 31)
     return -1;
   struct Tile {
     int kind, bm, bn;
@@ -590,19 +639,38 @@ bool one_product(const GluShape& s) { return s.kept > 0 && !small_batch(s) && pl
 
 // The workspace: what the products read or write first, their partial sums behind it.
 struct Space {
-  size_t head, part;
-  size_t bytes() const { return head + part; }
+  size_t head, part, wc, xc;
+  size_t bytes() const { return head + part + wc + xc; }
+  template <typename T>
+  T* weights(char* ws) const { return wc ? reinterpret_cast<T*>(ws + head + part) : nullptr; }
+  template <typename T>
+  T* inputs(char* ws) const { return xc ? reinterpret_cast<T*>(ws + head + part + wc) : nullptr; }
 };
+size_t copy_w(const GluShape& s) {
+  return s.K * s.es % 16 ? al256(static_cast<size_t>(2) * s.kept * s.ldk * s.es) : 0;
+}
+size_t copy_x(const GluShape& s) { return s.B * s.es % 16 ? al256(static_cast<size_t>(s.K) * s.ldd * s.es) : 0; }
+// The forward's copies are a launch of their own, 2 to 4 us: for the tiles, which take no
+// other rows, and for products that gain more: bf16 100 x 1023 -> 512 kept 18.0 to 15.8 us,
+// but 70 x 301 -> 500 12.1 to 13.8; fp32 594 x 735 -> 1804 73 to 64, 474 x 719 -> 1220 47 to
+// 47, 100 x 1023 -> 512 17.8 to 19.8. The backward always copies: the derivatives' launch
+// does it beside its own work (bf16 70 x 301 -> 500 24 to 19, 1681 x 1194 -> 1330 190 to 84).
+bool fwd_copies(const GluShape& s) {
+  return one_product(s) || static_cast<double>(s.kept) * s.K * s.B >= (s.es == 2 ? 32e6 : 400e6);
+}
 template <typename T>
 Space fwd_space(const GluShape& s) {
-  if (s.kept == 0 || small_batch(s) || one_product(s)) return {0, 0};
-  return {al256(static_cast<size_t>(2) * s.kept * s.B * 4), al256(4 * partial_floats<T>(s.kept, s.B, s.K, 1, 2))};
+  if (s.kept == 0 || small_batch(s)) return {0, 0, 0, 0};
+  const bool c = fwd_copies(s);
+  const size_t w = c ? copy_w(s) : 0, x = c ? copy_x(s) : 0;
+  if (one_product(s)) return {0, 0, w, x};
+  return {al256(static_cast<size_t>(2) * s.kept * s.B * 4), al256(4 * partial_floats<T>(s.kept, s.B, s.K, 1, 2)), w, x};
 }
 template <typename T>
 Space bwd_space(const GluShape& s) {
-  if (s.kept == 0) return {0, 0};
+  if (s.kept == 0) return {0, 0, 0, 0};
   const size_t d = partial_floats<T>(s.K, s.B, s.kept, 2, 1), w = partial_floats<T>(s.kept, s.K, s.B, 1, 2);
-  return {al256(static_cast<size_t>(2) * s.kept * s.ldd * sizeof(T)), al256(4 * std::max(d, w))};
+  return {al256(static_cast<size_t>(2) * s.kept * s.ldd * sizeof(T)), al256(4 * std::max(d, w)), copy_w(s), copy_x(s)};
 }
 
 int check_ws(const Space& sp, const void* ws, size_t ws_bytes) {
@@ -613,9 +681,15 @@ int check_ws(const Space& sp, const void* ws, size_t ws_bytes) {
   return ARD_OK;
 }
 
-// The kept rows of both projections, W[2][N][K], one after the other `stride` apart.
-GemmOperand kept_weights(const GluShape& s, const void* W) {
+// The kept rows of both projections, in W[2][N][K] or in their copy.
+GemmOperand kept_weights(const GluShape& s, const void* W, const void* copy) {
   GemmOperand o = {};
+  if (copy) {
+    o.p = copy;
+    o.ld = s.ldk;
+    o.bstride = o.kbstride = s.kept * s.ldk;
+    return o;
+  }
   o.p = static_cast<const char*>(W) + static_cast<size_t>(s.offset) * s.K * s.es;
   o.ld = static_cast<int64_t>(s.K) * s.period;
   o.bstride = o.kbstride = static_cast<int64_t>(s.N) * s.K;
@@ -671,10 +745,10 @@ hipError_t launch_small_fwd(const ard_glu_desc* d, const GluShape& s, const void
   return with(integral_constant<int, 1>{});
 }
 
-template <class Cfg, int LD>
+template <class Cfg>
 hipError_t launch_tile(const GluTileArgs& g, hipStream_t stream) {
-  auto kern = glu_tile_kernel<Cfg, LD>;
-  constexpr int LDS = GluLds<Cfg, LD>::BYTES;
+  auto kern = glu_tile_kernel<Cfg>;
+  constexpr int LDS = GluLds<Cfg>::BYTES;
   static const hipError_t attr =
       hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return attr;
@@ -685,13 +759,11 @@ hipError_t launch_tile(const GluTileArgs& g, hipStream_t stream) {
 }
 hipError_t run_tile(const GluTileArgs& g, hipStream_t stream) {
   using C = FastCfgs<bf16>;
-  // rows off 16 bytes: register loads, of which a 256-wide tile has too few to spare
-  if (g.s.K % 8 || g.s.B % 8) return launch_tile<C::Big, LOAD_ANY>(g, stream);
   switch (plan_tile(g.s)) {
-    case FAST_HUGE: return launch_tile<C::Huge, LOAD_DMA>(g, stream);
-    case FAST_WIDE: return launch_tile<C::Wide, LOAD_DMA>(g, stream);
-    case FAST_TALL: return launch_tile<C::Tall, LOAD_DMA>(g, stream);
-    default: return launch_tile<C::Big, LOAD_DMA>(g, stream);
+    case FAST_HUGE: return launch_tile<C::Huge>(g, stream);
+    case FAST_WIDE: return launch_tile<C::Wide>(g, stream);
+    case FAST_TALL: return launch_tile<C::Tall>(g, stream);
+    default: return launch_tile<C::Big>(g, stream);
   }
 }
 
@@ -702,21 +774,33 @@ int fwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
     ARD_HIP_CHECK(launch_small_fwd<T>(d, s, Xt, W, bias, Zt, Ht, stream));
     return ARD_OK;
   }
+  const Space sp = fwd_space<T>(s);
+  T *wc = sp.weights<T>(ws), *xc = sp.inputs<T>(ws);
+  if (wc || xc) {
+    const int64_t rows = (wc ? 2 * static_cast<int64_t>(s.kept) : 0) + (xc ? s.K : 0);
+    hipLaunchKernelGGL(glu_copy_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>((rows + 3) / 4, 65536))),
+                       dim3(256), 0, stream, s, static_cast<const T*>(Xt), static_cast<const T*>(W), xc, wc);
+    ARD_LAUNCH_CHECK();
+  }
+  const void* x = xc ? xc : Xt;
+  const int64_t ldx = xc ? s.ldd : s.B;
   if (one_product(s)) {
-    ARD_HIP_CHECK(run_tile(GluTileArgs{s, Xt, W, bias, Zt, Ht, d->act, d->scale}, stream));
+    const T* w = wc ? wc : static_cast<const T*>(W) + static_cast<int64_t>(s.offset) * s.K;
+    ARD_HIP_CHECK(run_tile(GluTileArgs{s, x, w, ldx, wc ? s.ldk : s.K, wc ? 1 : s.period, wc ? s.kept : s.N, bias, Zt, Ht,
+                                       d->act, d->scale},
+                           stream));
     if (s.zero && s.period > 1) {
       hipLaunchKernelGGL(glu_clear_kernel<T>, dim3(s.N), dim3(256), 0, stream, s, static_cast<T*>(Ht));
       ARD_LAUNCH_CHECK();
     }
     return ARD_OK;
   }
-  const Space sp = fwd_space<T>(s);
   float* zf = reinterpret_cast<float*>(ws);
   if (s.kept > 0) {
     GemmArgs g = {};
     g.M = s.kept, g.N = s.B, g.K = s.K;
-    g.a = kept_weights(s, W);
-    g.b = plain(Xt, s.B, 0);
+    g.a = kept_weights(s, W, wc);
+    g.b = plain(x, ldx, 0);
     g.c.p = zf, g.c.ld = s.B, g.c.bstride = static_cast<int64_t>(s.kept) * s.B;
     ARD_HIP_CHECK((product<T, false, true, float>(g, 2, stream, reinterpret_cast<float*>(ws + sp.head), sp.part / 4)));
   }
@@ -732,10 +816,10 @@ int bwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
   const Space sp = bwd_space<T>(s);
   float* part = reinterpret_cast<float*>(ws + sp.head);
   const int64_t half = static_cast<int64_t>(s.kept) * s.ldd;
-  const int vec = static_cast<int64_t>(s.B) * s.es % 16 == 0;
+  T *wc = dXt ? sp.weights<T>(ws) : nullptr, *xc = dW ? sp.inputs<T>(ws) : nullptr;
   hipLaunchKernelGGL((glu_derive_kernel<T, G>), dim3(s.N), dim3(256), 0, stream, s, static_cast<const T*>(Zt),
-                     static_cast<const T*>(dHt), d->act, d->scale, vec, reinterpret_cast<T*>(ws), static_cast<G*>(dW),
-                     dbias);
+                     static_cast<const T*>(dHt), static_cast<const T*>(Xt), static_cast<const T*>(W), d->act, d->scale,
+                     reinterpret_cast<T*>(ws), static_cast<G*>(dW), dbias, xc, wc);
   ARD_LAUNCH_CHECK();
   if (s.kept == 0) {  // nothing is kept: nothing depends on the input
     if (dXt) ARD_HIP_CHECK(fill_zero(dXt, static_cast<size_t>(s.K) * s.B * s.es, stream));
@@ -743,7 +827,7 @@ int bwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
     GemmArgs g = {};
     if (dXt) {
       g.M = s.K, g.N = s.B, g.K = s.kept, g.kbatch = 2;
-      g.a = kept_weights(s, W);
+      g.a = kept_weights(s, W, wc);
       g.b = plain(ws, s.ldd, half);
       g.c.p = dXt, g.c.ld = s.B;
       ARD_HIP_CHECK((product<T, true, true, T>(g, 1, stream, part, sp.part / 4)));
@@ -752,7 +836,7 @@ int bwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
       g = {};
       g.M = s.kept, g.N = s.K, g.K = s.B;
       g.a = plain(ws, s.ldd, half);
-      g.b = plain(Xt, s.B, 0);
+      g.b = xc ? plain(xc, s.ldd, 0) : plain(Xt, s.B, 0);
       g.c.p = static_cast<G*>(dW) + static_cast<int64_t>(s.offset) * s.K;
       g.c.ld = static_cast<int64_t>(s.K) * s.period;
       g.c.bstride = static_cast<int64_t>(s.N) * s.K;

@@ -117,6 +117,10 @@ SIZES = [  # dtype, B, K, N, period, offset, act
     ("bf16", 31, 95, 4200, 1, 0, "silu"), ("bf16", 64, 33, 9000, 2, 1, "gelu"), ("bf16", 3, 31, 4500, 1, 0, "relu"),
     ("f32", 2, 17, 4500, 1, 0, "silu"), ("bf16", 1, 31, 17, 1, 0, "silu"), ("bf16", 64, 1, 3, 1, 0, "silu"),
     ("bf16", 33, 2, 40, 1, 0, "silu"), ("bf16", 49, 700, 33, 2, 0, "gelu"), ("f32", 16, 15, 5, 2, 0, "gelu"),
+    # products large enough for copies of rows off 16 bytes: of both operands, of one, more inputs than units
+    ("bf16", 100, 1023, 640, 2, 1, "silu"), ("f32", 171, 1025, 1300, 1, 0, "gelu"), ("bf16", 104, 1023, 400, 1, 0, "silu"),
+    ("bf16", 101, 1024, 400, 1, 0, "relu"), ("bf16", 77, 5003, 90, 1, 0, "silu"), ("f32", 203, 1024, 1000, 1, 0, "silu"),
+    ("f32", 204, 1030, 2003, 2, 0, "sigmoid"), ("bf16", 643, 64, 4200, 2, 1, "silu"), ("bf16", 640, 65, 4200, 2, 1, "silu"),
 ]
 
 
