@@ -547,6 +547,10 @@ constexpr int kBlocks = 512;  // workgroups that fill the chip: two on a compute
 // 128 columns, fp32, forward and backward: 11.6 us, in four launches of wide rows 18.5).
 constexpr int kOneLaunch = 256;
 bool one_launch(const ard_distill_desc* d) { return d->classes <= kOneLaunch; }
+// The backward's one launch compares every entry with every other from memory: 16 entries
+// of 238 classes 8.2 us, with a launch for the entries 11; but 32 14 to 10 and 64 36 to 12.
+constexpr int kInside = 16;
+bool one_launch_bwd(const ard_distill_desc* d) { return one_launch(d) && d->top <= kInside; }
 
 int vector_of(const ard_distill_desc* d) {
   const int ve = d->dtype == ARD_BF16 ? 8 : 4;
@@ -623,14 +627,14 @@ int bwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, cons
 // Calls f with a value of the element type, the columns per thread, whether the two
 // softmaxes differ and whether one launch does it all.
 template <class F>
-int dispatch(const ard_distill_desc* d, F f) {
+int dispatch(const ard_distill_desc* d, bool one, F f) {
   using std::integral_constant;
   const bool two = d->temperature != 1.0f;
-  auto with = [&](auto t, auto ve, auto one) {
-    return two ? f(t, ve, std::true_type{}, one) : f(t, ve, std::false_type{}, one);
+  auto with = [&](auto t, auto ve, auto single) {
+    return two ? f(t, ve, std::true_type{}, single) : f(t, ve, std::false_type{}, single);
   };
   auto typed = [&](auto t, auto wide) {
-    if (one_launch(d)) return with(t, integral_constant<int, 1>{}, std::true_type{});
+    if (one) return with(t, integral_constant<int, 1>{}, std::true_type{});
     if (vector_of(d) == 1) return with(t, integral_constant<int, 1>{}, std::false_type{});
     return with(t, wide, std::false_type{});
   };
@@ -660,7 +664,7 @@ int ard_distill_fwd(const ard_distill_desc* desc, const void* Zt, const int32_t*
   if (workspace_bytes(desc) > 0 && (!ws || ws_bytes < workspace_bytes(desc)))
     return fail(ARD_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", workspace_bytes(desc), ws ? ws_bytes : 0);
   if ((st = may_ptr(ws, "workspace"))) return st;
-  return dispatch(desc, [&](auto t, auto ve, auto two, auto one) {
+  return dispatch(desc, one_launch(desc), [&](auto t, auto ve, auto two, auto one) {
     return fwd_impl<decltype(t), decltype(ve)::value, decltype(two)::value, decltype(one)::value>(
         desc, Zt, top_idx, top_logits, labels, loss, stats, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
   });
@@ -675,7 +679,7 @@ int ard_distill_bwd(const ard_distill_desc* desc, const void* Zt, const int32_t*
       (st = may_ptr(dloss, "dloss")) || (st = check_teacher(desc, top_idx, top_logits, labels)))
     return st;
   if (dZt == Zt) return fail(ARD_ERR_INVALID_ARG, "dZt must not be Zt: the logits are read again after the first pass");
-  return dispatch(desc, [&](auto t, auto ve, auto two, auto one) {
+  return dispatch(desc, one_launch_bwd(desc), [&](auto t, auto ve, auto two, auto one) {
     return bwd_impl<decltype(t), decltype(ve)::value, decltype(two)::value, decltype(one)::value>(
         desc, Zt, top_idx, top_logits, labels, stats, dloss, dZt, static_cast<hipStream_t>(stream));
   });

@@ -138,10 +138,11 @@ def test_loss_and_gradient(dtype, V, B, top, T, a):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("top", [15, 16, 31, 32, 127, 128, 129])
-def test_entries_in_blocks_of_threads(top):
+@pytest.mark.parametrize("top", [15, 16, 17, 31, 32, 127, 128, 129])
+@pytest.mark.parametrize("V", [40, 400])
+def test_entries_in_blocks_of_threads(V, top):
     """Entry counts on both sides of what a workgroup holds, classes named more than once."""
-    Z, idx, t, labels, dloss = _inputs("bf16", 400, 19, top, top)
+    Z, idx, t, labels, dloss = _inputs("bf16", V, 19, top, top)
     idx[: top // 3] = idx[top - top // 3:]
     _check("bf16", Z, idx, t, labels, 2.0, 0.5, dloss)
 
