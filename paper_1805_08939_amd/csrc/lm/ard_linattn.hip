@@ -1106,10 +1106,27 @@ MixPlan plan_mix(const ard_linattn_desc* d, int ydim, int wdim) {
   const int64_t full = std::min<int64_t>(d->n_seqs, (d->tokens - 1) / d->max_len + 1);
   const int64_t base = full * d->q_heads * p.wtiles, fill = p.yd == 64 ? kFill4 : kFill8;
   // fp32 is bound by its products, which a second pass adds to, but not by as much as idle units
-  int64_t n = base >= (d->dtype == ARD_BF16 ? fill / 2 : fill) ? 1 : (fill + base - 1) / base;
+  const int64_t n = base >= (d->dtype == ARD_BF16 ? fill / 2 : fill) ? 1 : (fill + base - 1) / base;
   const int64_t chunks = (static_cast<int64_t>(d->max_len) + kChunk - 1) / kChunk;
-  n = std::max<int64_t>(1, std::min(n, chunks / 4));  // four chunks at least
-  const int64_t per = (chunks + n - 1) / n;
+  int64_t per = (chunks + n - 1) / n;
+  if (n > 1) {
+    // Segments, shorter than four chunks where it gains: the chunks that one workgroup goes
+    // through (one of states is a third of one of outputs) against two more launches and the
+    // states, written, read twice and scanned (of every sequence, though most be short). us:
+    // bf16, 8 x 256 tokens, 8 heads of 64: 11.6 in one segment, 17.8 in four; 1 x 256, 8 of 128:
+    // 22.7 and 17.8; 16 x 256, 4 of 128: 24.5 and 31.8. fp32, 3 x 781, 8 of 80: 87 with four
+    // chunks to a segment, 63 with three; 5 x 303, 8 of 128: 64 in one segment, 37 in five.
+    const bool wide = p.yd == 128, wider = p.wd == 128;
+    const double tc = d->dtype == ARD_F32 ? (wide ? 15.0 : 7.5) : wide && wider ? 5.5 : wide || wider ? 4.0 : 2.4;
+    const double state = 4.0 * static_cast<double>(d->n_seqs) * d->q_heads * p.wtiles * p.yd * p.wd * 4 / 5.2e6;
+    double least = chunks * tc;
+    int64_t best = chunks;
+    for (int64_t q = std::max(per, std::min<int64_t>(4, chunks - 1)); q >= per && q < chunks; --q) {
+      const double us = q * tc * 4 / 3 + 11.0 + (state + 0.25) * static_cast<double>((chunks + q - 1) / q);
+      if (us < 0.97 * least) least = us, best = q;
+    }
+    per = best;
+  }
   p.seg_len = static_cast<int>(per * kChunk);
   p.nseg = static_cast<int>((chunks + per - 1) / per);
   return p;
