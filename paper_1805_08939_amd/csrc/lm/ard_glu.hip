@@ -60,20 +60,20 @@ struct GluShape {
 // backward (where the derivatives' launch makes the copies) 2866 to 679; 407 x 5687 -> 517
 // forward 142 to 36.
 
-// A row of n elements to one that starts on 16 bytes, 0 in the rest of its last 16; a wave.
-template <typename T>
+// A row of n elements to one that starts on 16 bytes, 0 in the rest of its last 16; LANES threads.
+template <int LANES, typename T>
 __device__ __forceinline__ void copy_row(const T* __restrict__ from, T* __restrict__ to, int32_t n) {
   constexpr int E = 16 / static_cast<int>(sizeof(T)), U = 4;
-  const int lane = threadIdx.x & 63, whole = n / E;
+  const int lane = threadIdx.x & (LANES - 1), whole = n / E;
   int c = lane;
-  for (; c + (U - 1) * 64 < whole; c += U * 64) {
+  for (; c + (U - 1) * LANES < whole; c += U * LANES) {
     u32x4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load16_any<sizeof(T)>(reinterpret_cast<const char*>(from + (c + u * 64) * E));
+    for (int u = 0; u < U; ++u) v[u] = load16_any<sizeof(T)>(reinterpret_cast<const char*>(from + (c + u * LANES) * E));
 #pragma unroll
-    for (int u = 0; u < U; ++u) reinterpret_cast<u32x4*>(to)[c + u * 64] = v[u];
+    for (int u = 0; u < U; ++u) reinterpret_cast<u32x4*>(to)[c + u * LANES] = v[u];
   }
-  for (; c < whole; c += 64)
+  for (; c < whole; c += LANES)
     reinterpret_cast<u32x4*>(to)[c] = load16_any<sizeof(T)>(reinterpret_cast<const char*>(from + c * E));
   if (c == whole && n % E) {
     T e[E];
@@ -91,9 +91,9 @@ __global__ void __launch_bounds__(256) glu_copy_kernel(GluShape s, const T* __re
   for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4ll) {
     if (r < rw) {
       const int64_t h = r >= s.kept, i = r - h * s.kept;
-      copy_row(W + (h * s.N + s.offset + i * s.period) * s.K, Wc + r * s.ldk, s.K);
+      copy_row<64>(W + (h * s.N + s.offset + i * s.period) * s.K, Wc + r * s.ldk, s.K);
     } else {
-      copy_row(X + (r - rw) * s.B, Xc + (r - rw) * s.ldd, s.B);
+      copy_row<64>(X + (r - rw) * s.B, Xc + (r - rw) * s.ldd, s.B);
     }
   }
 }
@@ -518,11 +518,13 @@ __global__ void __launch_bounds__(256) glu_derive_kernel(GluShape s, const T* __
     *reinterpret_cast<u32x4*>(dg + b) = og;
     *reinterpret_cast<u32x4*>(du + b) = ou;
   }
-  // the products' copies, a row a wave: this unit's weights, and X's rows i, i + kept, ...
-  for (int64_t r = threadIdx.x >> 6; Wc && r < 2; r += 4)
-    copy_row(W + (r * s.N + n) * s.K, Wc + (r * s.kept + i) * s.ldk, s.K);
+  // the products' copies: this unit's weights, and X's rows i, i + kept, ...
+  if (Wc) {
+    const int64_t h = threadIdx.x >> 7;
+    copy_row<128>(W + (h * s.N + n) * s.K, Wc + (h * s.kept + i) * s.ldk, s.K);
+  }
   for (int64_t r = i + (threadIdx.x >> 6) * static_cast<int64_t>(s.kept); Xc && r < s.K; r += 4 * static_cast<int64_t>(s.kept))
-    copy_row(X + r * s.B, Xc + r * s.ldd, s.B);
+    copy_row<64>(X + r * s.B, Xc + r * s.ldd, s.B);
   if (!dbias) return;
   __shared__ float red[8];
 #pragma unroll
@@ -650,14 +652,16 @@ size_t copy_w(const GluShape& s) {
   return s.K * s.es % 16 ? al256(static_cast<size_t>(2) * s.kept * s.ldk * s.es) : 0;
 }
 size_t copy_x(const GluShape& s) { return s.B * s.es % 16 ? al256(static_cast<size_t>(s.K) * s.ldd * s.es) : 0; }
+double work_of(const GluShape& s) { return static_cast<double>(s.kept) * s.K * s.B; }
 // The forward's copies are a launch of their own, 2 to 4 us: for the tiles, which take no
 // other rows, and for products that gain more: bf16 100 x 1023 -> 512 kept 18.0 to 15.8 us,
 // but 70 x 301 -> 500 12.1 to 13.8; fp32 594 x 735 -> 1804 73 to 64, 474 x 719 -> 1220 47 to
-// 47, 100 x 1023 -> 512 17.8 to 19.8. The backward always copies: the derivatives' launch
-// does it beside its own work (bf16 70 x 301 -> 500 24 to 19, 1681 x 1194 -> 1330 190 to 84).
-bool fwd_copies(const GluShape& s) {
-  return one_product(s) || static_cast<double>(s.kept) * s.K * s.B >= (s.es == 2 ? 32e6 : 400e6);
-}
+// 47, 100 x 1023 -> 512 17.8 to 19.8.
+bool fwd_copies(const GluShape& s) { return one_product(s) || work_of(s) >= (s.es == 2 ? 32e6 : 400e6); }
+// The backward copies beside the derivatives: the weights always (bf16 70 x 301 -> 500 24 to
+// 19, 1681 x 1194 -> 1330 190 to 84), X for dW where its product is more than a few slabs:
+// 133 x 2729 -> 2735 83 to 74, 255 x 2000 -> 2000 48 to 42, but 100 x 1023 -> 512 kept 24 to 30.
+bool bwd_copies_x(const GluShape& s) { return work_of(s) >= 100e6; }
 template <typename T>
 Space fwd_space(const GluShape& s) {
   if (s.kept == 0 || small_batch(s)) return {0, 0, 0, 0};
@@ -670,7 +674,8 @@ template <typename T>
 Space bwd_space(const GluShape& s) {
   if (s.kept == 0) return {0, 0, 0, 0};
   const size_t d = partial_floats<T>(s.K, s.B, s.kept, 2, 1), w = partial_floats<T>(s.kept, s.K, s.B, 1, 2);
-  return {al256(static_cast<size_t>(2) * s.kept * s.ldd * sizeof(T)), al256(4 * std::max(d, w)), copy_w(s), copy_x(s)};
+  return {al256(static_cast<size_t>(2) * s.kept * s.ldd * sizeof(T)), al256(4 * std::max(d, w)), copy_w(s),
+          bwd_copies_x(s) ? copy_x(s) : 0};
 }
 
 int check_ws(const Space& sp, const void* ws, size_t ws_bytes) {

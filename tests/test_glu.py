@@ -121,6 +121,7 @@ SIZES = [  # dtype, B, K, N, period, offset, act
     ("bf16", 100, 1023, 640, 2, 1, "silu"), ("f32", 171, 1025, 1300, 1, 0, "gelu"), ("bf16", 104, 1023, 400, 1, 0, "silu"),
     ("bf16", 101, 1024, 400, 1, 0, "relu"), ("bf16", 77, 5003, 90, 1, 0, "silu"), ("f32", 203, 1024, 1000, 1, 0, "silu"),
     ("f32", 204, 1030, 2003, 2, 0, "sigmoid"), ("bf16", 643, 64, 4200, 2, 1, "silu"), ("bf16", 640, 65, 4200, 2, 1, "silu"),
+    ("bf16", 333, 700, 450, 1, 0, "gelu"), ("f32", 333, 701, 451, 1, 0, "silu"), ("bf16", 331, 3001, 101, 1, 0, "silu"),
 ]
 
 
