@@ -280,48 +280,111 @@ __device__ __forceinline__ void split(const float (&f)[8], bf16x8 (&s)[N]) {
 
 // Tokens behind the mask that are not finite. As an operand y they are kept from the
 // inner products by mul_masked (0 times anything is 0). As an operand w they make NaN of
-// the outputs in front of them, 0 times not finite in the matrix product: a lane that has
-// such an output computes it again from the tiles, where its row of w is finite up to it.
+// the outputs in front of them, 0 times not finite in the matrix product: a wave that has
+// an output that is not finite computes its outputs again (mend_outputs).
 extern "C" __device__ __attribute__((const)) float mul_masked(float p, float weight) __asm("llvm.amdgcn.fmul.legacy");
 
-__device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= 3.4028234663852886e38f; }
-
-template <typename T, int COLS>
-__device__ __forceinline__ float tile_at(const char* t, int row, int col) {
-  constexpr int EPC = 16 / static_cast<int>(sizeof(T));
-  return static_cast<float>(reinterpret_cast<const T*>(t + tile_off<sizeof(T), COLS>(row, col / EPC))[col % EPC]);
+// Four values that w holds of a row: 0 in place of those that are not finite, and 1 for
+// each of those.
+template <typename V>
+__device__ __forceinline__ void sort_out(V& w, V& bad) {
+  constexpr int N = sizeof(V) / sizeof(w[0]);
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float f = static_cast<float>(w[e]);
+    const bool fin = fabsf(f) <= 3.4028234663852886e38f;
+    w[e] = fin ? w[e] : static_cast<decltype(f)>(0.0f);
+    bad[e] = fin ? static_cast<decltype(f)>(0.0f) : static_cast<decltype(f)>(1.0f);
+  }
 }
 
-// Outputs (tokens i0 .. i0 + 3, row) of a chunk, in Out: out = p w + x R, computed in order
-// for the tokens in front of the first of w that is not finite. S[SROW ? row : k][...]. Slow,
-// 8 ms for a chunk of 128 rows that all end in NaN, but a sequence has one such chunk: the
-// state that the next ones read is not finite then. Finite inputs pay for the check of the
-// outputs: 128 x 128 3 to 4% (4 x 4096 tokens, 16 heads: 123 us in place of 119), 64 x 64 1%.
+// The outputs of 16 tokens again (whole waves), from the tiles in LDS and in the order of
+// the first computation, with 0 in place of the values of w that are not finite. A second
+// product of the mask and the places of those values tells which outputs the formula has
+// one of them in; the others are written over what Out holds. Blocks b0 .. b0 + blocks - 1
+// of 16 rows; SROW: the state is read along its rows, S[row][k], else across, S[k][row].
+// A chunk that needs it costs a second computation of its outputs, whatever the values: 4 x
+// 4096 tokens, 16 heads of 128, bf16: 128 us forward and 300 backward, with a token that is
+// not finite in every chunk 190 and 470; fp32 472 and 1470, then 940 and 2890. Finite inputs
+// pay for the check of the outputs, 128 x 128 3 to 4%, 64 x 64 1%.
 template <typename T, typename OutT, int XD, int SCOLS, bool SROW, bool REV>
-__device__ __forceinline__ void mend_outputs(const char* X, const char* Y, const char* W, const char* S, char* Out,
-                                             int i0, int row, int L, const Decay& a, float cp, float cx) {
-  int stop = REV ? L - 1 : 0;  // the first token that is not finite
+__device__ __forceinline__ void mend_outputs(const char* X, const char* Y, char* W, const char* S, char* Out, int ib,
+                                             int b0, int blocks, int L, const Decay& a, float cp, float cx) {
+  using O = Ops<T>;
+  using OutOps = Ops<OutT>;
+  // nothing of this is computed ahead of the chunks and kept in registers for them
+  int lane = threadIdx.x & 63, at_block = O::template base_block<kChunk>();
+  auto at_cols = O::template base_across<kChunk>();
+  asm volatile("" : "+v"(lane), "+v"(at_block));
+  if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(at_cols.lo), "+v"(at_cols.hi));
+  else asm volatile("" : "+v"(at_cols));
+  const int grp = lane >> 4;
+  f32x4 p[4], in[4];  // weighted inner products, and the mask
+#pragma unroll
+  for (int jb = 0; jb < 4; ++jb) p[jb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
-  for (; REV ? stop >= 0 : stop < L; stop += REV ? -1 : 1)
-    if (!is_finite(tile_at<T, kChunk>(W, row, stop))) break;
-  if (REV ? stop < 0 : stop >= L) return;
-#pragma unroll 1
-  for (int i = max(i0, REV ? stop + 1 : 0); i < min(i0 + 4, REV ? L : stop); ++i) {
-    float s = 0.0f;
-#pragma unroll 1
-    for (int k = 0; k < XD; ++k)
-      s = fmaf(tile_at<T, kChunk>(X, k, i), tile_at<T, SCOLS>(S, SROW ? row : k, SROW ? k : row), s);
-    s *= cx * a.pow(REV ? L - 1 - i : i + 1);
-#pragma unroll 1
-    for (int j = REV ? i : 0; j < (REV ? L : i + 1); ++j) {
-      float p = 0.0f;
-#pragma unroll 1
-      for (int k = 0; k < XD; ++k) p = fmaf(tile_at<T, kChunk>(X, k, i), tile_at<T, kChunk>(Y, k, j), p);
-      p *= cp * a.pow(REV ? j - i : i - j);
-      s = fmaf(static_cast<float>(from_f32<T>(p)), tile_at<T, kChunk>(W, row, j), s);
+  for (int k = 0; k < XD; k += O::ACROSS) {
+    const auto xf = O::template across<kChunk>(X, at_cols, k, 16 * ib);
+#pragma unroll
+    for (int jb = 0; jb < 4; ++jb) p[jb] = O::mma(O::template across<kChunk>(Y, at_cols, k, 16 * jb), xf, p[jb]);
+  }
+#pragma unroll
+  for (int jb = 0; jb < 4; ++jb)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int n = (REV ? -1 : 1) * (16 * (ib - jb) + (lane & 15) - 4 * grp - r);
+      p[jb][r] = mul_masked(p[jb][r], n >= 0 ? cp * a.pow(max(n, 0)) : 0.0f);
+      in[jb][r] = n >= 0 ? 1.0f : 0.0f;
     }
-    constexpr int EPC = 16 / static_cast<int>(sizeof(OutT));
-    reinterpret_cast<OutT*>(Out + tile_off<sizeof(OutT), kChunk>(row, i / EPC))[i % EPC] = from_f32<OutT>(s);
+#pragma unroll 1
+  for (int b = b0; b < b0 + blocks; ++b) {
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f}, q = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int k = 0; k < XD; k += O::ACROSS) {
+      auto xf = O::template across<kChunk>(X, at_cols, k, 16 * ib);
+      if constexpr (SROW) {  // its rows in order (bf16)
+        xf = __builtin_shufflevector(xf, xf, 0, 1, 4, 5, 2, 3, 6, 7);
+        acc = O::mma(xf, O::template along<SCOLS>(S, O::template base_along<SCOLS>(), 16 * b, k), acc);
+      } else {
+        acc = O::mma(xf, O::template across<SCOLS>(S, O::template base_across<SCOLS>(), k, 16 * b), acc);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = 16 * ib + 4 * grp + r;
+      acc[r] *= cx * a.pow(max(REV ? L - 1 - i : i + 1, 0));
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        bf16x4 lo = *O::template block<kChunk>(W, at_block, 16 * b, 32 * h), lob;
+        bf16x4 hi = *O::template block<kChunk>(W, at_block, 16 * b, 32 * h + 16), hib;
+        sort_out(lo, lob);
+        sort_out(hi, hib);
+        acc = O::mma(__builtin_shufflevector(O::round(p[2 * h]), O::round(p[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7),
+                     __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), acc);
+        q = O::mma(__builtin_shufflevector(O::round(in[2 * h]), O::round(in[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7),
+                   __builtin_shufflevector(lob, hib, 0, 1, 2, 3, 4, 5, 6, 7), q);
+      }
+    } else {
+#pragma unroll
+      for (int jb = 0; jb < 4; ++jb) {
+        if ((REV ? jb < ib : jb > ib) || 16 * jb >= L) continue;
+        f32x4 w = O::template along<kChunk>(W, at_block, 16 * b, 16 * jb), bad;
+        sort_out(w, bad);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          acc = O::mma(p[jb][r], w[r], acc);
+          q = O::mma(in[jb][r], bad[r], q);
+        }
+      }
+    }
+    auto* to = OutOps::template block<kChunk>(Out, OutOps::template base_block<kChunk>(), 16 * b, 16 * ib);
+    auto v = *to;
+    const auto clean = OutOps::round(acc);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = q[r] == 0.0f ? clean[r] : v[r];
+    *to = v;
   }
 }
 
@@ -642,12 +705,8 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
     }
     update();
     if constexpr (M::OUT) {
-      if (bad != bad) {
-#pragma unroll 1
-        for (int b = b0; b < b0 + M::OB; ++b)
-          mend_outputs<T, OutT, M::YD, M::WD, false, M::REV>(X, Y, W, S, Out, 16 * ib + 4 * grp, 16 * b + (lane & 15), L,
-                                                              a, g.cp, g.cx);
-      }
+      if (__any(bad != bad))  // whole waves
+        mend_outputs<T, OutT, M::YD, M::WD, false, M::REV>(X, Y, W, S, Out, ib, b0, M::OB, L, a, g.cp, g.cx);
     }
     lds_barrier();  // the outputs are whole; no wave reads the tiles or the state any more
     if (M::OUT && g.out) {
@@ -888,17 +947,9 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
         for (int q = P::PARTS - 1; q >= 0; --q) st[i] = O::mma(wf, ys[q], st[i]);
       }
     }
-    if (bad != bad) {
-      const int i0 = 16 * ib + 4 * grp, row = lane & 15;
-      if (wv < 4) {
-#pragma unroll 1
-        for (int b = 0; b < P::WD; b += 16)
-          mend_outputs<T, OutT, P::YD, P::WD, false, true>(K, Q, D, S, OutV, i0, b + row, L, a, g.cp, g.cx);
-      } else {
-#pragma unroll 1
-        for (int b = 0; b < P::YD; b += 16)
-          mend_outputs<T, OutT, P::WD, P::WD, true, true>(V, D, Q, S, OutK, i0, b + row, L, a, g.cp, g.cx);
-      }
+    if (__any(bad != bad)) {  // whole waves
+      if (wv < 4) mend_outputs<T, OutT, P::YD, P::WD, false, true>(K, Q, D, S, OutV, ib, 0, P::WD / 16, L, a, g.cp, g.cx);
+      else mend_outputs<T, OutT, P::WD, P::WD, true, true>(V, D, Q, S, OutK, ib, 0, P::YD / 16, L, a, g.cp, g.cx);
     }
     lds_barrier();  // the outputs are whole; no wave reads the tiles or the state any more
     auto put = [&](char* Out, void* to, int dim, auto rows_c) {

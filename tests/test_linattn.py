@@ -446,3 +446,64 @@ def test_in_a_graph(dtype, lens, heads, kv):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, o) for a, o in zip(eager, outs))
+
+
+def _right(c, got, want, size, what, state):
+    """What is finite by the formula is right, and nothing else is finite."""
+    got = got.double().cpu().numpy()
+    on = np.isfinite(want)
+    assert (np.isfinite(got) == on).all(), f"{what}: {np.argwhere(np.isfinite(got) != on)[:5]}"
+    got, want, size = got[on], want[on], size[on]
+    bound = 2 * (max(c.lens) + 200) * U32 * size + (U32 if state or c.dtype == "f32" else UBF) * np.abs(want) + 1e-30
+    if c.dtype == "bf16" and not state:
+        bound = bound + 2 * UBF * size
+    assert (np.abs(got - want) <= bound).all(), what
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ["Q", "K", "V", "dO"])
+def test_tokens_that_are_not_finite_in_every_chunk(dtype, name):
+    """One row after the other is spoilt, late in every chunk: right where the formula is finite, and at most ten times
+    as long as with finite tokens (a second computation of a chunk's outputs is less than once more; values computed one
+    by one were a hundred times)."""
+    from gpu_util import device, workspace
+    c = Case(dtype, [1000], 2, 1, 128, 128, True, seed=16)
+    d = c.desc()
+    ws = workspace(api.ard_linattn_workspace_bytes(d))
+
+    def calls():
+        put = [_put(x) for x in (c.Q, c.K, c.V, c.g, c.S0, c.dO, c.dST)]
+        O, ST = torch.empty_like(put[5]), torch.empty_like(put[4])
+        grads = [torch.empty_like(x) for x in put[:3]] + [torch.empty_like(put[4])]
+
+        def fwd():
+            api.ard_linattn_fwd(d, *put[:5], O, ST, ws)
+
+        def bwd():
+            api.ard_linattn_bwd(d, *put[:5], *put[5:], *grads, ws)
+        return fwd, bwd
+
+    def shortest(call):
+        times = []
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            call()
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    clean = [shortest(call) for call in calls()]
+    x = getattr(c, name)
+    for i in range(0, 15):
+        x[7 * i, 64 * i + 62] = float("nan") if i % 2 else float("inf")
+    spoilt = [shortest(call) for call in calls()]
+    with np.errstate(invalid="ignore"):
+        forward, backward = (c.forward(), c.forward(size=True)), (c.backward(), c.backward(size=True))
+    for i, (g, what) in enumerate(zip(_fwd(c), ("O", "ST"))):
+        _right(c, g, forward[0][i], forward[1][i], what, i == 1)
+    for i, (g, what) in enumerate(zip(_bwd(c), ("dQ", "dK", "dV", "dS0"))):
+        _right(c, g, backward[0][i], backward[1][i], what, i == 3)
+    for a, b in zip(clean, spoilt):
+        assert b < 10 * a, (clean, spoilt)
