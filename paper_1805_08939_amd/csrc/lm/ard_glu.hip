@@ -44,6 +44,12 @@ __device__ __forceinline__ Act act_of(int act, float g) {
   return {g * s, s * (1.0f + g * (1.0f - s))};
 }
 
+// Launches of a workgroup for each hidden unit (or block of units): in rows of 2^20
+// workgroups, since the threads along x have to stay below 2^32.
+constexpr int32_t kGridRow = 1 << 20;
+dim3 unit_grid(int32_t groups) { return dim3(std::min(groups, kGridRow), (groups - 1) / kGridRow + 1); }
+__device__ __forceinline__ int32_t unit_group() { return static_cast<int32_t>(blockIdx.y * gridDim.x + blockIdx.x); }
+
 struct GluShape {
   int32_t B, K, N, kept, period, offset;
   int64_t ldd;   // row length of the derivatives in the workspace, and of X's copy
@@ -104,7 +110,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) glu_join_kernel(GluShape s, const float* __restrict__ zf,
                                                        const float* __restrict__ bias, int act, float scale,
                                                        T* __restrict__ Z, T* __restrict__ H) {
-  const int64_t n = blockIdx.x;
+  const int64_t n = unit_group();
+  if (n >= s.N) return;
   T* h = H + n * s.B;
   if (static_cast<int32_t>(n % s.period) != s.offset) {
     if (s.zero)
@@ -160,7 +167,8 @@ __global__ void __launch_bounds__(64 * kSmallWaves) glu_small_kernel(GluShape s,
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row = lane & 15, grp = lane >> 4;
-  const int i0 = xcd_position(blockIdx.x, gridDim.x) * PAIRS;
+  const int i0 = xcd_position(unit_group(), static_cast<int>(gridDim.x * gridDim.y)) * PAIRS;
+  if (i0 >= s.kept) return;
   const int64_t K = s.K, B = s.B;
 
   // the lane's weight rows: gate and other projection, or (8 units) one of them
@@ -439,8 +447,8 @@ __global__ void __launch_bounds__(Cfg::NT) glu_tile_kernel(GluTileArgs g) {
 // Clears the dropped rows of H.
 template <typename T>
 __global__ void __launch_bounds__(256) glu_clear_kernel(GluShape s, T* __restrict__ H) {
-  const int64_t n = blockIdx.x;
-  if (static_cast<int32_t>(n % s.period) == s.offset) return;
+  const int64_t n = unit_group();
+  if (n >= s.N || static_cast<int32_t>(n % s.period) == s.offset) return;
   T* h = H + n * s.B;
   constexpr int E = 16 / static_cast<int>(sizeof(T));
   if (s.B % E == 0) {
@@ -462,7 +470,8 @@ __global__ void __launch_bounds__(256) glu_derive_kernel(GluShape s, const T* __
                                                          T* __restrict__ D, G* __restrict__ dW,
                                                          float* __restrict__ dbias, T* __restrict__ Xc,
                                                          T* __restrict__ Wc) {
-  const int64_t n = blockIdx.x;
+  const int64_t n = unit_group();
+  if (n >= s.N) return;
   if (static_cast<int32_t>(n % s.period) != s.offset) {
     if (!s.zero) return;
     if (dW) {
@@ -619,7 +628,7 @@ bool small_batch(const GluShape& s) { return s.B <= (s.es == 2 ? 64 : 16) && s.k
 // 64 x 64 tiles included, and what a fused epilogue saved there (1 to 5 us) the tiles
 // with 64 rows in a wave lost several times over (700 x 1500 -> 2000 units 113 to 94 us).
 int plan_tile(const GluShape& s) {
-  if (s.es != 2 || 4 * s.N * s.ldk + 4096 >= int64_t{1} << 31 || 514 * s.ldd >= int64_t{1} << 31)
+  if (s.es != 2 || int64_t{4} * s.N * s.ldk + 4096 >= int64_t{1} << 31 || 514 * s.ldd >= int64_t{1} << 31)
     return -1;
   struct Tile {
     int kind, bm, bn;
@@ -727,7 +736,7 @@ hipError_t launch_small_pairs(const ard_glu_desc* d, const GluShape& s, const vo
   static const hipError_t attr =
       hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL(kern, dim3((s.kept + PAIRS - 1) / PAIRS), dim3(64 * kSmallWaves), C::LDS, stream, s,
+  hipLaunchKernelGGL(kern, unit_grid((s.kept + PAIRS - 1) / PAIRS), dim3(64 * kSmallWaves), C::LDS, stream, s,
                      static_cast<const T*>(X), static_cast<const T*>(W), bias, d->act, d->scale, static_cast<T*>(Z),
                      static_cast<T*>(H));
   return hipGetLastError();
@@ -795,7 +804,7 @@ int fwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
                                        d->act, d->scale},
                            stream));
     if (s.zero && s.period > 1) {
-      hipLaunchKernelGGL(glu_clear_kernel<T>, dim3(s.N), dim3(256), 0, stream, s, static_cast<T*>(Ht));
+      hipLaunchKernelGGL(glu_clear_kernel<T>, unit_grid(s.N), dim3(256), 0, stream, s, static_cast<T*>(Ht));
       ARD_LAUNCH_CHECK();
     }
     return ARD_OK;
@@ -809,7 +818,7 @@ int fwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
     g.c.p = zf, g.c.ld = s.B, g.c.bstride = static_cast<int64_t>(s.kept) * s.B;
     ARD_HIP_CHECK((product<T, false, true, float>(g, 2, stream, reinterpret_cast<float*>(ws + sp.head), sp.part / 4)));
   }
-  hipLaunchKernelGGL(glu_join_kernel<T>, dim3(s.N), dim3(256), 0, stream, s, zf, bias, d->act, d->scale,
+  hipLaunchKernelGGL(glu_join_kernel<T>, unit_grid(s.N), dim3(256), 0, stream, s, zf, bias, d->act, d->scale,
                      static_cast<T*>(Zt), static_cast<T*>(Ht));
   ARD_LAUNCH_CHECK();
   return ARD_OK;
@@ -822,7 +831,7 @@ int bwd_impl(const ard_glu_desc* d, const GluShape& s, const void* Xt, const voi
   float* part = reinterpret_cast<float*>(ws + sp.head);
   const int64_t half = static_cast<int64_t>(s.kept) * s.ldd;
   T *wc = dXt ? sp.weights<T>(ws) : nullptr, *xc = dW ? sp.inputs<T>(ws) : nullptr;
-  hipLaunchKernelGGL((glu_derive_kernel<T, G>), dim3(s.N), dim3(256), 0, stream, s, static_cast<const T*>(Zt),
+  hipLaunchKernelGGL((glu_derive_kernel<T, G>), unit_grid(s.N), dim3(256), 0, stream, s, static_cast<const T*>(Zt),
                      static_cast<const T*>(dHt), static_cast<const T*>(Xt), static_cast<const T*>(W), d->act, d->scale,
                      reinterpret_cast<T*>(ws), static_cast<G*>(dW), dbias, xc, wc);
   ARD_LAUNCH_CHECK();

@@ -302,3 +302,116 @@ def test_in_a_graph(size):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, o) for a, o in zip(eager, outs))
+
+
+# ---------------------------------------------------------------- past the sizes of 32-bit offsets and launches
+
+def test_the_plan_counts_weights_in_64_bits():
+    """From 2^29 units on 4 N passes 32 bits: the tiles, whose offsets have 32 bits, must not be planned. What is asked
+    for then are the sums of the batched products."""
+    B = 100
+    for N in (1 << 29, (1 << 30) - 1):
+        desc = api.glu_desc(api.ARD_BF16, B, 8, N)
+        assert api.ard_glu_workspace_bytes(desc) >= 2 * N * B * 4
+
+
+def _torch_sums(x, w, rows, b=None):
+    """Exact pre-activations of some units, and the sums of the terms' absolute values, in 64 bits on the device."""
+    z = torch.stack([w[i, rows].double() @ x.double() for i in (0, 1)])
+    size = torch.stack([w[i, rows].double().abs() @ x.double().abs() for i in (0, 1)])
+    if b is not None:
+        z, size = z + b[:, rows].double()[..., None], size + b[:, rows].double().abs()[..., None]
+    return z.cpu().numpy(), size.cpu().numpy()
+
+
+def _check_units(dtype, K, H, Z, z, size, scale, name, rows):
+    out, sums = (UBF if dtype == "bf16" else U32), (K + 16) * U32 * size
+    a = oglu.act(name, z[0])[0]
+    bound = scale * ((1.2 * sums[0] + 16 * U32 * np.abs(a)) * (np.abs(z[1]) + sums[1]) + np.abs(a) * sums[1])
+    want = scale * a * z[1]
+    _inside(H[rows], want, bound * (1 + out) + out * np.abs(want) + 1e-30, "H")
+    for i in (0, 1):
+        _inside(Z[i, rows], z[i], sums[i] * (1 + out) + out * np.abs(z[i]) + 1e-30, "Z")
+
+
+def _check_derivatives(dtype, K, grads, x, w, z, dh, kept, rows, columns, scale, name):
+    """dW and dbias of some units and dX of some columns, in 64 bits on the device."""
+    dX, dW, db = grads
+    out = UBF if dtype == "bf16" else U32
+
+    def derivatives(zz, dhh):
+        zz, dhh = zz.double().cpu().numpy(), dhh.double().cpu().numpy()
+        a, d, dabs = oglu.act(name, zz[0])
+        m = scale * np.abs(dhh)
+        size = np.stack([m * np.abs(zz[1]) * (dabs + np.abs(d) + 1e-6), m * (np.abs(a) + 1e-6)])
+        both = np.stack([scale * dhh * zz[1] * d, scale * dhh * a])
+        err = 16 * U32 * size
+        return both, err, err + (UBF * (np.abs(both) + err) if dtype == "bf16" else 0)
+    n, B = len(kept), x.shape[1]
+    both, err, rounded = derivatives(z[:, rows], dh[rows])
+    xs = x.double().cpu().numpy()
+    for i in (0, 1):
+        want, size = both[i] @ xs.T, (np.abs(both[i]) + rounded[i]) @ np.abs(xs).T
+        bound = rounded[i] @ np.abs(xs).T + (B + 16) * U32 * size
+        _inside(dW[i, rows], want, bound + U32 * np.abs(want) + 1e-30, "dW")
+        _inside(db[i, rows], both[i].sum(1), err[i].sum(1) + (B + 16) * U32 * np.abs(both[i]).sum(1) + 1e-30, "dbias")
+    both, _, rounded = derivatives(z[:, kept][:, :, columns], dh[kept][:, columns])
+    ws = w[:, kept].double().cpu().numpy()
+    want = sum(ws[i].T @ both[i] for i in (0, 1))
+    size = sum(np.abs(ws[i]).T @ (np.abs(both[i]) + rounded[i]) for i in (0, 1))
+    bound = sum(np.abs(ws[i]).T @ rounded[i] for i in (0, 1)) + (2 * n + 16) * U32 * size
+    _inside(dX[:, columns], want, bound * (1 + out) + out * np.abs(want) + 1e-30, "dX")
+
+
+def _large(dtype, B, K, N, period, offset, name, scale, backward=True):
+    """Forward and backward of a layer whose tensors are made on the device; a few units and columns checked."""
+    from gpu_util import ard_dtype, device, workspace
+    dev, st = device(), synth.storage_dtype(dtype)
+    gen = torch.Generator(device=dev).manual_seed(1805)
+    r = lambda *s, std=1.0: torch.randn(*s, generator=gen, device=dev, dtype=st) * std  # noqa: E731
+    x, w, b = r(K, B), r(2, N, K, std=K ** -0.5), torch.randn(2, N, generator=gen, device=dev)
+    desc = api.glu_desc(ard_dtype(dtype), B, K, N, api.ard_plan_rows(N, period, offset, None), scale, ACTS[name])
+    ws = workspace(api.ard_glu_workspace_bytes(desc))
+    H, Z = torch.full((N, B), 7.0, dtype=st, device=dev), torch.full((2, N, B), 7.0, dtype=st, device=dev)
+    api.ard_glu_fwd(desc, x, w, b, Z, H, ws)
+    torch.cuda.synchronize()
+    kept = torch.arange(offset, N, period, device=dev)
+    rows = kept[[0, 1, len(kept) // 2, len(kept) - 2, len(kept) - 1]]
+    _check_units(dtype, K, H, Z, *_torch_sums(x, w, rows, b), scale, name, rows)
+    dropped = torch.arange(N, device=dev) % period != offset
+    count = lambda t, value: int(sum((c == value).all(-1).sum() for c in t.split(1 << 20)))  # noqa: E731
+    assert count(H[dropped] if N < 1 << 22 else H, 0.0) == int(dropped.sum())
+    if not backward:
+        return
+    del H
+    dh = r(N, B)
+    dX, dW, db = torch.full_like(x, 7.0), torch.full((2, N, K), 7.0, device=dev), torch.full((2, N), 7.0, device=dev)
+    api.ard_glu_bwd(desc, x, w, Z, dh, dX, dW, db, ws)
+    torch.cuda.synchronize()
+    columns = torch.tensor([0, 1, B // 2, B - 1], device=dev).unique()
+    _check_derivatives(dtype, K, (dX, dW, db), x, w, Z, dh, kept, rows, columns, scale, name)
+    for t in (dW[0], dW[1], db[0][:, None], db[1][:, None]):
+        assert count(t, 0.0) == int(dropped.sum())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,B", [("f32", 17), ("bf16", 66), ("bf16", 3)])
+def test_more_units_than_a_row_of_workgroups(dtype, B):
+    """2^24 units and a few, one of 1024 kept: a launch with 256 threads for each would pass 2^32."""
+    _large(dtype, B, 4, (1 << 24) + 3, 1024, 2, "silu", 1.5)
+
+
+@pytest.mark.gpu
+def test_weights_past_the_load_offsets():
+    """A projection of more than 2^31 bytes: no tiles, and a forward product of the general kernel."""
+    N, K = 70000, 16384
+    assert 2 * N * K > 2 ** 31
+    _large("bf16", 72, K, N, 1, 0, "gelu", 0.5, backward=False)
+
+
+@pytest.mark.gpu
+def test_columns_past_the_load_offsets():
+    """Derivatives of more than 2^31 bytes, along which dW is summed, by the general kernel."""
+    N, B = 8300, 1 << 18
+    assert N // 2 * B * 2 > 2 ** 31
+    _large("bf16", B, 8, N, 2, 1, "silu", 2.0)
