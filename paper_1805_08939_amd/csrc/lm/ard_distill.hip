@@ -70,6 +70,14 @@ __device__ __forceinline__ void store_cols(T* p, const float (&v)[VE]) {
   }
 }
 
+// Launches of a workgroup for each group of columns, y such rows of workgroups: the groups
+// in layers of 2^20 along z, since the threads along x have to stay below 2^32.
+constexpr int32_t kGridRow = 1 << 20;
+dim3 column_grid(int32_t groups, int32_t y) {
+  return dim3(groups < kGridRow ? groups : kGridRow, y, (groups - 1) / kGridRow + 1);
+}
+__device__ __forceinline__ int64_t column_group() { return static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x; }
+
 // How a launch lays its threads over the logits: tx threads side by side along
 // a row (a power of two), 256 / tx rows at a time, `splits` ranges of rows.
 struct Grid {
@@ -86,7 +94,7 @@ struct Columns {
 // at the last column (its columns are then computed twice, alike).
 template <int VE>
 __device__ __forceinline__ Columns columns_of(int32_t B, int32_t tx) {
-  const int64_t c = (static_cast<int64_t>(blockIdx.x) * tx + (threadIdx.x & (tx - 1))) * VE;
+  const int64_t c = (column_group() * tx + (threadIdx.x & (tx - 1))) * VE;
   return {c + VE <= B ? c : static_cast<int64_t>(B) - VE, c < B};
 }
 
@@ -297,7 +305,7 @@ __global__ void __launch_bounds__(256) distill_loss_kernel(const T* __restrict__
   __shared__ Run red[256];
   __shared__ float fin[256];
   const int tx = threadIdx.x % NX, ty = threadIdx.x / NX;
-  const int64_t col = static_cast<int64_t>(blockIdx.x) * NX + tx;
+  const int64_t col = column_group() * NX + tx;
   const bool on = col < B;
   const float inv_t = 1.0f / temp;
   Run a = {-__builtin_inff(), 0.0f, 0.0f};
@@ -463,7 +471,7 @@ __global__ void __launch_bounds__(256) distill_sparse_kernel(const T* __restrict
   __shared__ int32_t si[PASSED][NX];
   __shared__ float se[PASSED][NX];
   const int tx = threadIdx.x % NX, ty = threadIdx.x / NX;
-  const int64_t b = B, at = static_cast<int64_t>(blockIdx.x) * NX + tx;
+  const int64_t b = B, at = column_group() * NX + tx;
   const bool on = at < b;
   const int64_t col = on ? at : b - 1;  // past the last: read again, nothing written
   const int64_t j0 = static_cast<int64_t>(blockIdx.y) * NY * OWN + ty;
@@ -588,13 +596,14 @@ int fwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, cons
              float* loss, float* stats, float* part, hipStream_t stream) {
   const Grid g = grid_of(d);
   const T* Z = static_cast<const T*>(Zt);
-  hipLaunchKernelGGL((distill_sums_kernel<T, VE, TWO, ONE>), dim3(g.blocks, g.splits), dim3(256), 0, stream, Z,
+  hipLaunchKernelGGL((distill_sums_kernel<T, VE, TWO, ONE>), column_grid(g.blocks, g.splits), dim3(256), 0, stream, Z,
                      d->classes, d->batch, g, d->top, idx, tl, labels, d->temperature, d->soft_weight, part, loss,
                      stats);
   ARD_LAUNCH_CHECK();
   if (ONE) return ARD_OK;
-  hipLaunchKernelGGL((distill_loss_kernel<T, TWO>), dim3((d->batch - 1) / 16 + 1), dim3(256), 0, stream, Z, d->classes,
-                     d->batch, d->top, idx, tl, labels, d->temperature, d->soft_weight, g.splits, part, loss, stats);
+  hipLaunchKernelGGL((distill_loss_kernel<T, TWO>), column_grid((d->batch - 1) / 16 + 1, 1), dim3(256), 0, stream, Z,
+                     d->classes, d->batch, d->top, idx, tl, labels, d->temperature, d->soft_weight, g.splits, part,
+                     loss, stats);
   ARD_LAUNCH_CHECK();
   return ARD_OK;
 }
@@ -605,7 +614,7 @@ int bwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, cons
   const Grid g = grid_of(d);
   const T* Z = static_cast<const T*>(Zt);
   T* dZ = static_cast<T*>(dZt);
-  hipLaunchKernelGGL((distill_dense_kernel<T, VE, TWO, ONE>), dim3(g.blocks, g.splits), dim3(256), 0, stream, Z,
+  hipLaunchKernelGGL((distill_dense_kernel<T, VE, TWO, ONE>), column_grid(g.blocks, g.splits), dim3(256), 0, stream, Z,
                      d->classes, d->batch, g, d->top, idx, tl, labels, stats, dloss, d->temperature, d->soft_weight,
                      dZ);
   ARD_LAUNCH_CHECK();
@@ -613,8 +622,8 @@ int bwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, cons
     // few entries: fewer for each thread (20 of 700 columns, 8800 classes: backward 22.7 us, with 8 24.5)
     auto entries = [&](auto own) {
       constexpr int OWN = decltype(own)::value;
-      hipLaunchKernelGGL((distill_sparse_kernel<T, TWO, OWN>), dim3((d->batch - 1) / 16 + 1, d->top / (16 * OWN) + 1),
-                         dim3(256), 0, stream, Z, d->classes, d->batch, d->top, idx, tl, labels, stats, dloss,
+      const dim3 grid = column_grid((d->batch - 1) / 16 + 1, d->top / (16 * OWN) + 1);
+      hipLaunchKernelGGL((distill_sparse_kernel<T, TWO, OWN>), grid, dim3(256), 0, stream, Z, d->classes, d->batch, d->top, idx, tl, labels, stats, dloss,
                          d->temperature, d->soft_weight, dZ);
     };
     if (d->top < 32) entries(std::integral_constant<int, 2>{});

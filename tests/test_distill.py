@@ -249,3 +249,29 @@ def test_in_a_graph(V, B):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(loss, eager[0]) and torch.equal(dZ, eager[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("top", [1, 17])
+def test_more_columns_than_a_row_of_workgroups(top):
+    """2^28 columns and a few of three classes: 16 threads for each would pass 2^32. Columns repeat after 1009."""
+    from gpu_util import device, workspace
+    dev, V, B, few = device(), 3, (1 << 28) + 5, 1009
+    Z, idx, t, labels, _ = _inputs("bf16", V, few, top, 33)
+    want, dwant = _run("bf16", Z, idx, t, labels, 2.0, 0.5, None)
+
+    def wide(x):
+        x = x.to(dev)
+        out = torch.empty(*x.shape[:-1], B, dtype=x.dtype, device=dev)
+        whole = B // few * few
+        out[..., :whole].unflatten(-1, (-1, few)).copy_(x[..., None, :].expand(*x.shape[:-1], B // few, few))
+        out[..., whole:] = x[..., :B - whole]
+        return out
+    desc = api.distill_desc(api.ARD_BF16, B, V, top, 2.0, 0.5)
+    Z, idx, t, labels = (wide(x) for x in (Z, idx, t, labels))
+    loss, stats, dZ = torch.full((B,), 7.0, device=dev), torch.empty(5, B, device=dev), torch.full_like(Z, 7.0)
+    ws = workspace(api.ard_distill_workspace_bytes(desc))
+    api.ard_distill_fwd(desc, Z, idx, t, labels, loss, stats, ws)
+    api.ard_distill_bwd(desc, Z, idx, t, labels, stats, None, dZ)
+    torch.cuda.synchronize()
+    assert torch.equal(loss, wide(torch.tensor(want).float())) and torch.equal(dZ, wide(torch.tensor(dwant).bfloat16()))
