@@ -29,6 +29,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "../ard_gemm_fast.hpp"
 #include "../ard_internal.hpp"
@@ -482,7 +483,7 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   id /= g.wtiles;
   const int head = id % g.heads, seq = id / g.heads;
   const Span sp = span_of(g, seq);
-  const int t0 = seg * g.seg_len, t1 = min(sp.len, t0 + g.seg_len);
+  const int t0 = seg * g.seg_len, t1 = t0 + min(sp.len - t0, g.seg_len);
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int w0 = wt * M::WD, wrows = min(g.wdim - w0, M::WD);
   const int64_t hs = static_cast<int64_t>(seq) * g.heads + head;
@@ -530,7 +531,7 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
   else at_icols ^= ic, at_scols ^= sc;
   const int at_out = OutOps::template base_block<kChunk>() ^ ((wv & 3) * 16 * M::OS);
 
-  const int nchunk = (t1 - t0 + kChunk - 1) / kChunk;
+  const int nchunk = static_cast<int>((static_cast<uint32_t>(t1 - t0) + kChunk - 1) / kChunk);
   auto first_of = [&](int c) { return t0 + (M::REV ? nchunk - 1 - c : c) * kChunk; };
   auto fetch = [&](int c) {
     const int t = first_of(c);
@@ -792,7 +793,7 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
   id /= g.nseg;
   const int head = id % g.heads, seq = id / g.heads;
   const Span sp = span_of(g, seq);
-  const int t0 = seg * g.seg_len, t1 = min(sp.len, t0 + g.seg_len);
+  const int t0 = seg * g.seg_len, t1 = t0 + min(sp.len - t0, g.seg_len);
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int64_t hs = static_cast<int64_t>(seq) * g.heads + head;
   const int64_t sdim = static_cast<int64_t>(g.ydim) * g.wdim;
@@ -841,7 +842,7 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
   at_icols.lo ^= ib * 32, at_icols.hi ^= ib * 32;
   const int at_out = OutOps::template base_block<kChunk>() ^ (ib * 16 * P::OS);
 
-  const int nchunk = (t1 - t0 + kChunk - 1) / kChunk;
+  const int nchunk = static_cast<int>((static_cast<uint32_t>(t1 - t0) + kChunk - 1) / kChunk);
   auto first_of = [&](int c) { return t0 + (nchunk - 1 - c) * kChunk; };
   auto fetch = [&](int c) {
     const int t = first_of(c);
@@ -1149,6 +1150,9 @@ constexpr int kFill4 = 512, kFill8 = 256;  // workgroups of four or eight waves 
 
 int pad_dim(int d) { return d <= 64 ? 64 : 128; }
 
+// The longest that a sequence can be: max_len may be any bound, and tokens are all there are.
+int longest(const ard_linattn_desc* d) { return std::min(d->max_len, d->tokens); }
+
 // How one run lays out its work: rows of a w tile, and segments.
 struct MixPlan {
   int yd, wd, wtiles, nseg, seg_len;
@@ -1159,11 +1163,11 @@ MixPlan plan_mix(const ard_linattn_desc* d, int ydim, int wdim) {
   p.wd = d->dtype == ARD_BF16 ? pad_dim(wdim) : 64;
   p.wtiles = (wdim + p.wd - 1) / p.wd;
   // as many sequences as there can be of the longest length: of ragged ones, most are shorter
-  const int64_t full = std::min<int64_t>(d->n_seqs, (d->tokens - 1) / d->max_len + 1);
+  const int64_t full = std::min<int64_t>(d->n_seqs, (d->tokens - 1) / longest(d) + 1);
   const int64_t base = full * d->q_heads * p.wtiles, fill = p.yd == 64 ? kFill4 : kFill8;
   // fp32 is bound by its products, which a second pass adds to, but not by as much as idle units
   const int64_t n = base >= (d->dtype == ARD_BF16 ? fill / 2 : fill) ? 1 : (fill + base - 1) / base;
-  const int64_t chunks = (static_cast<int64_t>(d->max_len) + kChunk - 1) / kChunk;
+  const int64_t chunks = (static_cast<int64_t>(longest(d)) + kChunk - 1) / kChunk;
   int64_t per = (chunks + n - 1) / n;
   if (n > 1) {
     // Segments, shorter than four chunks where it gains: the chunks that one workgroup goes
@@ -1183,7 +1187,7 @@ MixPlan plan_mix(const ard_linattn_desc* d, int ydim, int wdim) {
     }
     per = best;
   }
-  p.seg_len = static_cast<int>(per * kChunk);
+  p.seg_len = static_cast<int>(std::min<int64_t>(per * kChunk, std::numeric_limits<int>::max()));
   p.nseg = static_cast<int>((chunks + per - 1) / per);
   return p;
 }
@@ -1247,7 +1251,7 @@ hipError_t run_mix(const MixArgs& g, bool part, hipStream_t stream) {
 void fill_args(const ard_linattn_desc* d, const MixPlan& p, MixArgs* g) {
   g->offsets = d->d_offsets;
   g->n_seqs = d->n_seqs;
-  g->max_len = d->max_len;
+  g->max_len = longest(d);
   g->tokens = d->tokens;
   g->heads = d->q_heads;
   g->group = d->q_heads / d->kv_heads;

@@ -507,3 +507,33 @@ def test_tokens_that_are_not_finite_in_every_chunk(dtype, name):
         _right(c, g, backward[0][i], backward[1][i], what, i == 3)
     for a, b in zip(clean, spoilt):
         assert b < 10 * a, (clean, spoilt)
+
+
+@pytest.mark.parametrize("dtype", [api.ARD_F32, api.ARD_BF16])
+def test_a_bound_of_the_length_past_the_tokens_is_the_tokens(dtype):
+    for n, heads in ((640, 4), (640, 300), (5000, 1)):
+        desc = lambda most: api.linattn_desc(dtype, 3, most, n, heads, heads, 64, 64, 1.0, 4096)  # noqa: E731
+        need = api.ard_linattn_workspace_bytes(desc(n))
+        for most in (n + 1, 1 << 20, (1 << 31) - 1):
+            assert api.ard_linattn_workspace_bytes(desc(most)) == need
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [2, 300])
+def test_the_largest_bound_of_the_length(dtype, heads):
+    """max_len 2^31 - 1, as of a caller that knows no bound: what the longest sequence's own length gives."""
+    from gpu_util import device, workspace
+    c = Case(dtype, [300, 1, 90], heads, heads, 8, 8, True, seed=17)
+    desc, dev = c.desc(), device()
+    desc.max_len = (1 << 31) - 1
+    ws = workspace(api.ard_linattn_workspace_bytes(desc))
+    put = [_put(x) for x in (c.Q, c.K, c.V, c.g, c.S0)]
+    O, ST = torch.full((c.heads * c.dv, c.n), 7.0, dtype=c.Q.dtype, device=dev), torch.full_like(put[4], 7.0)
+    grads = [torch.full_like(x, 7.0) for x in put[:3] + put[4:]]
+    api.ard_linattn_fwd(desc, *put, O, ST, ws)
+    api.ard_linattn_bwd(desc, *put, _put(c.dO), _put(c.dST), *grads, ws)
+    torch.cuda.synchronize()
+    want, size = c.forward() + c.backward(), c.forward(size=True) + c.backward(size=True)
+    for got, w, s, what in zip([O, ST] + grads, want, size, ("O", "ST", "dQ", "dK", "dV", "dS0")):
+        c.inside(got, w, s, what, state="S" in what)
