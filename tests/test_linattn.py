@@ -537,3 +537,28 @@ def test_the_largest_bound_of_the_length(dtype, heads):
     want, size = c.forward() + c.backward(), c.forward(size=True) + c.backward(size=True)
     for got, w, s, what in zip([O, ST] + grads, want, size, ("O", "ST", "dQ", "dK", "dV", "dS0")):
         c.inside(got, w, s, what, state="S" in what)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("told", [[-7, 30, 200], [50, 20, 140], [200, 300, -4], [0, 126, 2 ** 31 - 1]])
+def test_offsets_are_held_to_the_row_and_lengths_to_the_bound(dtype, told):
+    """Offsets in front of the row, past it and decreasing, and a sequence longer than max_len (60, of 126 columns): the
+    columns that are meant, and nothing anywhere else."""
+    from gpu_util import ard_dtype, device, workspace
+    dev, n, heads, dk, dv = device(), 126, 2, 24, 40
+    c = Case(dtype, [n, 0], heads, 1, dk, dv, True, seed=18)
+    put = [_put(x) for x in (c.Q, c.K, c.V, c.g, c.S0, c.dO, c.dST)]
+    O, ST = torch.full_like(put[5], 7.0), torch.full_like(put[4], 7.0)
+    grads = [torch.full_like(x, 7.0) for x in put[:3] + put[4:5]]
+    off = torch.tensor(told, dtype=torch.int32, device=dev)
+    d = api.linattn_desc(ard_dtype(dtype), 2, 60, n, heads, 1, dk, dv, c.scale, off)
+    ws = workspace(api.ard_linattn_workspace_bytes(d))
+    api.ard_linattn_fwd(d, *put[:5], O, ST, ws)
+    api.ard_linattn_bwd(d, *put, *grads, ws)
+    torch.cuda.synchronize()
+    held = [[min(max(x, 0), n) for x in told[s:s + 2]] for s in (0, 1)]
+    c.spans = [(b, b + min(max(e - b, 0), 60)) for b, e in held]
+    want, size = c.forward() + c.backward(), c.forward(size=True) + c.backward(size=True)
+    for g, w, s, what in zip((O, ST, *grads), want, size, ("O", "ST", "dQ", "dK", "dV", "dS0")):
+        c.inside(g, w, s, what, state="S" in what)
