@@ -623,8 +623,8 @@ int bwd_impl(const ard_distill_desc* d, const void* Zt, const int32_t* idx, cons
     auto entries = [&](auto own) {
       constexpr int OWN = decltype(own)::value;
       const dim3 grid = column_grid((d->batch - 1) / 16 + 1, d->top / (16 * OWN) + 1);
-      hipLaunchKernelGGL((distill_sparse_kernel<T, TWO, OWN>), grid, dim3(256), 0, stream, Z, d->classes, d->batch, d->top, idx, tl, labels, stats, dloss,
-                         d->temperature, d->soft_weight, dZ);
+      hipLaunchKernelGGL((distill_sparse_kernel<T, TWO, OWN>), grid, dim3(256), 0, stream, Z, d->classes, d->batch,
+                         d->top, idx, tl, labels, stats, dloss, d->temperature, d->soft_weight, dZ);
     };
     if (d->top < 32) entries(std::integral_constant<int, 2>{});
     else entries(std::integral_constant<int, 8>{});

@@ -275,3 +275,43 @@ def test_more_columns_than_a_row_of_workgroups(top):
     api.ard_distill_bwd(desc, Z, idx, t, labels, stats, None, dZ)
     torch.cuda.synchronize()
     assert torch.equal(loss, wide(torch.tensor(want).float())) and torch.equal(dZ, wide(torch.tensor(dwant).bfloat16()))
+
+
+def _terms(z, idx, t, labels, T, a):
+    """The sums of the absolute values of each gradient value's terms, in 64 bits."""
+    V, B = z.shape
+    out = np.zeros((V, B))
+    for b in range(B):
+        if z[:, b].max() == -INF:
+            continue
+        ok = [j for j in range(idx.shape[0]) if 0 <= idx[j, b] < V]
+        if a > 0 and ok and max(t[j, b] for j in ok) > -INF:
+            out[:, b] += a * T * od._softmax(z[:, b] / T)
+            for j, p in zip(ok, od._softmax(np.array([t[j, b] for j in ok]) / T)):
+                out[idx[j, b], b] += a * T * p
+        if a < 1 and labels is not None and 0 <= labels[b] < V:
+            out[:, b] += (1 - a) * od._softmax(z[:, b])
+            out[labels[b], b] += 1 - a
+    return out
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,B,top,T,a", [
+    (10, 128, 5, 4.0, 0.9), (333, 9, 1, 1.0, 1.0), (257, 100, 17, 0.5, 0.5), (8800, 20, 20, 2.0, 0.5),
+    (1031, 65, 8, 1.0, 0.7), (64, 700, 4, 2.0, 0.3), (5003, 16, 300, 1.5, 0.4), (700, 12, 0, 2.0, 0.5)])
+def test_each_value_of_the_gradient_for_its_size(dtype, V, B, top, T, a):
+    """Small probabilities too: each value against its own terms. A term is an exponential (the rounding of its argument x,
+    three times, is 3 |x| 2^-24 of it, |x| at most `span`) over a sum, times a factor: 64 + 4 span units of its size, and the
+    rounding of the result; values below the smallest normal numbers may be 0."""
+    Z, idx, t, labels, dloss = _inputs(dtype, V, B, top, V + B)
+    for lab, dl in ((labels, dloss), (None, None)):
+        _, dgot = _run(dtype, Z, idx, t, lab, T, a, dl)
+        z, i, tt = Z.double().numpy(), idx.numpy(), t.double().numpy()
+        ll, d = None if lab is None else lab.numpy(), 1.0 if dl is None else dl.double().numpy()
+        want, terms = od.batch(z, i, tt, ll, T, a)[1] * d, _terms(z, i, tt, ll, T, a) * np.abs(d)
+        span = 1 + (z.max(0) - z.min(0)).max() / min(T, 1.0)
+        out = UBF if dtype == "bf16" else U32
+        bound = (64 + 4 * span) * U32 * terms
+        bound += out * (np.abs(want) + bound) + 2.0 ** -126 * (1 + a * T) * np.abs(d)
+        assert (np.abs(dgot - want) <= bound).all(), (np.abs(dgot - want) / bound).max()
