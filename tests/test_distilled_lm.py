@@ -75,3 +75,55 @@ def test_gradients_against_differences():
         want, got = (up - down) / (2 * h), float((grad * step).sum())
         # rounding of the two losses (2^-22 each of about 5) over 2 h, and the third derivative's part
         assert abs(got - want) < 2e-2 * float(grad.norm() * step.norm()) / W.numel() ** 0.5 + 2e-6 / h, (name, got, want)
+
+
+@pytest.mark.gpu
+def test_gradients_of_every_kept_weight():
+    """As above along directions that follow from the pattern, not from the gradients: one that a call leaves at 0 by
+    mistake counts. The three parts of the first projection (queries, keys, values) and the two of the gated layer each for
+    themselves; dropped weights have no gradient."""
+    from paper_1805_08939_amd import api
+    lm, model = _model()
+    dev, seqs, length, w = model.dev, 2, 20, model.width
+    n = seqs * length
+    teacher = lm.Teacher(61, 6, dev)
+    tokens, idx, t, labels = teacher.batch(seqs, length, torch.Generator(device=dev).manual_seed(5))
+    plan = api.ard_plan_rows(96, 2, 1, None)
+    dist = api.distill_desc(lm.ARD_DTYPE, n, 61, 6, 1.0, 0.5)
+    loss, stats, share = torch.empty(n, device=dev), torch.empty(5, n, device=dev), torch.full((n,), 1.0 / n, device=dev)
+
+    def value():
+        logits, _, saved = model.forward(tokens, plan, 2.0, train=True)
+        ws = model._space(api.ard_distill_workspace_bytes(dist))
+        api.ard_distill_fwd(dist, logits, idx, t, labels, loss, stats, ws)
+        return logits, saved, float(loss.double().mean())
+
+    logits, saved, _ = value()
+    dlogits = torch.empty_like(logits)
+    api.ard_distill_bwd(dist, logits, idx, t, labels, stats, share, dlogits)
+    model.backward(dlogits, plan, saved)
+    units = (torch.arange(96, device=dev) % 2 == 1).float()
+    on = {name: torch.ones_like(getattr(model, name).W) for name in ("mix", "head")}
+    on["down"] = units.expand(w, 96).clone()
+    for i in (0, 1):
+        on["glu", i] = torch.zeros_like(model.glu.W)
+        on["glu", i][i] = units[:, None]
+    for i in (0, 1, 2):
+        on["qkv", i] = torch.zeros_like(model.qkv.W)
+        on["qkv", i][i * w:(i + 1) * w] = 1.0
+    gen = torch.Generator(device=dev).manual_seed(6)
+    for name, mask in on.items():
+        p = getattr(model, name if isinstance(name, str) else name[0])
+        W, grad = p.W.clone(), p.dW.double()
+        step = torch.randn(W.shape, device=dev, generator=gen) * mask
+        h = 2e-3 * float((W * mask).norm() / step.norm())
+        p.W.copy_(W + h * step)
+        up = value()[2]
+        p.W.copy_(W - h * step)
+        down = value()[2]
+        p.W.copy_(W)
+        want, part = (up - down) / (2 * h), grad * mask
+        got, size = float((part * step).sum()), float(part.norm() * step.norm()) / float(mask.sum()) ** 0.5
+        # rounding of the two losses (2^-22 each of about 5) over 2 h, and the third derivative's part
+        assert size > 0 and abs(got - want) < 2e-2 * size + 2e-6 / h, (name, got, want, size)
+    assert not (model.glu.dW * (1 - units)[:, None]).any() and not (model.down.dW * (1 - units)).any()
