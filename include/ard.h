@@ -579,9 +579,11 @@ int ard_glu_bwd(const ard_glu_desc* desc, const void* Xt, const void* W, const v
  * are all -inf) has no first term, one whose label is outside 0 .. V - 1
  * (labels NULL: every one) no second term, and one whose logits are all -inf
  * neither: loss and gradient are then 0 there. Logits of -inf are masked
- * classes: their gradient is 0, and a teacher's entry of positive weight there
- * makes the loss +inf. NaN propagates within its column. An entry that names a
- * class again adds its own share.
+ * classes: q and q1 are 0 there, and the gradient is 0 where no valid entry of
+ * positive weight and no label names the class. One that does makes the loss
+ * +inf, with the gradient of the formula, -a T p_j and -(1 - a), there. NaN
+ * propagates within its column. An entry that names a class again adds its own
+ * share.
  * fwd: loss[B]; stats[5][B] is kept for the backward.
  * bwd: dloss[B] (NULL = 1) -> dZt[V][B], not in place.
  */

@@ -315,3 +315,29 @@ def test_each_value_of_the_gradient_for_its_size(dtype, V, B, top, T, a):
         bound = (64 + 4 * span) * U32 * terms
         bound += out * (np.abs(want) + bound) + 2.0 ** -126 * (1 + a * T) * np.abs(d)
         assert (np.abs(dgot - want) <= bound).all(), (np.abs(dgot - want) / bound).max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [6, 700])
+def test_masked_classes_that_an_entry_or_the_label_names(dtype, V):
+    """Logits of -inf: gradient 0, but for the classes of the teacher's entries (-a T p) and the label (-(1 - a)), whose
+    columns have a loss of +inf. Powers of two, so that every value is exact."""
+    Z = torch.full((V, 4), -INF, dtype=synth.storage_dtype(dtype))
+    Z[0], Z[1] = 0.0, 0.0                                # q = q1 = 1/2 each
+    idx = torch.tensor([[3, 0, 0, 3], [4, 1, 1, 0]], dtype=torch.int32)
+    t = torch.tensor([[1.0, 1, 1, -INF], [1.0, 1, 1, 1]])  # p = 1/2 each, in the last column 0 and 1
+    labels = torch.tensor([0, 5, 1, 1], dtype=torch.int32)
+    loss, dZ = _run(dtype, Z, idx, t, labels, 2.0, 0.5, None)
+    want = np.zeros((V, 4))
+    want[0], want[1] = 0.75, 0.75                        # a T q + (1 - a) q1
+    want[[3, 4], 0] = -0.5                               # - a T p
+    want[0, 0] -= 0.5                                    # - (1 - a)
+    want[[0, 1], 1] -= 0.5
+    want[5, 1] = -0.5
+    want[[0, 1], 2] -= 0.5
+    want[1, 2] -= 0.5
+    want[0, 3] -= 1.0
+    want[1, 3] -= 0.5
+    assert np.array_equal(np.isposinf(loss), [True, True, False, False]) and np.isfinite(loss[2:]).all()
+    assert np.array_equal(dZ, want)
