@@ -1140,7 +1140,7 @@ int check_desc(const ard_linattn_desc* d) {
   if (reinterpret_cast<uintptr_t>(d->d_offsets) % 4) return fail(ARD_ERR_INVALID_ARG, "d_offsets is not 4-byte aligned");
   if (static_cast<int64_t>(d->kv_heads) * std::max(d->key_dim, d->value_dim) > 65535)
     return fail(ARD_ERR_UNSUPPORTED, "%d key heads: at most 65535 rows of keys or values", d->kv_heads);
-  // one workgroup per sequence, head, tile and segment, numbered in 31 bits
+  // a workgroup of up to 512 threads for each sequence, head, tile (two at most) and segment (plan_mix)
   if (static_cast<int64_t>(d->n_seqs) * d->q_heads >= (int64_t{1} << 22))
     return fail(ARD_ERR_UNSUPPORTED, "%d sequences of %d heads: at most 2^22 states", d->n_seqs, d->q_heads);
   return ARD_OK;
@@ -1181,7 +1181,9 @@ MixPlan plan_mix(const ard_linattn_desc* d, int ydim, int wdim) {
     const double state = 4.0 * static_cast<double>(d->n_seqs) * d->q_heads * p.wtiles * p.yd * p.wd * 4 / 5.2e6;
     double least = chunks * tc;
     int64_t best = chunks;
+    const int64_t tiles = static_cast<int64_t>(d->n_seqs) * d->q_heads * p.wtiles;
     for (int64_t q = std::max(per, std::min<int64_t>(4, chunks - 1)); q >= per && q < chunks; --q) {
+      if (tiles * ((chunks + q - 1) / q) >= int64_t{1} << 23) continue;  // threads of a launch below 2^32
       const double us = q * tc * 4 / 3 + 11.0 + (state + 0.25) * static_cast<double>((chunks + q - 1) / q);
       if (us < 0.97 * least) least = us, best = q;
     }

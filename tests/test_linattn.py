@@ -518,6 +518,16 @@ def test_a_bound_of_the_length_past_the_tokens_is_the_tokens(dtype):
             assert api.ard_linattn_workspace_bytes(desc(most)) == need
 
 
+@pytest.mark.parametrize("dtype,dim", [(api.ARD_F32, 64), (api.ARD_F32, 128), (api.ARD_BF16, 64), (api.ARD_BF16, 128)])
+def test_no_plan_passes_the_threads_of_a_launch(dtype, dim):
+    """Many short sequences told with a loose bound: a workgroup of up to 512 threads for each state of a segment (fp32: for
+    each 64 of its columns)."""
+    tile = dim * (64 if dtype == api.ARD_F32 else dim) * 4
+    for tokens in (1 << 20, 1 << 24, 1 << 27, (1 << 31) - 1):
+        desc = api.linattn_desc(dtype, (1 << 22) - 1, tokens, tokens, 1, 1, dim, dim, 1.0, 4096)
+        assert api.ard_linattn_workspace_bytes(desc) // tile * 512 < 1 << 32
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("heads", [2, 300])
