@@ -415,3 +415,10 @@ def test_columns_past_the_load_offsets():
     N, B = 8300, 1 << 18
     assert N // 2 * B * 2 > 2 ** 31
     _large("bf16", B, 8, N, 2, 1, "silu", 2.0)
+
+
+@pytest.mark.gpu
+def test_every_one_of_many_units():
+    """More tiles of units than 2^16 in the products, and more groups of units than a row in the few-column kernel."""
+    _large("f32", 17, 4, (1 << 23) + 5, 1, 0, "silu", 1.0)
+    _large("bf16", 3, 4, (1 << 24) + 3, 1, 0, "gelu", 1.0, backward=False)
