@@ -550,7 +550,7 @@ typedef struct {
   int32_t dtype;
   int32_t batch;            /* B >= 1 */
   int32_t in_features;      /* K >= 1 */
-  int32_t hidden_features;  /* N >= 1 */
+  int32_t hidden_features;  /* N: 1 .. 2^30 - 1 */
   const ard_row_plan* hidden_plan;  /* n == N (a list is not needed), or NULL = every unit kept */
   float scale;
   int32_t act;              /* ARD_GLU_* */
@@ -615,7 +615,8 @@ int ard_distill_bwd(const ard_distill_desc* desc, const void* Zt, const int32_t*
  * S[n_seqs][q_heads][key_dim][value_dim] fp32. Head h reads the keys and
  * values of head h / (q_heads / kv_heads). Sequence s is the columns
  * d_offsets[s] .. d_offsets[s + 1] - 1 (device memory; at most max_len of
- * them, none is allowed; entries are clamped to 0 .. tokens), or, with
+ * them, none is allowed; entries are clamped to 0 .. tokens; plan and workspace
+ * follow from max_len, a bound past tokens counting as tokens), or, with
  * d_offsets NULL, the columns s * max_len .. (s + 1) * max_len - 1. Columns of
  * no sequence are not touched. A token that is not finite reaches only what the
  * formulas have it in, not the tokens in front of it.

@@ -553,6 +553,9 @@ constexpr int kBlocks = 512;  // workgroups that fill the chip: two on a compute
 // Few classes: one column per thread and 16 threads down its rows, the whole pass in
 // one launch. A launch costs what the reading of some hundred rows does (10 classes,
 // 128 columns, fp32, forward and backward: 11.6 us, in four launches of wide rows 18.5).
+// 256 classes, bf16, 5 entries, forward and backward, calls with their host's part: 1024
+// columns 16.1 us in two launches, 24.2 in four; 8192 16.7 and 25.9. Only at 65536 columns
+// do the single elements cost more than the launches: 73.2 and 65.7 (64 classes 32.8 and 43.5).
 constexpr int kOneLaunch = 256;
 bool one_launch(const ard_distill_desc* d) { return d->classes <= kOneLaunch; }
 // The backward's one launch compares every entry with every other from memory: 16 entries

@@ -5,10 +5,12 @@
 // the matrix cores; grids too small for its tiles (and weights past 2^31 bytes) run both
 // projections as a batched product and join them. Backward: one pass writes the derivatives
 //   dg = scale dh u act'(g),  du = scale dh act(g)
-// of the kept rows (rounded to the element type once) and their row sums, the
-// bias gradients, from the unrounded values; then dX = W0^T dg + W1^T du as one
-// product over both halves, and dW as a batch of two. A pattern's kept rows are an
-// arithmetic progression, so every gather is a row stride.
+// of the kept rows and their row sums, the bias gradients; then dX = W0^T dg + W1^T du as one
+// product over both halves, and dW as a batch of two. The derivatives are rounded to the
+// element type once, as operands of those products (the row sums are not): with bf16 the
+// gradients' error is 1.4 times that of fp32 derivatives, whose products would run at 1/7
+// of the rate. A pattern's kept rows are an arithmetic progression, so every gather is a
+// row stride.
 
 #include <hip/hip_runtime.h>
 
@@ -668,8 +670,11 @@ double work_of(const GluShape& s) { return static_cast<double>(s.kept) * s.K * s
 // 47, 100 x 1023 -> 512 17.8 to 19.8.
 bool fwd_copies(const GluShape& s) { return one_product(s) || work_of(s) >= (s.es == 2 ? 32e6 : 400e6); }
 // The backward copies beside the derivatives: the weights always (bf16 70 x 301 -> 500 24 to
-// 19, 1681 x 1194 -> 1330 190 to 84), X for dW where its product is more than a few slabs:
-// 133 x 2729 -> 2735 83 to 74, 255 x 2000 -> 2000 48 to 42, but 100 x 1023 -> 512 kept 24 to 30.
+// 19, 1681 x 1194 -> 1330 190 to 84), X for dW from 1e8 multiply-adds of a projection on,
+// where both types gain. us without and with the copy of X, dW in fp32: bf16 133 x 512 -> 512
+// (3.5e7) 17.8 to 20.4, 255 x 512 -> 512 (6.7e7) 18.4 to 17.5, 101 x 1024 -> 1024 (1.1e8) 29.0
+// to 27.1, 255 x 2048 -> 2048 (1.1e9) 49.3 to 43.9; fp32 22.0 to 23.1, 24.2 to 24.6, 30.0 to
+// 28.6, 103.5 to 91.1. Smaller ones lie between a gain of 4 us and a loss of 3.
 bool bwd_copies_x(const GluShape& s) { return work_of(s) >= 100e6; }
 template <typename T>
 Space fwd_space(const GluShape& s) {
