@@ -76,6 +76,12 @@ struct Decay {
   __device__ __forceinline__ explicit Decay(float g) : l2((g < -1e30f ? -1e30f : g) * 1.44269504088896340736f) {}
   __device__ __forceinline__ float pow(int n) const { return pow(static_cast<float>(n)); }
   __device__ __forceinline__ float pow(float n) const { return __builtin_amdgcn_exp2f(l2 * n); }
+  // Of an inner product that is no masked one: not 0, which mul_masked would take for the
+  // mask (what the smallest normal number adds is below every rounding).
+  __device__ __forceinline__ float weight(int n) const {
+    const float w = pow(n);
+    return w < 1.17549435e-38f ? 1.17549435e-38f : w;
+  }
 };
 
 // ------------------------------------------------------------------ LDS tiles
@@ -340,9 +346,15 @@ __device__ __forceinline__ void mend_outputs(const char* X, const char* Y, char*
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int n = (REV ? -1 : 1) * (16 * (ib - jb) + (lane & 15) - 4 * grp - r);
-      p[jb][r] = mul_masked(p[jb][r], n >= 0 ? cp * a.pow(max(n, 0)) : 0.0f);
+      p[jb][r] = mul_masked(p[jb][r], n >= 0 ? cp * a.weight(max(n, 0)) : 0.0f);
       in[jb][r] = n >= 0 ? 1.0f : 0.0f;
     }
+  bf16x8 pf[2], inf[2];  // of 32 tokens j each
+#pragma unroll
+  for (int h = 0; h < 2 && sizeof(T) == 2; ++h) {
+    pf[h] = __builtin_shufflevector(Ops<bf16>::round(p[2 * h]), Ops<bf16>::round(p[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
+    inf[h] = __builtin_shufflevector(Ops<bf16>::round(in[2 * h]), Ops<bf16>::round(in[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
+  }
 #pragma unroll 1
   for (int b = b0; b < b0 + blocks; ++b) {
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f}, q = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -368,10 +380,8 @@ __device__ __forceinline__ void mend_outputs(const char* X, const char* Y, char*
         bf16x4 hi = *O::template block<kChunk>(W, at_block, 16 * b, 32 * h + 16), hib;
         sort_out(lo, lob);
         sort_out(hi, hib);
-        acc = O::mma(__builtin_shufflevector(O::round(p[2 * h]), O::round(p[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7),
-                     __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), acc);
-        q = O::mma(__builtin_shufflevector(O::round(in[2 * h]), O::round(in[2 * h + 1]), 0, 1, 2, 3, 4, 5, 6, 7),
-                   __builtin_shufflevector(lob, hib, 0, 1, 2, 3, 4, 5, 6, 7), q);
+        acc = O::mma(pf[h], __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), acc);
+        q = O::mma(inf[h], __builtin_shufflevector(lob, hib, 0, 1, 2, 3, 4, 5, 6, 7), q);
       }
     } else {
 #pragma unroll
@@ -564,7 +574,7 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int n = (M::REV ? -1 : 1) * (16 * (ib - jb) + (lane & 15) - 4 * grp - r);
-        pw[jb][r] = n >= 0 ? g.cp * a.pow(n) : 0.0f;
+        pw[jb][r] = n >= 0 ? g.cp * a.weight(n) : 0.0f;
       }
   }
   auto weigh = [&](int L) {
@@ -729,9 +739,12 @@ __global__ void __launch_bounds__(M::NT, M::MINW) mix_kernel(MixArgs g) {
         if (n >= EPC) {
           *reinterpret_cast<u32x4_any*>(p) = v;
         } else {
-          const OutT* e = reinterpret_cast<const OutT*>(Out + tile_off<M::OS, kChunk>(r, cc));
+          int rc = r;  // addresses of their own: kept from chunk to chunk they would take the sums' registers
+          asm volatile("" : "+v"(rc));
+          OutT* o = op + rc * ld + cc * EPC;
+          const OutT* e = reinterpret_cast<const OutT*>(Out + tile_off<M::OS, kChunk>(rc, cc));
 #pragma unroll 1
-          for (int u = 0; u < n; ++u) p[u] = e[u];
+          for (int u = 0; u < n; ++u) o[u] = e[u];
         }
       }
     }
@@ -913,7 +926,7 @@ __global__ void __launch_bounds__(P::NT, 2) pair_kernel(PairArgs pa) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int n = 16 * (jb - ib) + 4 * grp + r - (lane & 15);
-          p[jb][r] = mul_masked(p[jb][r], n >= 0 ? g.cp * here.pow(max(n, 0)) : 0.0f);
+          p[jb][r] = mul_masked(p[jb][r], n >= 0 ? g.cp * here.weight(max(n, 0)) : 0.0f);
         }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {

@@ -572,3 +572,21 @@ def test_offsets_are_held_to_the_row_and_lengths_to_the_bound(dtype, told):
     want, size = c.forward() + c.backward(), c.forward(size=True) + c.backward(size=True)
     for g, w, s, what in zip((O, ST, *grads), want, size, ("O", "ST", "dQ", "dK", "dV", "dS0")):
         c.inside(g, w, s, what, state="S" in what)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ["Q", "K", "V", "dO"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_token_that_is_not_finite_is_not_forgotten(dtype, name, dim):
+    """Decays whose powers are 0 in 32 bits after some tokens, and 0 itself: what the formula has a token in that is not
+    finite is not finite, however far behind it, and the rest is right."""
+    c = Case(dtype, [200], 2, 2, dim, dim, True, decays=[1e-4, 0.0], seed=19)
+    x = getattr(c, name)
+    x[3, 37], x[dim + 5, 70], x[:, 130] = float("inf"), float("nan"), float("nan")
+    with np.errstate(invalid="ignore"):
+        forward, backward = (c.forward(), c.forward(size=True)), (c.backward(), c.backward(size=True))
+    for i, (g, what) in enumerate(zip(_fwd(c), ("O", "ST"))):
+        _right(c, g, forward[0][i], forward[1][i], what, i == 1)
+    for i, (g, what) in enumerate(zip(_bwd(c), ("dQ", "dK", "dV", "dS0"))):
+        _right(c, g, backward[0][i], backward[1][i], what, i == 3)
