@@ -341,3 +341,39 @@ def test_masked_classes_that_an_entry_or_the_label_names(dtype, V):
     want[1, 3] -= 0.5
     assert np.array_equal(np.isposinf(loss), [True, True, False, False]) and np.isfinite(loss[2:]).all()
     assert np.array_equal(dZ, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,B,top", [(1, 1, 1), (10, 3, 4), (256, 17, 16), (256, 17, 40), (257, 9, 5), (700, 1, 3), (5003, 13, 33),
+                                     (8800, 20, 0)])
+def test_nothing_else_is_read(dtype, V, B, top):
+    """NaN behind each operand's end, in the logits of entries that are none, in the workspace and in the outputs changes no
+    bit of what is computed."""
+    from gpu_util import ard_dtype, device
+    dev, nan = device(), float("nan")
+    Z, idx, t, labels, dloss = _inputs(dtype, V, B, top, 91)
+    if top > 1:
+        idx[1, ::2] = -1
+    desc = api.distill_desc(ard_dtype(dtype), B, V, top, 2.0, 0.5)
+
+    def inside(x, fill):  # on 16 bytes, `fill` behind it
+        whole = torch.full((x.numel() + 4096,), fill, dtype=x.dtype, device=dev)
+        whole[:x.numel()] = x.contiguous().flatten().to(dev)
+        return whole[:x.numel()].view(x.shape)
+
+    def run(fill, spoil):
+        tl = t.clone()
+        if spoil:
+            tl[idx < 0] = nan
+        z, i, tl, lab, dl = inside(Z, fill), inside(idx, 0), inside(tl, fill), inside(labels, 0), inside(dloss, fill)
+        ws = torch.full((api.ard_distill_workspace_bytes(desc) // 4 + 4,), fill, device=dev)
+        loss, stats, dZ = (torch.full(s, fill, device=dev) for s in ((B,), (5, B), (V, B)))
+        dZ = dZ.to(z.dtype)
+        told = (z, i, tl, lab) if top else (z, None, None, lab)
+        api.ard_distill_fwd(desc, *told, loss, stats, ws)
+        api.ard_distill_bwd(desc, *told, stats, dl, dZ)
+        torch.cuda.synchronize()
+        return loss, dZ
+    for got, want in zip(run(nan, True), run(0.0, False)):
+        assert torch.equal(got, want)

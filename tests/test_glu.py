@@ -422,3 +422,40 @@ def test_every_one_of_many_units():
     """More tiles of units than 2^16 in the products, and more groups of units than a row in the few-column kernel."""
     _large("f32", 17, 4, (1 << 23) + 5, 1, 0, "silu", 1.0)
     _large("bf16", 3, 4, (1 << 24) + 3, 1, 0, "gelu", 1.0, backward=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", SIZES)
+def test_nothing_else_is_read(size):
+    """NaN in the dropped rows of every operand, behind each operand's end, in the workspace and in the outputs changes no
+    bit of what is computed."""
+    from gpu_util import ard_dtype, device
+    dtype, B, K, N, period, offset, name = size
+    X, W, b, dH, Z, keep = _case(dtype, B, K, N, period, offset, name, seed=6)
+    dev, st, nan = device(), synth.storage_dtype(dtype), float("nan")
+    drop = torch.tensor(keep == 0)
+    desc = api.glu_desc(ard_dtype(dtype), B, K, N, api.ard_plan_rows(N, period, offset, None), 1.5, ACTS[name])
+    need = api.ard_glu_workspace_bytes(desc)
+
+    def inside(t, fill):  # on 16 bytes, `fill` behind it
+        t = t.contiguous()
+        whole = torch.full((t.numel() + 4096,), fill, dtype=t.dtype, device=dev)
+        whole[:t.numel()] = t.flatten().to(dev)
+        return whole[:t.numel()].view(t.shape)
+
+    def run(fill, spoil):
+        w, z, dh, bias = W.clone(), Z.transpose(1, 2).contiguous(), dH.T.contiguous(), b.clone()
+        if spoil:
+            w[:, drop], z[:, drop], dh[drop], bias[:, drop] = nan, nan, nan, nan
+        ws = torch.full((need // 4 + 4,), fill, device=dev)
+        x, w, z, dh, bias = (inside(t, fill) for t in (X.T, w, z, dh, bias))
+        H, Zt = torch.full((N, B), fill, dtype=st, device=dev), torch.zeros(2, N, B, dtype=st, device=dev)
+        api.ard_glu_fwd(desc, x, w, bias, Zt, H, ws)
+        dX, dW = torch.full((K, B), fill, dtype=st, device=dev), torch.full((2, N, K), fill, device=dev)
+        db = torch.full((2, N), fill, device=dev)
+        ws.fill_(fill)
+        api.ard_glu_bwd(desc, x, w, z, dh, dX, dW, db, ws)
+        torch.cuda.synchronize()
+        return H, Zt, dX, dW, db
+    for got, want in zip(run(nan, True), run(0.0, False)):
+        assert torch.equal(got, want)

@@ -590,3 +590,37 @@ def test_a_token_that_is_not_finite_is_not_forgotten(dtype, name, dim):
         _right(c, g, forward[0][i], forward[1][i], what, i == 1)
     for i, (g, what) in enumerate(zip(_bwd(c), ("dQ", "dK", "dV", "dS0"))):
         _right(c, g, backward[0][i], backward[1][i], what, i == 3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_nothing_behind_the_operands_is_read(dtype, shape):
+    """NaN behind each operand's end, in the workspace and in the outputs changes no bit of what is computed."""
+    from gpu_util import device
+    dev, nan = device(), float("nan")
+    c = Case(dtype, *shape, seed=sum(shape[0]) + 2)
+    d = c.desc()
+
+    def inside(t, fill):  # on 16 bytes, `fill` behind it
+        if t is None:
+            return None
+        whole = torch.full((t.numel() + 4096,), fill, dtype=t.dtype, device=dev)
+        whole[:t.numel()] = t.contiguous().flatten().to(dev)
+        return whole[:t.numel()].view(t.shape)
+
+    def run(fill):
+        put = [inside(x, fill) for x in (c.Q, c.K, c.V, c.g, c.S0, c.dO, c.dST)]
+        ws = torch.full((api.ard_linattn_workspace_bytes(d) // 4 + 4,), fill, device=dev)
+        O, ST = torch.full_like(put[5], fill), torch.full((len(c.lens), c.heads, c.dk, c.dv), fill, device=dev)
+        grads = [torch.full_like(x, fill) for x in put[:3]] + [torch.full_like(ST, fill)]
+        api.ard_linattn_fwd(d, *put[:5], O, ST, ws)
+        ws.fill_(fill)
+        api.ard_linattn_bwd(d, *put, *grads, ws)
+        torch.cuda.synchronize()
+        on = torch.zeros(c.n, dtype=torch.bool)
+        for b, e in c.spans:
+            on[b:e] = True
+        return [x[:, on] for x in (O, *grads[:3])] + [ST, grads[3]]
+    for got, want in zip(run(nan), run(0.0)):
+        assert torch.equal(got, want)
