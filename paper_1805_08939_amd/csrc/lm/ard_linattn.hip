@@ -294,7 +294,7 @@ __device__ __forceinline__ void split(const float (&f)[8], bf16x8 (&s)[N]) {
 //
 // v_mul_legacy_f32 by the name of its intrinsic, which the compiler has no builtin for (one
 // that lacks the intrinsic fails to link). A comparison and a choice in its place cost 2 to 8%:
-// 9 sequences of 16411 tokens, 16 heads of 64, bf16 83.5 to 89.4 us, their gradients 259 to 275.
+// 9 sequences, 16411 tokens in all, 16 heads of 64, bf16: 83.5 to 89.4 us, gradients 259 to 275.
 extern "C" __device__ __attribute__((const)) float mul_masked(float p, float weight) __asm("llvm.amdgcn.fmul.legacy");
 
 // Four values that w holds of a row: 0 in place of those that are not finite, and 1 for
