@@ -653,6 +653,39 @@ int ard_linattn_bwd(const ard_linattn_desc* desc, const void* Qt, const void* Kt
 int ard_linattn_step(const ard_linattn_desc* desc, const void* Qt, const void* Kt, const void* Vt,
                      const float* log_decay, const float* S0, void* Ot, float* ST, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* Root-mean-square norm of a sum (device).                                 */
+/* ------------------------------------------------------------------------ */
+/*
+ * For each column (token) of Xt and the residual stream Rt (NULL = 0):
+ *   s = x + r,  inv = 1 / sqrt(mean_k s_k^2 + eps),  y_k = gain_k s_k inv
+ * Layouts: Xt, Rt, St, Yt and the gradients [K][B] (dtype), gain and dgain [K]
+ * fp32 (gain NULL = 1), inv_rms[B] fp32. s is taken in fp32, before it is
+ * rounded into St; the sums over a column are 64 bits wide. A column that is
+ * not finite affects no other; with eps = 0 one of zeros gives NaN.
+ * fwd: St (may be NULL) receives s, the residual stream of the next layer,
+ * inv_rms (may be NULL) is kept for the backward.
+ * bwd, from St (Xt where there was no Rt) and inv_rms as the forward left them,
+ * with u = gain dY and xh = s inv:
+ *   dX = dS + inv (u - xh mean_k(u xh)),  dgain_k = sum_b dY_k xh_k
+ * dSt (NULL = 0) is the gradient that reaches s past the norm; dX is that of x
+ * and of r. dXt and dgain may be NULL. Outputs may be inputs of the same shape
+ * (the same buffer, whole), but St is not Yt.
+ */
+typedef struct {
+  int32_t dtype;
+  int32_t batch;     /* B >= 1 */
+  int32_t features;  /* K >= 1 */
+  float eps;         /* >= 0 */
+} ard_rmsnorm_desc;
+
+/* Workspace of fwd and bwd (0 is possible; NULL is accepted then). */
+size_t ard_rmsnorm_workspace_bytes(const ard_rmsnorm_desc* desc);
+int ard_rmsnorm_fwd(const ard_rmsnorm_desc* desc, const void* Xt, const void* Rt, const float* gain, void* St,
+                    void* Yt, float* inv_rms, void* ws, size_t ws_bytes, void* stream);
+int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* gain, const float* inv_rms,
+                    const void* dYt, const void* dSt, void* dXt, float* dgain, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

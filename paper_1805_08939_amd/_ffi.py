@@ -84,6 +84,10 @@ class ard_linattn_desc(ctypes.Structure):
                 ("d_offsets", c_vp)]
 
 
+class ard_rmsnorm_desc(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("batch", c_i32), ("features", c_i32), ("eps", c_f32)]
+
+
 # name -> (restype, argtypes); every symbol the header declares.
 SIGNATURES = {
     "ard_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -158,6 +162,11 @@ SIGNATURES = {
                                        c_vp, c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
     "ard_linattn_step": (ctypes.c_int, [ctypes.POINTER(ard_linattn_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
                                         c_vp]),
+    "ard_rmsnorm_workspace_bytes": (c_size, [ctypes.POINTER(ard_rmsnorm_desc)]),
+    "ard_rmsnorm_fwd": (ctypes.c_int, [ctypes.POINTER(ard_rmsnorm_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                       c_size, c_vp]),
+    "ard_rmsnorm_bwd": (ctypes.c_int, [ctypes.POINTER(ard_rmsnorm_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                       c_vp, c_size, c_vp]),
 }
 
 _lib = None

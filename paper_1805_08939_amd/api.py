@@ -16,7 +16,7 @@ from ._ffi import (ARD_ACT_NONE, ARD_ACT_RELU, ARD_BF16, ARD_DROPPED_SKIP, ARD_D
                    ARD_WEIGHTS_COMPACT, ARD_WEIGHTS_COMPACT_GRAD, ARD_WEIGHTS_FULL, ARD_WEIGHTS_INPUT_MAJOR,
                    ard_fc_desc, ard_lstm_desc, ard_lstm_tile_desc, ard_row_plan, ard_search_info, ard_search_opts,
                    ard_tile_desc, ard_tile_plan,
-                   ard_glu_desc, ard_distill_desc, ard_linattn_desc)
+                   ard_glu_desc, ard_distill_desc, ard_linattn_desc, ard_rmsnorm_desc)
 
 
 class ArdError(RuntimeError):
@@ -425,3 +425,26 @@ def ard_linattn_step(desc, Qt, Kt, Vt, log_decay, S0, Ot, ST, stream=None):
     """One token for each sequence; ST may be S0 (the state is then updated in place)."""
     _check(_ffi.lib().ard_linattn_step(ctypes.byref(desc), _ptr(Qt), _ptr(Kt), _ptr(Vt), _ptr(log_decay), _ptr(S0),
                                        _ptr(Ot), _ptr(ST), _stream(stream)))
+
+
+# --------------------------------------------------------------------------- root-mean-square norm
+
+def rmsnorm_desc(dtype, batch, features, eps=1e-5):
+    return ard_rmsnorm_desc(dtype, batch, features, eps)
+
+
+def ard_rmsnorm_workspace_bytes(desc):
+    return _ffi.lib().ard_rmsnorm_workspace_bytes(ctypes.byref(desc))
+
+
+def ard_rmsnorm_fwd(desc, Xt, Rt, gain, St, Yt, inv_rms, ws=None, stream=None):
+    """Rt None: no residual; St None: the sum is not kept."""
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_rmsnorm_fwd(ctypes.byref(desc), _ptr(Xt), _ptr(Rt), _ptr(gain), _ptr(St), _ptr(Yt),
+                                      _ptr(inv_rms), p, n, _stream(stream)))
+
+
+def ard_rmsnorm_bwd(desc, St, gain, inv_rms, dYt, dSt, dXt, dgain, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_rmsnorm_bwd(ctypes.byref(desc), _ptr(St), _ptr(gain), _ptr(inv_rms), _ptr(dYt), _ptr(dSt),
+                                      _ptr(dXt), _ptr(dgain), p, n, _stream(stream)))
