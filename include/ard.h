@@ -686,6 +686,52 @@ int ard_rmsnorm_fwd(const ard_rmsnorm_desc* desc, const void* Xt, const void* Rt
 int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* gain, const float* inv_rms,
                     const void* dYt, const void* dSt, void* dXt, float* dgain, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* Softmax cross entropy of a head layer, its logits never kept (device).   */
+/* ------------------------------------------------------------------------ */
+/*
+ * For each column x of Xt, over the classes v and the kept inputs:
+ *   z = W x + bias,  loss = log sum_v exp z_v - z_label
+ * and, with dz = (exp z / sum_v exp z_v - onehot(label)) dloss,
+ *   dX = W^T dz,  dW = dz X^T,  dbias = sum over columns of dz.
+ * Layouts: Xt, dXt [K][B], W and dW [V][K] (weight_layout ARD_WEIGHTS_FULL) or
+ * input-major [K][V] (ARD_WEIGHTS_INPUT_MAJOR: dropped inputs are then skipped
+ * rows and no compact copy is made), bias, dbias [V] and loss, dloss [B] fp32,
+ * labels[B]. in_plan is the row pattern of the inputs (the output pattern of the
+ * layer below): only kept rows of Xt and kept columns of W are read; dropped
+ * rows of dXt and columns of dW are 0 or untouched as `dropped` says.
+ * The logits exist in fp32 within a kernel only; the workspace holds dz of some
+ * of the classes at a time (rounded once to dtype, as the operand of dX and dW;
+ * dbias is summed before that). A label outside 0 .. V - 1 stands for none
+ * (padding): loss and dz are 0 there and the column of Xt, whatever it holds,
+ * reaches no gradient. Classes are masked by a bias of -inf: they have no
+ * probability and no gradient, but as a label an infinite loss, with the
+ * gradient of the formula. A column whose logits are all -inf has loss and
+ * gradient 0. NaN propagates within its column, and from there to dW.
+ * fwd: stats[2][B] (may be NULL) is kept for the backward.
+ * bwd: dloss NULL = 1; dXt, dW and dbias may be NULL. dW is of grad_dtype:
+ * ARD_F32, as ard_fc_sgd_momentum and ard_fc_muon read it, or dtype.
+ */
+typedef struct {
+  int32_t dtype;
+  int32_t batch;          /* B: 1 .. 2^22 - 8 */
+  int32_t in_features;    /* K: 1 .. 2^22 - 8 */
+  int32_t classes;        /* V >= 1; input-major: V times the period below 2^22 */
+  const ard_row_plan* in_plan;  /* n == K (a list is not needed), or NULL = every input kept */
+  int32_t weight_layout;  /* ARD_WEIGHTS_FULL or ARD_WEIGHTS_INPUT_MAJOR */
+  int32_t dropped;        /* ARD_DROPPED_ZERO or ARD_DROPPED_SKIP */
+  int32_t grad_dtype;     /* of dW: ARD_F32, or dtype */
+  int32_t reserved;
+} ard_headloss_desc;
+
+/* Workspace of fwd and bwd. */
+size_t ard_headloss_workspace_bytes(const ard_headloss_desc* desc);
+int ard_headloss_fwd(const ard_headloss_desc* desc, const void* Xt, const void* W, const float* bias,
+                     const int32_t* labels, float* loss, float* stats, void* ws, size_t ws_bytes, void* stream);
+int ard_headloss_bwd(const ard_headloss_desc* desc, const void* Xt, const void* W, const float* bias,
+                     const int32_t* labels, const float* stats, const float* dloss, void* dXt, void* dW, float* dbias,
+                     void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

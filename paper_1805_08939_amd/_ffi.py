@@ -88,6 +88,12 @@ class ard_rmsnorm_desc(ctypes.Structure):
     _fields_ = [("dtype", c_i32), ("batch", c_i32), ("features", c_i32), ("eps", c_f32)]
 
 
+class ard_headloss_desc(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("batch", c_i32), ("in_features", c_i32), ("classes", c_i32),
+                ("in_plan", ctypes.POINTER(ard_row_plan)), ("weight_layout", c_i32), ("dropped", c_i32),
+                ("grad_dtype", c_i32), ("reserved", c_i32)]
+
+
 # name -> (restype, argtypes); every symbol the header declares.
 SIGNATURES = {
     "ard_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -167,6 +173,11 @@ SIGNATURES = {
                                        c_size, c_vp]),
     "ard_rmsnorm_bwd": (ctypes.c_int, [ctypes.POINTER(ard_rmsnorm_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
                                        c_vp, c_size, c_vp]),
+    "ard_headloss_workspace_bytes": (c_size, [ctypes.POINTER(ard_headloss_desc)]),
+    "ard_headloss_fwd": (ctypes.c_int, [ctypes.POINTER(ard_headloss_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                        c_size, c_vp]),
+    "ard_headloss_bwd": (ctypes.c_int, [ctypes.POINTER(ard_headloss_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                        c_vp, c_vp, c_vp, c_size, c_vp]),
 }
 
 _lib = None

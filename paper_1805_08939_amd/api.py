@@ -16,7 +16,8 @@ from ._ffi import (ARD_ACT_NONE, ARD_ACT_RELU, ARD_BF16, ARD_DROPPED_SKIP, ARD_D
                    ARD_WEIGHTS_COMPACT, ARD_WEIGHTS_COMPACT_GRAD, ARD_WEIGHTS_FULL, ARD_WEIGHTS_INPUT_MAJOR,
                    ard_fc_desc, ard_lstm_desc, ard_lstm_tile_desc, ard_row_plan, ard_search_info, ard_search_opts,
                    ard_tile_desc, ard_tile_plan,
-                   ard_glu_desc, ard_distill_desc, ard_linattn_desc, ard_rmsnorm_desc)
+                   ard_glu_desc, ard_distill_desc, ard_linattn_desc, ard_rmsnorm_desc,
+                   ard_headloss_desc)
 
 
 class ArdError(RuntimeError):
@@ -448,3 +449,29 @@ def ard_rmsnorm_bwd(desc, St, gain, inv_rms, dYt, dSt, dXt, dgain, ws=None, stre
     p, n = _ws(ws)
     _check(_ffi.lib().ard_rmsnorm_bwd(ctypes.byref(desc), _ptr(St), _ptr(gain), _ptr(inv_rms), _ptr(dYt), _ptr(dSt),
                                       _ptr(dXt), _ptr(dgain), p, n, _stream(stream)))
+
+
+# --------------------------------------------------------------------------- cross entropy of the head
+
+def headloss_desc(dtype, batch, in_features, classes, in_plan=None, weight_layout=ARD_WEIGHTS_FULL,
+                  dropped=ARD_DROPPED_ZERO, grad_dtype=ARD_F32):
+    d = ard_headloss_desc(dtype, batch, in_features, classes, _plan_ptr(in_plan), weight_layout, dropped, grad_dtype, 0)
+    d._keep = in_plan
+    return d
+
+
+def ard_headloss_workspace_bytes(desc):
+    return _ffi.lib().ard_headloss_workspace_bytes(ctypes.byref(desc))
+
+
+def ard_headloss_fwd(desc, Xt, W, bias, labels, loss, stats, ws, stream=None):
+    """stats: 2 * batch floats, read by ard_headloss_bwd (None: not kept)."""
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_headloss_fwd(ctypes.byref(desc), _ptr(Xt), _ptr(W), _ptr(bias), _ptr(labels), _ptr(loss),
+                                       _ptr(stats), p, n, _stream(stream)))
+
+
+def ard_headloss_bwd(desc, Xt, W, bias, labels, stats, dloss, dXt, dW, dbias, ws, stream=None):
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_headloss_bwd(ctypes.byref(desc), _ptr(Xt), _ptr(W), _ptr(bias), _ptr(labels), _ptr(stats),
+                                       _ptr(dloss), _ptr(dXt), _ptr(dW), _ptr(dbias), p, n, _stream(stream)))

@@ -72,6 +72,10 @@ hipError_t product(const GemmArgs& g, hipStream_t stream, float* partial, size_t
   return run_gemm<T, OutT, A, A, B, B, false, false, EPI_STORE>(g, 1, false, false, stream, floats ? partial : nullptr);
 }
 
+// Sixteen bytes of an array of any type.
+typedef u32x4 u32x4_any __attribute__((may_alias));
+typedef u32x4 u32x4_any2 __attribute__((aligned(2), may_alias));
+
 // Sixteen bytes of a row as loaded, and its elements in fp32; rows start at any element.
 template <typename T, int VE>
 struct Chunk {
@@ -99,12 +103,11 @@ __device__ __forceinline__ void store_chunk(T* p, const float (&v)[VE], int n) {
   if constexpr (VE == 1) {
     *p = from_f32<T>(v[0]);
   } else {
-    typedef u32x4 u32x4_a2 __attribute__((aligned(2), may_alias));
     T w[VE];
 #pragma unroll
     for (int e = 0; e < VE; ++e) w[e] = from_f32<T>(v[e]);
     if (n >= VE) {
-      *reinterpret_cast<u32x4_a2*>(p) = *reinterpret_cast<const u32x4*>(w);
+      *reinterpret_cast<u32x4_any2*>(p) = *reinterpret_cast<const u32x4_any*>(w);
     } else {
 #pragma unroll
       for (int e = 0; e < VE; ++e)
