@@ -732,6 +732,44 @@ int ard_headloss_bwd(const ard_headloss_desc* desc, const void* Xt, const void* 
                      const int32_t* labels, const float* stats, const float* dloss, void* dXt, void* dW, float* dbias,
                      void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* Update of the kept weights by their orthogonalised momentum (device).    */
+/* ------------------------------------------------------------------------ */
+/*
+ * The update of ard_fc_sgd_momentum with the kept block's momentum replaced by
+ * the nearly orthogonal matrix of the same singular vectors. Over the kept
+ * output rows and input columns of the layer's patterns:
+ *   V = momentum V + dW,  U = dW + momentum V (nesterov) or V,
+ *   X = U / (|U| + eps)  (Frobenius norm), then `iterations` times
+ *   X = (a + b A + c A^2) X with A = X X^T,
+ *   W = (1 - lr weight_decay) W - lr sqrt(max(1, kept outputs / kept inputs)) X
+ * Each iteration maps the singular values s to a s + b s^3 + c s^5: with the
+ * defaults those above a few thousandths end between 0.7 and 1.2 after five.
+ * The kept biases take momentum SGD with bias_lr: Vb = momentum Vb + dbias,
+ * bias -= bias_lr Vb. What is dropped is frozen for the step. W, V and dW as
+ * ard_fc_sgd_momentum takes them (FULL, COMPACT and COMPACT_GRAD: dW[N][K] or
+ * compact; INPUT_MAJOR), each aligned to its elements; bias, Vb and dbias all
+ * given or all NULL. batch, scale, act and dropped of the descriptor are not
+ * used. V is fp32; a gradient that is not finite makes the whole block so.
+ */
+typedef struct {
+  float lr;            /* 0.02 */
+  float momentum;      /* 0.95 */
+  float weight_decay;  /* 0 */
+  float bias_lr;       /* 0.02 */
+  float eps;           /* > 0; 1e-7 */
+  float a, b, c;       /* 3.4445, -4.7750, 2.0315 */
+  int32_t iterations;  /* 1 .. 64; 5 */
+  int32_t nesterov;    /* 1 */
+} ard_muon_opts;
+
+/* The defaults above. */
+void ard_muon_opts_default(ard_muon_opts* opts);
+size_t ard_fc_muon_workspace_bytes(const ard_fc_desc* desc);
+/* opts NULL = defaults. */
+int ard_fc_muon(const ard_fc_desc* desc, const ard_muon_opts* opts, void* W, float* V, const float* dW, float* bias,
+                float* Vb, const float* dbias, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -94,6 +94,11 @@ class ard_headloss_desc(ctypes.Structure):
                 ("grad_dtype", c_i32), ("reserved", c_i32)]
 
 
+class ard_muon_opts(ctypes.Structure):
+    _fields_ = [("lr", c_f32), ("momentum", c_f32), ("weight_decay", c_f32), ("bias_lr", c_f32), ("eps", c_f32),
+                ("a", c_f32), ("b", c_f32), ("c", c_f32), ("iterations", c_i32), ("nesterov", c_i32)]
+
+
 # name -> (restype, argtypes); every symbol the header declares.
 SIGNATURES = {
     "ard_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -178,6 +183,10 @@ SIGNATURES = {
                                         c_size, c_vp]),
     "ard_headloss_bwd": (ctypes.c_int, [ctypes.POINTER(ard_headloss_desc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
                                         c_vp, c_vp, c_vp, c_size, c_vp]),
+    "ard_muon_opts_default": (None, [ctypes.POINTER(ard_muon_opts)]),
+    "ard_fc_muon_workspace_bytes": (c_size, [ctypes.POINTER(ard_fc_desc)]),
+    "ard_fc_muon": (ctypes.c_int, [ctypes.POINTER(ard_fc_desc), ctypes.POINTER(ard_muon_opts), c_vp, c_vp, c_vp, c_vp,
+                                   c_vp, c_vp, c_vp, c_size, c_vp]),
 }
 
 _lib = None

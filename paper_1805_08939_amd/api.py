@@ -17,7 +17,7 @@ from ._ffi import (ARD_ACT_NONE, ARD_ACT_RELU, ARD_BF16, ARD_DROPPED_SKIP, ARD_D
                    ard_fc_desc, ard_lstm_desc, ard_lstm_tile_desc, ard_row_plan, ard_search_info, ard_search_opts,
                    ard_tile_desc, ard_tile_plan,
                    ard_glu_desc, ard_distill_desc, ard_linattn_desc, ard_rmsnorm_desc,
-                   ard_headloss_desc)
+                   ard_headloss_desc, ard_muon_opts)
 
 
 class ArdError(RuntimeError):
@@ -475,3 +475,22 @@ def ard_headloss_bwd(desc, Xt, W, bias, labels, stats, dloss, dXt, dW, dbias, ws
     p, n = _ws(ws)
     _check(_ffi.lib().ard_headloss_bwd(ctypes.byref(desc), _ptr(Xt), _ptr(W), _ptr(bias), _ptr(labels), _ptr(stats),
                                        _ptr(dloss), _ptr(dXt), _ptr(dW), _ptr(dbias), p, n, _stream(stream)))
+
+
+# --------------------------------------------------------------------------- orthogonalised momentum
+
+def ard_muon_opts_default():
+    o = ard_muon_opts()
+    _ffi.lib().ard_muon_opts_default(ctypes.byref(o))
+    return o
+
+
+def ard_fc_muon_workspace_bytes(desc):
+    return _ffi.lib().ard_fc_muon_workspace_bytes(ctypes.byref(desc))
+
+
+def ard_fc_muon(desc, opts, W, V, dW, bias=None, Vb=None, dbias=None, ws=None, stream=None):
+    """Updates the kept weights by their orthogonalised momentum (opts None: the defaults) and the kept biases by momentum SGD."""
+    p, n = _ws(ws)
+    _check(_ffi.lib().ard_fc_muon(ctypes.byref(desc), None if opts is None else ctypes.byref(opts), _ptr(W), _ptr(V),
+                                  _ptr(dW), _ptr(bias), _ptr(Vb), _ptr(dbias), p, n, _stream(stream)))

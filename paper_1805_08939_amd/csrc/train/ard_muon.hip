@@ -1,0 +1,258 @@
+// Momentum update of a layer's kept weights by the orthogonalised momentum:
+//   V = mu V + dW,  U = dW + mu V (Nesterov) or V,  X = U / (|U| + eps)
+//   iterations times, with A = X X^T (or X^T X, whichever is smaller):
+//     X = (a + b A + c A^2) X
+//   W = (1 - lr decay) W - lr sqrt(max(1, outputs / inputs)) X
+// Each iteration applies the odd polynomial a s + b s^3 + c s^5 to the singular values of X
+// and leaves its singular vectors; |U| is the Frobenius norm, so that they start within 1.
+//
+// The kept block is gathered once, into a dense matrix. A and A^2 are symmetric, the third
+// product has the shape of the block. Bound by the matrix cores, for small blocks by the
+// latency of three products after one another.
+
+#include "ard_train.hpp"
+
+namespace ard {
+namespace {
+
+// The kept block as it is stored: rows row_offset + row_period * i of W and V (rows of ld
+// elements), columns likewise; the gradient in the same places or (ldg > 0) dense.
+struct Block {
+  int32_t R, C;                       // kept rows and columns
+  int32_t row_period, row_offset, col_period, col_offset;
+  int64_t ld, ldg;
+  int64_t ldx;                        // rows of the dense copies
+};
+__device__ __forceinline__ int64_t place(const Block& b, int64_t i, int64_t j) {
+  return (b.row_offset + i * b.row_period) * b.ld + b.col_offset + j * b.col_period;
+}
+
+constexpr int kNormBlocks = 1024;  // workgroups of the first pass, at most: one sum of squares each
+
+// V and U, and the sum of U's squares of each workgroup, in 64 bits (momenta far below 1
+// have squares below the smallest fp32 number).
+__global__ void __launch_bounds__(256) muon_momentum_kernel(Block b, float* __restrict__ V, const float* __restrict__ dW,
+                                                            float mu, bool nesterov, float* __restrict__ U,
+                                                            double* __restrict__ sums) {
+  double sum = 0.0;
+  for (int64_t i = blockIdx.x; i < b.R; i += gridDim.x)
+    for (int64_t j = threadIdx.x; j < b.C; j += 256) {
+      const int64_t at = place(b, i, j);
+      const float g = b.ldg > 0 ? dW[i * b.ldg + j] : dW[at];
+      const float v = mu * V[at] + g, u = nesterov ? g + mu * v : v;
+      V[at] = v;
+      U[i * b.ldx + j] = u;
+      sum += static_cast<double>(u) * u;
+    }
+  __shared__ double red[4];
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_down(sum, o);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) sums[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// 1 / (|U| + eps) from the workgroups' sums, in their order; every thread has it.
+__device__ __forceinline__ double inverse_norm(const double* sums, int blocks, float eps) {
+  __shared__ double red[256];
+  double v = 0.0;
+  for (int q = threadIdx.x; q < blocks; q += 256) v += sums[q];
+  red[threadIdx.x] = v;
+  __syncthreads();
+  for (int o = 128; o > 0; o >>= 1) {
+    if (static_cast<int>(threadIdx.x) < o) red[threadIdx.x] += red[threadIdx.x + o];
+    __syncthreads();
+  }
+  return 1.0 / (sqrt(red[0]) + static_cast<double>(eps));
+}
+
+// X = U / (|U| + eps), in place.
+__global__ void __launch_bounds__(256) muon_scale_kernel(Block b, float* __restrict__ X, const double* __restrict__ sums,
+                                                         int blocks, float eps) {
+  const double inv = inverse_norm(sums, blocks, eps);
+  for (int64_t i = blockIdx.x; i < b.R; i += gridDim.x)
+    for (int64_t j = threadIdx.x; j < b.C; j += 256) X[i * b.ldx + j] = static_cast<float>(X[i * b.ldx + j] * inv);
+}
+
+// P = a + b A + c S, into S.
+__global__ void __launch_bounds__(256) muon_poly_kernel(int32_t m, int64_t lda, const float* __restrict__ A,
+                                                        float* __restrict__ S, float a, float b, float c) {
+  for (int64_t i = blockIdx.x; i < m; i += gridDim.x)
+    for (int64_t j = threadIdx.x; j < m; j += 256) {
+      const int64_t at = i * lda + j;
+      S[at] = c * S[at] + b * A[at] + (i == j ? a : 0.0f);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) muon_update_kernel(Block b, const float* __restrict__ X, T* __restrict__ W, float keep,
+                                                          float step) {
+  for (int64_t i = blockIdx.x; i < b.R; i += gridDim.x)
+    for (int64_t j = threadIdx.x; j < b.C; j += 256) {
+      const int64_t at = place(b, i, j);
+      W[at] = from_f32<T>(keep * to_f32(W[at]) - step * X[i * b.ldx + j]);
+    }
+}
+
+// Momentum SGD of the kept outputs' bias.
+__global__ void __launch_bounds__(256) muon_bias_kernel(Kept out, float* __restrict__ bias, float* __restrict__ Vb,
+                                                        const float* __restrict__ db, float lr, float mu) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= out.kept) return;
+  const int64_t n = out.offset + i * out.period;
+  const float v = mu * Vb[n] + db[n];
+  Vb[n] = v;
+  bias[n] -= lr * v;
+}
+
+// ------------------------------------------------------------------ host
+struct MuonShape {
+  Block b;
+  Kept out;
+  int32_t m, l;   // smaller and larger side
+  int64_t lda;
+  double stretch;  // sqrt(max(1, kept outputs / kept inputs))
+};
+
+int check_desc(const ard_fc_desc* d, MuonShape* s) {
+  if (!d) return fail(ARD_ERR_INVALID_ARG, "desc is NULL");
+  if (d->dtype != ARD_F32 && d->dtype != ARD_BF16) return fail(ARD_ERR_UNSUPPORTED, "dtype %d not supported", d->dtype);
+  if (d->in_features < 1 || d->out_features < 1)
+    return fail(ARD_ERR_INVALID_ARG, "sizes must be >= 1 (in %d, out %d)", d->in_features, d->out_features);
+  if (d->weight_layout < ARD_WEIGHTS_FULL || d->weight_layout > ARD_WEIGHTS_INPUT_MAJOR)
+    return fail(ARD_ERR_INVALID_ARG, "unknown weight layout %d", d->weight_layout);
+  int st = check_row_plan(d->in_plan, d->in_features, "in_plan", false);
+  if (st != ARD_OK) return st;
+  st = check_row_plan(d->out_plan, d->out_features, "out_plan", false);
+  if (st != ARD_OK) return st;
+  const Kept in = kept_of(d->in_plan, d->in_features), out = kept_of(d->out_plan, d->out_features);
+  const bool input_major = d->weight_layout == ARD_WEIGHTS_INPUT_MAJOR;
+  if (input_major && out.period != 1)
+    return fail(ARD_ERR_UNSUPPORTED, "input-major weights need every output kept (out_plan NULL or period 1)");
+  const Kept &r = input_major ? in : out, &c = input_major ? out : in;
+  s->b = {r.kept, c.kept, r.period, r.offset, c.period, c.offset, c.n,
+          d->weight_layout == ARD_WEIGHTS_COMPACT_GRAD ? up8(c.kept) : 0, up8(c.kept)};
+  s->out = out;
+  s->m = std::min(r.kept, c.kept);
+  s->l = std::max(r.kept, c.kept);
+  s->lda = up8(s->m);
+  s->stretch = in.kept > 0 ? std::sqrt(std::max(1.0, static_cast<double>(out.kept) / in.kept)) : 1.0;
+  return ARD_OK;
+}
+
+int check_opts(const ard_muon_opts* o) {
+  const float all[] = {o->lr, o->momentum, o->weight_decay, o->bias_lr, o->eps, o->a, o->b, o->c};
+  for (float x : all)
+    if (!std::isfinite(x)) return fail(ARD_ERR_INVALID_ARG, "every option must be finite");
+  if (!(o->eps > 0.0f)) return fail(ARD_ERR_INVALID_ARG, "eps must be > 0");
+  if (o->iterations < 1 || o->iterations > 64)
+    return fail(ARD_ERR_INVALID_ARG, "iterations %d: 1 to 64", o->iterations);
+  return ARD_OK;
+}
+
+struct Space {
+  size_t x, a, sums, part;
+  size_t bytes() const { return 2 * x + 2 * a + sums + part; }
+};
+Space space_of(const MuonShape& s) {
+  if (s.m == 0) return {0, 0, 0, 0};
+  const size_t part = std::max({partial_floats<float>(s.m, s.m, s.l), partial_floats<float>(s.m, s.m, s.m),
+                                partial_floats<float>(s.b.R, s.b.C, s.m)});
+  return {al256(static_cast<size_t>(s.b.R) * s.b.ldx * 4), al256(static_cast<size_t>(s.m) * s.lda * 4), kNormBlocks * 8,
+          al256(4 * part)};
+}
+
+template <typename T>
+int muon_impl(const MuonShape& s, const ard_muon_opts& o, void* W, float* V, const float* dW, char* ws, hipStream_t stream) {
+  const Space sp = space_of(s);
+  const Block& b = s.b;
+  float *X = reinterpret_cast<float*>(ws), *Y = reinterpret_cast<float*>(ws + sp.x);
+  float *A = reinterpret_cast<float*>(ws + 2 * sp.x), *S = reinterpret_cast<float*>(ws + 2 * sp.x + sp.a);
+  double* sums = reinterpret_cast<double*>(ws + 2 * sp.x + 2 * sp.a);
+  float* part = reinterpret_cast<float*>(ws + 2 * sp.x + 2 * sp.a + sp.sums);
+  const unsigned rows = static_cast<unsigned>(std::min(b.R, kNormBlocks));
+  hipLaunchKernelGGL(muon_momentum_kernel, dim3(rows), dim3(256), 0, stream, b, V, dW, o.momentum, o.nesterov != 0, X, sums);
+  ARD_LAUNCH_CHECK();
+  hipLaunchKernelGGL(muon_scale_kernel, dim3(rows), dim3(256), 0, stream, b, X, sums, static_cast<int>(rows), o.eps);
+  ARD_LAUNCH_CHECK();
+  for (int it = 0; it < o.iterations; ++it) {
+    GemmArgs g = {};
+    g.M = g.N = s.m, g.K = s.l;
+    g.a = g.b = view(X, b.ldx);
+    g.c.p = A, g.c.ld = s.lda;
+    ARD_HIP_CHECK((b.R <= b.C ? product<float, false, false, float>(g, stream, part, sp.part / 4)
+                              : product<float, true, true, float>(g, stream, part, sp.part / 4)));
+    g = {};
+    g.M = g.N = g.K = s.m;
+    g.a = g.b = view(A, s.lda);  // A is its own transpose
+    g.c.p = S, g.c.ld = s.lda;
+    ARD_HIP_CHECK((product<float, false, false, float>(g, stream, part, sp.part / 4)));
+    hipLaunchKernelGGL(muon_poly_kernel, dim3(static_cast<unsigned>(std::min(s.m, 4096))), dim3(256), 0, stream, s.m, s.lda, A, S,
+                       o.a, o.b, o.c);
+    ARD_LAUNCH_CHECK();
+    g = {};
+    g.M = b.R, g.N = b.C, g.K = s.m;
+    g.c.p = Y, g.c.ld = b.ldx;
+    if (b.R <= b.C) {
+      g.a = view(S, s.lda), g.b = view(X, b.ldx);
+      ARD_HIP_CHECK((product<float, false, true, float>(g, stream, part, sp.part / 4)));
+    } else {
+      g.a = view(X, b.ldx), g.b = view(S, s.lda);
+      ARD_HIP_CHECK((product<float, false, false, float>(g, stream, part, sp.part / 4)));
+    }
+    std::swap(X, Y);
+  }
+  hipLaunchKernelGGL(muon_update_kernel<T>, dim3(rows), dim3(256), 0, stream, b, X, static_cast<T*>(W),
+                     static_cast<float>(1.0 - static_cast<double>(o.lr) * o.weight_decay),
+                     static_cast<float>(o.lr * s.stretch));
+  ARD_LAUNCH_CHECK();
+  return ARD_OK;
+}
+
+}  // namespace
+}  // namespace ard
+
+using namespace ard;
+
+extern "C" {
+
+void ard_muon_opts_default(ard_muon_opts* opts) {
+  if (!opts) return;
+  *opts = ard_muon_opts{0.02f, 0.95f, 0.0f, 0.02f, 1e-7f, 3.4445f, -4.7750f, 2.0315f, 5, 1};
+}
+
+size_t ard_fc_muon_workspace_bytes(const ard_fc_desc* desc) {
+  MuonShape s;
+  if (check_desc(desc, &s) != ARD_OK) return 0;
+  return space_of(s).bytes();
+}
+
+int ard_fc_muon(const ard_fc_desc* desc, const ard_muon_opts* opts, void* W, float* V, const float* dW, float* bias, float* Vb,
+                const float* dbias, void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  MuonShape s;
+  int st = check_desc(desc, &s);
+  if (st != ARD_OK) return st;
+  ard_muon_opts o;
+  ard_muon_opts_default(&o);
+  if (opts) o = *opts;
+  if ((st = check_opts(&o)) != ARD_OK) return st;
+  if (!W || !V || !dW) return fail(ARD_ERR_INVALID_ARG, "W, V or dW is NULL");
+  if ((bias == nullptr) != (Vb == nullptr) || (bias == nullptr) != (dbias == nullptr))
+    return fail(ARD_ERR_INVALID_ARG, "bias, Vb and dbias must be all given or all NULL");
+  if (reinterpret_cast<uintptr_t>(W) % (desc->dtype == ARD_BF16 ? 2 : 4) || reinterpret_cast<uintptr_t>(V) % 4 ||
+      reinterpret_cast<uintptr_t>(dW) % 4 || reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(Vb) % 4 ||
+      reinterpret_cast<uintptr_t>(dbias) % 4)
+    return fail(ARD_ERR_INVALID_ARG, "W, V, dW or the bias is not aligned to its element size");
+  if ((st = check_space(space_of(s).bytes(), ws, ws_bytes)) != ARD_OK) return st;
+  hipStream_t sm = static_cast<hipStream_t>(stream);
+  if (bias && s.out.kept > 0) {
+    hipLaunchKernelGGL(muon_bias_kernel, dim3((s.out.kept + 255) / 256), dim3(256), 0, sm, s.out, bias, Vb, dbias, o.bias_lr,
+                       o.momentum);
+    ARD_LAUNCH_CHECK();
+  }
+  if (s.m == 0) return ARD_OK;
+  char* w = static_cast<char*>(ws);
+  return desc->dtype == ARD_BF16 ? muon_impl<bf16>(s, o, W, V, dW, w, sm) : muon_impl<float>(s, o, W, V, dW, w, sm);
+}
+
+}  // extern "C"

@@ -1,0 +1,318 @@
+"""The orthogonalised momentum update: the oracle against its singular values (CPU), refusals (CPU), and the kernels
+against the definition in 64 bits (GPU).
+
+Tolerances, with u = 2^-24: one iteration's products are sums of n terms, off by at most n u of the sum of their absolute
+values; for bf16 weights an operand is kept to 2^-16 (two bf16 parts), and products of two second parts, 2^-16, are left
+out. Over several iterations errors are followed in the Frobenius norm: an iteration maps singular values by the
+polynomial p, and a difference of matrices by at most the largest divided difference of p over the range of the singular
+values, which is below max |p'| there: p' = a + 3 b s^2 + 5 c s^4 is 3.45 at 0, -1.61 at its least and, since p has its largest
+value 1.2024 at s = 0.5545, 3.97 at the end of the range: below 4.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import muon as omuon
+from paper_1805_08939_amd import api, synth
+
+U, UBF = 2.0 ** -24, 2.0 ** -8
+A, B, C = omuon.COEFFS
+FULL, COMPACT, INPUT = api.ARD_WEIGHTS_FULL, api.ARD_WEIGHTS_COMPACT_GRAD, api.ARD_WEIGHTS_INPUT_MAJOR
+
+
+# ---------------------------------------------------------------- the oracle
+
+def test_oracle_maps_singular_values():
+    r = np.random.default_rng(8)
+    G = r.normal(size=(5, 9))
+    u, s, vt = np.linalg.svd(G, full_matrices=False)
+    s = s / np.sqrt((s * s).sum())
+    for _ in range(5):
+        s = A * s + B * s ** 3 + C * s ** 5
+    assert s.min() > 0.6 and s.max() < 1.25
+    for M, want in ((G, (u * s) @ vt), (G.T, ((u * s) @ vt).T)):
+        assert np.abs(omuon.polynomial(M, 0.0, 5)[-1] - want).max() < 1e-12
+    W, V = omuon.update(np.zeros((9, 5)), np.zeros((9, 5)), G.T, 1.0, 0.9, 0.0, False, 0.0, 5)
+    assert np.abs(W + np.sqrt(9 / 5) * ((u * s) @ vt).T).max() < 1e-12 and np.array_equal(V, G.T)
+
+
+def test_divided_differences_are_below_the_bound():
+    s = np.linspace(1e-6, 1.2025, 1500)
+    p = A * s + B * s ** 3 + C * s ** 5
+    assert p.max() < 1.2025 and p.min() > 0
+    d = np.abs(p[:, None] - p[None]) / np.where(s[:, None] == s[None], np.inf, np.abs(s[:, None] - s[None]))
+    t = (p[:, None] + p[None]) / (s[:, None] + s[None])
+    assert max(d.max(), t.max()) < 4.0 and np.abs(A + 3 * B * s ** 2 + 5 * C * s ** 4).max() < 4.0
+
+
+# ---------------------------------------------------------------- refusals
+
+def test_refuses_bad_calls():
+    a = 4096  # an aligned address; never read
+
+    def refused(status, *args):
+        with pytest.raises(api.ArdError) as e:
+            api.ard_fc_muon(*args, stream=0)
+        assert e.value.status == status and e.value.message
+
+    space = (a, 1 << 40)
+    desc = lambda **k: api.fc_desc(**{**dict(dtype=api.ARD_F32, batch=1, in_features=8, out_features=6), **k})  # noqa: E731
+    for bad, status in ((dict(dtype=4), 2), (dict(in_features=0), 1), (dict(out_features=-1), 1), (dict(weight_layout=4), 1),
+                        (dict(weight_layout=-1), 1), (dict(in_plan=api.ard_plan_rows(7, 2, 0, None)), 1),
+                        (dict(out_plan=api.ard_plan_rows(8, 2, 0, None)), 1),
+                        (dict(out_plan=api.ard_plan_rows(6, 2, 0, None), weight_layout=INPUT), 2)):
+        d = desc(**bad)
+        assert api.ard_fc_muon_workspace_bytes(d) == 0
+        refused(status, d, None, a, a, a, None, None, None, space)
+    d = desc()
+    assert api.ard_fc_muon_workspace_bytes(d) > 0
+    for field, x in (("lr", float("nan")), ("momentum", float("inf")), ("weight_decay", float("nan")), ("bias_lr", float("nan")),
+                     ("eps", 0.0), ("eps", -1.0), ("a", float("nan")), ("b", float("inf")), ("c", float("nan")),
+                     ("iterations", 0), ("iterations", 65)):
+        o = api.ard_muon_opts_default()
+        setattr(o, field, x)
+        refused(1, d, o, a, a, a, None, None, None, space)
+    for args in ((None, a, a), (a, None, a), (a, a, None), (a + 2, a, a), (a, a + 2, a), (a, a, a + 1)):
+        refused(1, d, None, *args, None, None, None, space)
+    for args in ((a, None, None), (a, a, None), (None, a, a), (a + 2, a, a), (a, a + 1, a), (a, a, a + 2)):
+        refused(1, d, None, a, a, a, *args, space)
+    refused(5, d, None, a, a, a, None, None, None, None)
+    refused(5, d, None, a, a, a, None, None, None, (a, 64))
+    refused(1, d, None, a, a, a, None, None, None, (a + 4, 1 << 40))
+
+
+def test_defaults():
+    o = api.ard_muon_opts_default()
+    assert (o.iterations, o.nesterov) == (5, 1)
+    assert np.allclose([o.a, o.b, o.c], omuon.COEFFS) and o.momentum == np.float32(0.95)
+
+
+# ---------------------------------------------------------------- the kernels
+
+def _local_error(X, part):
+    """What one iteration on X (rows no more than columns) may add, value by value; part: what an operand is kept to."""
+    n, k = X.shape
+    Xa = X.abs()
+    A_, Aa = X @ X.T, Xa @ Xa.T
+    eA = ((k + 4) * U + 3 * part) * Aa + part * A_.abs()
+    eS = ((n + 4) * U + 3 * part) * (A_.abs() @ A_.abs()) + 2 * (A_.abs() @ eA)
+    S = A_ @ A_
+    P = C * S + B * A_ + A * torch.eye(n, dtype=X.dtype, device=X.device)
+    eP = abs(C) * eS + abs(B) * eA + (4 * U + part) * (abs(C) * S.abs() + abs(B) * A_.abs() + A * torch.eye(n, dtype=X.dtype, device=X.device))
+    return P @ X, eP @ Xa + ((n + 4) * U + 4 * part) * (P.abs() @ Xa)
+
+
+def _check(got, W0, V0, G, o, dtype, ratio):
+    """Kept block of W after the update against the definition; all in 64 bits, rows are outputs."""
+    V = o.momentum * V0 + G
+    Um = G + o.momentum * V if o.nesterov else V
+    step, keep = o.lr * max(1.0, ratio) ** 0.5, 1.0 - o.lr * o.weight_decay
+    X = Um / (Um.square().sum().sqrt() + o.eps)
+    wide = X.shape[0] <= X.shape[1]
+    X = X if wide else X.T
+    part = 2.0 ** -16 if dtype == "bf16" else 0.0
+    size = (o.momentum * V0).abs() + G.abs() * 2 + (o.momentum * V).abs()
+    e0 = ((size if wide else size.T) * 4 * U) / (Um.square().sum().sqrt() + o.eps) + (4 * U + part) * X.abs()
+    off, value = float(e0.norm()), None
+    for it in range(o.iterations):
+        X, e = _local_error(X, part)
+        if it == 0 and o.iterations == 1:
+            Z = X if wide else X.T
+            # one iteration value by value; the error of its start within the norm's bound
+            value = (e if wide else e.T) + 4.0 * off
+        off = 4.0 * off + float(e.norm())
+    X = X if wide else X.T
+    want = keep * W0 - step * X
+    rounding = (UBF if dtype == "bf16" else U) * want.abs() + 3 * U * (W0.abs() + step * X.abs())
+    assert torch.isfinite(got).all()
+    miss = (got - want).abs()
+    if value is not None:
+        assert (miss <= rounding * (1 + UBF) + step * value).all()
+    assert float(miss.norm()) <= float(rounding.norm()) * (1 + UBF) + step * off, (float(miss.norm()), float(rounding.norm()), step * off)
+    return float(miss.norm()), float(X.norm()) * step, off / float(X.norm())
+
+
+SIZES = [  # dtype, outputs, inputs, out period, offset, in period, offset, layout
+    ("f32", 1, 1, 1, 0, 1, 0, FULL), ("bf16", 1, 7, 1, 0, 1, 0, FULL), ("f32", 9, 1, 1, 0, 1, 0, FULL), ("f32", 6, 6, 1, 0, 1, 0, FULL),
+    ("bf16", 33, 40, 1, 0, 1, 0, FULL), ("f32", 100, 63, 3, 1, 2, 1, FULL), ("bf16", 100, 63, 3, 1, 2, 1, COMPACT),
+    ("f32", 65, 129, 1, 0, 2, 0, COMPACT), ("bf16", 64, 200, 1, 0, 3, 2, INPUT), ("f32", 200, 64, 1, 0, 3, 2, INPUT),
+    ("f32", 256, 256, 1, 0, 1, 0, FULL), ("bf16", 256, 256, 1, 0, 1, 0, FULL), ("bf16", 300, 520, 2, 1, 1, 0, FULL),
+    ("f32", 512, 784, 1, 0, 1, 0, FULL), ("bf16", 784, 512, 1, 0, 1, 0, FULL), ("bf16", 1537, 1023, 3, 2, 1, 0, FULL),
+    ("f32", 1025, 333, 1, 0, 1, 0, FULL), ("bf16", 1100, 2048, 2, 0, 2, 1, COMPACT), ("bf16", 1024, 1024, 1, 0, 1, 0, INPUT),
+    ("bf16", 2047, 700, 1, 0, 1, 0, FULL), ("f32", 700, 2047, 1, 0, 1, 0, INPUT), ("bf16", 40, 3001, 1, 0, 1, 0, FULL),
+    ("f32", 3001, 40, 1, 0, 1, 0, FULL), ("bf16", 4100, 130, 1, 0, 1, 0, FULL), ("bf16", 2300, 2400, 1, 0, 1, 0, FULL),
+    ("f32", 1600, 1700, 1, 0, 1, 0, FULL), ("bf16", 5000, 1030, 1, 0, 1, 0, FULL), ("bf16", 8, 8, 4, 3, 4, 3, FULL),
+]
+
+
+def _setup(dtype, outs, ins, op, oo, ip, io, layout, seed=0, scale=1e-3):
+    from gpu_util import ard_dtype, device
+    dev = device()
+    gen = torch.Generator(device=dev).manual_seed(seed + outs + 7 * ins)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=dev)  # noqa: E731
+
+    def gradient():  # a few strong directions above noise
+        r = max(1, min(outs, ins) // 16)
+        return (rand(outs, r) @ rand(r, ins) / r ** 0.5 + 0.3 * rand(outs, ins)) * scale
+
+    W, V, G, b = (rand(outs, ins) / ins ** 0.5).to(synth.storage_dtype(dtype)), gradient() * 10, gradient(), rand(outs)
+    iplan, oplan = api.ard_plan_rows(ins, ip, io, None), api.ard_plan_rows(outs, op, oo, None)
+    desc = api.fc_desc(ard_dtype(dtype), 1, ins, outs, iplan, oplan, weight_layout=layout)
+    rows, cols = slice(oo, None, op), slice(io, None, ip)
+    if layout == COMPACT:
+        kept = G[rows, cols]
+        dense = torch.full((kept.shape[0], (kept.shape[1] + 7) // 8 * 8), float("nan"), device=dev)
+        dense[:, :kept.shape[1]] = kept
+        stored = [W, V, dense]
+    else:
+        drop = torch.ones_like(G, dtype=torch.bool)
+        drop[rows, cols] = False
+        G[drop] = float("nan")
+        stored = [W, V, G]
+    if layout == INPUT:
+        stored = [t.T for t in stored]
+    return desc, [t.contiguous() for t in stored], W, V, G, b, (rows, cols)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("iterations,nesterov", [(1, 0), (5, 1)])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "-".join(map(str, s)))
+def test_update(size, iterations, nesterov):
+    from gpu_util import workspace
+    dtype, outs, ins, layout = size[0], size[1], size[2], size[7]
+    desc, (Wd, Vd, Gd), W, V, G, b, kept = _setup(*size)
+    o = api.ard_muon_opts_default()
+    o.iterations, o.nesterov, o.lr, o.weight_decay, o.momentum, o.bias_lr = iterations, nesterov, 0.05, 0.1, 0.9, 0.3
+    zero = iterations == 5 and outs % 2 == 0  # from no weights: the update alone
+    if zero:
+        Wd.zero_()
+        W = torch.zeros_like(W)
+    ws = workspace(api.ard_fc_muon_workspace_bytes(desc))
+    ws.fill_(float("nan"))
+    bias, Vb, db = b.clone(), b * 2, b * 3
+    given = Gd.clone()
+    W_, V_ = Wd.clone(), Vd.clone()
+    api.ard_fc_muon(desc, o, W_, V_, Gd, bias, Vb, db, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(given.view(torch.int32), Gd.view(torch.int32))
+    if layout == INPUT:
+        W_, V_ = W_.T, V_.T
+    W64, V64, G64 = W[kept].double(), V[kept].double(), G[kept].double()
+    mu = float(o.momentum)
+    newV = mu * V64 + G64
+    assert ((V_[kept].double() - newV).abs() <= 2 * U * ((mu * V64).abs() + G64.abs())).all()
+    drop = torch.ones_like(W, dtype=torch.bool)
+    drop[kept] = False
+    assert torch.equal(W_[drop], W[drop]) and torch.equal(V_[drop], V[drop])
+    _check(W_[kept].double(), W64, V64, G64, o, dtype, W64.shape[0] / W64.shape[1])
+    on = torch.zeros(outs, dtype=torch.bool, device=W.device)
+    on[kept[0]] = True
+    nv = mu * 2 * b.double() + 3 * b.double()
+    assert ((Vb.double() - torch.where(on, nv, 2 * b.double())).abs() <= 4 * U * nv.abs()).all()
+    nb = b.double() - float(o.bias_lr) * nv
+    assert ((bias.double() - torch.where(on, nb, b.double())).abs() <= 6 * U * (b.double().abs() + nv.abs())).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_singular_values_of_the_update(dtype):
+    """From no weights and lr 1 the new weights are the negated block: its singular values are near one, and those of
+    directions that the gradient does not have are near none."""
+    from gpu_util import device, workspace
+    dev = device()
+    n, k, r = 192, 320, 100
+    gen = torch.Generator(device=dev).manual_seed(3)
+    G = torch.randn(n, r, generator=gen, device=dev) @ torch.randn(r, k, generator=gen, device=dev)
+    W, V = torch.zeros(n, k, dtype=synth.storage_dtype(dtype), device=dev), torch.zeros(n, k, device=dev)
+    desc = api.fc_desc(api.ARD_BF16 if dtype == "bf16" else api.ARD_F32, 1, k, n)
+    o = api.ard_muon_opts_default()
+    o.lr = 1.0
+    api.ard_fc_muon(desc, o, W, V, G, None, None, None, workspace(api.ard_fc_muon_workspace_bytes(desc)))
+    s = torch.linalg.svdvals(W.double())
+    # 3.4445^5 = 485 times the noise of an operand over 192 directions, and the output's rounding
+    noise = (485 * 2.0 ** -16 + UBF) * 2 if dtype == "bf16" else 485 * 2 * U * 20
+    assert s[0] < 1.25 and s[r - 1] > 0.6 and s[r] < noise, (s[0], s[r - 1], s[r], noise)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_at_the_ends_of_the_range(dtype):
+    """No gradient leaves the decay alone; the size of a gradient does not matter; one that is not finite stays within the
+    kept block."""
+    from gpu_util import workspace
+    size = (dtype, 90, 70, 2, 1, 1, 0, FULL)
+    results = []
+    for scale in (1.0, 2.0 ** 90, 2.0 ** -60):
+        desc, (W, V, G), W0, *_, kept = _setup(*size, scale=1.0)
+        ws = workspace(api.ard_fc_muon_workspace_bytes(desc))
+        o = api.ard_muon_opts_default()
+        o.eps = 1e-30
+        V.mul_(scale), G.mul_(scale)
+        api.ard_fc_muon(desc, o, W, V, G, None, None, None, ws)
+        results.append(W.clone())
+    assert torch.isfinite(results[0]).all()
+    assert torch.equal(results[0], results[1]) and torch.equal(results[0], results[2])
+    desc, (W, V, G), W0, *_, kept = _setup(*size)
+    o = api.ard_muon_opts_default()
+    o.lr, o.weight_decay = 0.5, 0.25
+    V.zero_(), G.zero_()
+    before = W.clone()
+    api.ard_fc_muon(desc, o, W, V, G, None, None, None, ws)
+    assert torch.equal(W[kept], (before[kept].float() * 0.875).to(W.dtype)) and (V == 0).all()
+    G[kept[0].start, 3] = float("inf")
+    before = W.clone()
+    api.ard_fc_muon(desc, o, W, V, G, None, None, None, ws)
+    drop = torch.ones_like(W, dtype=torch.bool)
+    drop[kept] = False
+    assert torch.isnan(W[kept]).all() and torch.equal(W[drop], before[drop])
+    # nothing kept: the call does nothing
+    desc = api.fc_desc(api.ARD_F32, 1, 4, 3, None, api.ard_plan_rows(3, 8, 7, None))
+    w = torch.ones(3, 4, device=W.device)
+    api.ard_fc_muon(desc, None, w, w, w, None, None, None, None)
+    assert (w == 1).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [("bf16", 300, 520, 2, 1, 1, 0, FULL), ("f32", 512, 300, 1, 0, 1, 0, FULL)])
+def test_captured_and_on_another_stream(size):
+    from gpu_util import workspace
+    desc, (W, V, G), *_ = _setup(*size)
+    nbytes = api.ard_fc_muon_workspace_bytes(desc)
+    ws, ws2 = workspace(nbytes), workspace(nbytes)
+    W2, V2 = W.clone(), V.clone()
+    Wg, Vg = W.clone(), V.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        api.ard_fc_muon(desc, None, W.clone(), V.clone(), G, None, None, None, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        api.ard_fc_muon(desc, None, Wg, Vg, G, None, None, None, ws)
+    for seed in range(4):
+        gen = torch.Generator(device=G.device).manual_seed(seed)
+        G.copy_(torch.randn(G.shape, generator=gen, device=G.device) * 1e-2)
+        graph.replay()
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.current_stream())
+            api.ard_fc_muon(desc, None, W2, V2, G, None, None, None, ws2)
+        torch.cuda.synchronize()
+        kept = torch.isfinite(G)
+        assert torch.equal(Wg, W2) and torch.equal(Vg, V2) and kept.all()
+
+
+@pytest.mark.gpu
+def test_weights_that_start_off_16_bytes():
+    """Slices of stacked weights (the two projections of a gated layer) start at any element."""
+    from gpu_util import device, workspace
+    dev, n, k = device(), 51, 77
+    gen = torch.Generator(device=dev).manual_seed(1)
+    W = torch.randn(2, n, k, generator=gen, device=dev).to(torch.bfloat16)
+    V, G = torch.randn(2, n, k, generator=gen, device=dev), torch.randn(2, n, k, generator=gen, device=dev)
+    desc = api.fc_desc(api.ARD_BF16, 1, k, n)
+    ws = workspace(api.ard_fc_muon_workspace_bytes(desc))
+    alone = [W[1].clone(), V[1].clone()]
+    api.ard_fc_muon(desc, None, *alone, G[1].clone(), None, None, None, ws)
+    first = W[0].clone()
+    api.ard_fc_muon(desc, None, W[1], V[1], G[1], None, None, None, ws)
+    assert torch.equal(W[1], alone[0]) and torch.equal(V[1], alone[1]) and torch.equal(W[0], first)

@@ -8,7 +8,7 @@ import test_isa_hazards as isa
 
 FOLDER = os.path.join(os.path.dirname(isa.BUILD), "csrc", "train")
 SOURCES = sorted(f for f in os.listdir(FOLDER) if f.endswith(".hip"))
-DIRECT_LOADS = {"ard_headloss.hip"}
+DIRECT_LOADS = {"ard_headloss.hip", "ard_muon.hip"}
 
 
 @pytest.mark.skipif(not all(os.path.exists(t) for t in isa.TOOLS), reason="ROCm LLVM tools not found")
