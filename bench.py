@@ -1148,12 +1148,12 @@ def code_text(src):
 
 def source_digest():
     """sha256 over the code of the layers' kernel sources and the header (comments
-    and layout left out, and csrc/lm, whose kernels no workload here runs): a
-    stored counter reading holds only for the code it was taken on."""
+    and layout left out, and the folders csrc/lm and csrc/train, whose kernels no
+    workload here runs): a stored counter reading holds only for the code it was taken on."""
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_1805_08939_amd", "csrc")
-    files = sorted(os.path.join(csrc, f) for f in os.listdir(csrc) if f != "lm")
+    files = sorted(os.path.join(csrc, f) for f in os.listdir(csrc) if os.path.isfile(os.path.join(csrc, f)))
     files.append(os.path.join(ROOT, "include", "ard.h"))
     for f in files:
         h.update(os.path.basename(f).encode())
