@@ -95,9 +95,9 @@ __device__ __forceinline__ int kc_swz(int r) {
 template <int CPR, int ES>
 __device__ __forceinline__ int mc_swz(int k) {
   if constexpr (ES == 2) {
-    if constexpr (CPR >= 16)
+    if constexpr (CPR % 16 == 0)
       return (k & 3) << 2;
-    else if constexpr (CPR == 8)
+    else if constexpr (CPR % 8 == 0)  // a row is an odd number of half turns around the banks
       return ((k >> 1) & 1) << 2;
     else
       return 0;

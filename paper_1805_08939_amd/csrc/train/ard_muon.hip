@@ -10,7 +10,7 @@
 // product has the shape of the block. Bound by the matrix cores, for small blocks by the
 // latency of three products after one another.
 
-#include "ard_train.hpp"
+#include "ard_parts_gemm.hpp"
 
 namespace ard {
 namespace {
@@ -65,22 +65,19 @@ __device__ __forceinline__ double inverse_norm(const double* sums, int blocks, f
   return 1.0 / (sqrt(red[0]) + static_cast<double>(eps));
 }
 
-// X = U / (|U| + eps), in place.
-__global__ void __launch_bounds__(256) muon_scale_kernel(Block b, float* __restrict__ X, const double* __restrict__ sums,
-                                                         int blocks, float eps) {
+// X = U / (|U| + eps), in parts.
+template <int P>
+__global__ void __launch_bounds__(256) muon_scale_kernel(Block b, const float* __restrict__ U, const double* __restrict__ sums,
+                                                         int blocks, float eps, bf16* __restrict__ X, int64_t plane) {
   const double inv = inverse_norm(sums, blocks, eps);
-  for (int64_t i = blockIdx.x; i < b.R; i += gridDim.x)
-    for (int64_t j = threadIdx.x; j < b.C; j += 256) X[i * b.ldx + j] = static_cast<float>(X[i * b.ldx + j] * inv);
-}
-
-// P = a + b A + c S, into S.
-__global__ void __launch_bounds__(256) muon_poly_kernel(int32_t m, int64_t lda, const float* __restrict__ A,
-                                                        float* __restrict__ S, float a, float b, float c) {
-  for (int64_t i = blockIdx.x; i < m; i += gridDim.x)
-    for (int64_t j = threadIdx.x; j < m; j += 256) {
-      const int64_t at = i * lda + j;
-      S[at] = c * S[at] + b * A[at] + (i == j ? a : 0.0f);
-    }
+  const int64_t per = b.ldx / 8, total = per * b.R, step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < total; at += step) {
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(U + at * 8), hi = *reinterpret_cast<const f32x4*>(U + at * 8 + 4);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(lo[e] * inv), v[4 + e] = static_cast<float>(hi[e] * inv);
+    store_parts<P>(X + at * 8, plane, v);
+  }
 }
 
 template <typename T>
@@ -135,6 +132,8 @@ int check_desc(const ard_fc_desc* d, MuonShape* s) {
   s->m = std::min(r.kept, c.kept);
   s->l = std::max(r.kept, c.kept);
   s->lda = up8(s->m);
+  if (s->l >= 1 << 22)  // offsets within a tile have 32 bits
+    return fail(ARD_ERR_UNSUPPORTED, "%d x %d kept weights: sides must be below 2^22", r.kept, c.kept);
   s->stretch = in.kept > 0 ? std::sqrt(std::max(1.0, static_cast<double>(out.kept) / in.kept)) : 1.0;
   return ARD_OK;
 }
@@ -149,59 +148,73 @@ int check_opts(const ard_muon_opts* o) {
   return ARD_OK;
 }
 
+// The workspace: the block in fp32 (U, at the end X), X twice and A and the polynomial in
+// parts, the sums of squares, the products' partial sums.
 struct Space {
-  size_t x, a, sums, part;
-  size_t bytes() const { return 2 * x + 2 * a + sums + part; }
+  size_t u, x, a, sums, part;
+  size_t bytes() const { return u + 2 * x + 2 * a + sums + part; }
 };
+template <int P>
 Space space_of(const MuonShape& s) {
-  if (s.m == 0) return {0, 0, 0, 0};
-  const size_t part = std::max({partial_floats<float>(s.m, s.m, s.l), partial_floats<float>(s.m, s.m, s.m),
-                                partial_floats<float>(s.b.R, s.b.C, s.m)});
-  return {al256(static_cast<size_t>(s.b.R) * s.b.ldx * 4), al256(static_cast<size_t>(s.m) * s.lda * 4), kNormBlocks * 8,
-          al256(4 * part)};
+  if (s.m == 0) return {0, 0, 0, 0, 0};
+  const size_t part = std::max({plan_parts<P>(s.m, s.m, s.l, true).floats, plan_parts<P>(s.m, s.m, s.m, true).floats,
+                                plan_parts<P>(s.b.R, s.b.C, s.m, false).floats});
+  const size_t x = static_cast<size_t>(s.b.R) * s.b.ldx, a = static_cast<size_t>(s.m) * s.lda;
+  return {al256(x * 4), al256(x * 2 * P), al256(a * 2 * P), kNormBlocks * 8, al256(4 * part)};
+}
+size_t space_bytes(const ard_fc_desc* d, const MuonShape& s) {
+  return d->dtype == ARD_BF16 ? space_of<2>(s).bytes() : space_of<3>(s).bytes();
 }
 
-template <typename T>
+template <int P, typename T>
 int muon_impl(const MuonShape& s, const ard_muon_opts& o, void* W, float* V, const float* dW, char* ws, hipStream_t stream) {
-  const Space sp = space_of(s);
+  const Space sp = space_of<P>(s);
   const Block& b = s.b;
-  float *X = reinterpret_cast<float*>(ws), *Y = reinterpret_cast<float*>(ws + sp.x);
-  float *A = reinterpret_cast<float*>(ws + 2 * sp.x), *S = reinterpret_cast<float*>(ws + 2 * sp.x + sp.a);
-  double* sums = reinterpret_cast<double*>(ws + 2 * sp.x + 2 * sp.a);
-  float* part = reinterpret_cast<float*>(ws + 2 * sp.x + 2 * sp.a + sp.sums);
+  const int64_t xp = static_cast<int64_t>(b.R) * b.ldx, ap = static_cast<int64_t>(s.m) * s.lda;  // planes
+  float* Uf = reinterpret_cast<float*>(ws);
+  bf16 *X = reinterpret_cast<bf16*>(ws + sp.u), *Y = reinterpret_cast<bf16*>(ws + sp.u + sp.x);
+  bf16 *A = reinterpret_cast<bf16*>(ws + sp.u + 2 * sp.x), *Q = reinterpret_cast<bf16*>(ws + sp.u + 2 * sp.x + sp.a);
+  char* rest = ws + sp.u + 2 * sp.x + 2 * sp.a;
+  double* sums = reinterpret_cast<double*>(rest);
+  float* part = reinterpret_cast<float*>(rest + sp.sums);
   const unsigned rows = static_cast<unsigned>(std::min(b.R, kNormBlocks));
-  hipLaunchKernelGGL(muon_momentum_kernel, dim3(rows), dim3(256), 0, stream, b, V, dW, o.momentum, o.nesterov != 0, X, sums);
+  hipLaunchKernelGGL(muon_momentum_kernel, dim3(rows), dim3(256), 0, stream, b, V, dW, o.momentum, o.nesterov != 0, Uf, sums);
   ARD_LAUNCH_CHECK();
-  hipLaunchKernelGGL(muon_scale_kernel, dim3(rows), dim3(256), 0, stream, b, X, sums, static_cast<int>(rows), o.eps);
+  const unsigned chunks = static_cast<unsigned>(std::min<int64_t>(2048, (xp / 8 + 255) / 256));
+  hipLaunchKernelGGL(muon_scale_kernel<P>, dim3(chunks), dim3(256), 0, stream, b, Uf, sums, static_cast<int>(rows), o.eps, X, xp);
   ARD_LAUNCH_CHECK();
+  const bool wide = b.R <= b.C;
   for (int it = 0; it < o.iterations; ++it) {
-    GemmArgs g = {};
+    const bool last = it + 1 == o.iterations;
+    PartsArgs g = {};
     g.M = g.N = s.m, g.K = s.l;
-    g.a = g.b = view(X, b.ldx);
-    g.c.p = A, g.c.ld = s.lda;
-    ARD_HIP_CHECK((b.R <= b.C ? product<float, false, false, float>(g, stream, part, sp.part / 4)
-                              : product<float, true, true, float>(g, stream, part, sp.part / 4)));
-    g = {};
-    g.M = g.N = g.K = s.m;
-    g.a = g.b = view(A, s.lda);  // A is its own transpose
-    g.c.p = S, g.c.ld = s.lda;
-    ARD_HIP_CHECK((product<float, false, false, float>(g, stream, part, sp.part / 4)));
-    hipLaunchKernelGGL(muon_poly_kernel, dim3(static_cast<unsigned>(std::min(s.m, 4096))), dim3(256), 0, stream, s.m, s.lda, A, S,
-                       o.a, o.b, o.c);
-    ARD_LAUNCH_CHECK();
+    g.a = g.b = PartsView{X, xp, b.ldx};
+    g.symmetric = true;
+    g.epi = PARTS_STORE;
+    g.out = A, g.plane = ap, g.ldo = s.lda;
+    ARD_HIP_CHECK((wide ? run_parts_gemm<P, false, false>(g, part, stream) : run_parts_gemm<P, true, true>(g, part, stream)));
+    g.K = s.m;
+    g.a = g.b = g.poly = PartsView{A, ap, s.lda};  // A is its own transpose
+    g.epi = PARTS_POLY;
+    g.out = Q;
+    g.pa = o.a, g.pb = o.b, g.pc = o.c;
+    ARD_HIP_CHECK((run_parts_gemm<P, false, false>(g, part, stream)));
     g = {};
     g.M = b.R, g.N = b.C, g.K = s.m;
-    g.c.p = Y, g.c.ld = b.ldx;
-    if (b.R <= b.C) {
-      g.a = view(S, s.lda), g.b = view(X, b.ldx);
-      ARD_HIP_CHECK((product<float, false, true, float>(g, stream, part, sp.part / 4)));
+    g.epi = last ? PARTS_FLOAT : PARTS_STORE;
+    g.out = Y, g.plane = xp, g.ldo = b.ldx;
+    g.fout = Uf;
+    const PartsView x{X, xp, b.ldx}, q{Q, ap, s.lda};
+    if (wide) {
+      g.a = q, g.b = x;
+      ARD_HIP_CHECK((run_parts_gemm<P, false, true>(g, part, stream)));
     } else {
-      g.a = view(X, b.ldx), g.b = view(S, s.lda);
-      ARD_HIP_CHECK((product<float, false, false, float>(g, stream, part, sp.part / 4)));
+      g.a = x, g.b = q;
+      ARD_HIP_CHECK((run_parts_gemm<P, false, false>(g, part, stream)));
     }
     std::swap(X, Y);
   }
-  hipLaunchKernelGGL(muon_update_kernel<T>, dim3(rows), dim3(256), 0, stream, b, X, static_cast<T*>(W),
+  hipLaunchKernelGGL(muon_update_kernel<T>, dim3(rows), dim3(256), 0, stream, b, Uf, static_cast<T*>(W),
                      static_cast<float>(1.0 - static_cast<double>(o.lr) * o.weight_decay),
                      static_cast<float>(o.lr * s.stretch));
   ARD_LAUNCH_CHECK();
@@ -223,7 +236,7 @@ void ard_muon_opts_default(ard_muon_opts* opts) {
 size_t ard_fc_muon_workspace_bytes(const ard_fc_desc* desc) {
   MuonShape s;
   if (check_desc(desc, &s) != ARD_OK) return 0;
-  return space_of(s).bytes();
+  return space_bytes(desc, s);
 }
 
 int ard_fc_muon(const ard_fc_desc* desc, const ard_muon_opts* opts, void* W, float* V, const float* dW, float* bias, float* Vb,
@@ -243,7 +256,7 @@ int ard_fc_muon(const ard_fc_desc* desc, const ard_muon_opts* opts, void* W, flo
       reinterpret_cast<uintptr_t>(dW) % 4 || reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(Vb) % 4 ||
       reinterpret_cast<uintptr_t>(dbias) % 4)
     return fail(ARD_ERR_INVALID_ARG, "W, V, dW or the bias is not aligned to its element size");
-  if ((st = check_space(space_of(s).bytes(), ws, ws_bytes)) != ARD_OK) return st;
+  if ((st = check_space(space_bytes(desc, s), ws, ws_bytes)) != ARD_OK) return st;
   hipStream_t sm = static_cast<hipStream_t>(stream);
   if (bias && s.out.kept > 0) {
     hipLaunchKernelGGL(muon_bias_kernel, dim3((s.out.kept + 255) / 256), dim3(256), 0, sm, s.out, bias, Vb, dbias, o.bias_lr,
@@ -252,7 +265,7 @@ int ard_fc_muon(const ard_fc_desc* desc, const ard_muon_opts* opts, void* W, flo
   }
   if (s.m == 0) return ARD_OK;
   char* w = static_cast<char*>(ws);
-  return desc->dtype == ARD_BF16 ? muon_impl<bf16>(s, o, W, V, dW, w, sm) : muon_impl<float>(s, o, W, V, dW, w, sm);
+  return desc->dtype == ARD_BF16 ? muon_impl<2, bf16>(s, o, W, V, dW, w, sm) : muon_impl<3, float>(s, o, W, V, dW, w, sm);
 }
 
 }  // extern "C"
