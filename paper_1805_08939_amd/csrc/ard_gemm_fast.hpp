@@ -866,7 +866,11 @@ __device__ __forceinline__ void run_slabs_reg(RegLoader<Cfg, AMC, BMC>& ld, int 
 // fp32, 8 bytes bf16): a store instruction covers whole 128-byte lines instead
 // of one element per lane. The ReLU gate of the layer below is read the same
 // way. Falls back to element stores when the output rows are not contiguous
-// or not aligned for those pieces. Called by all waves (it holds a barrier).
+// or, with an epilogue that may read a gate, not aligned for those pieces; plain
+// results go out in unaligned pieces (bf16 5001 x 331 times 331 x 1023: 20.2 to 17.8 us).
+// Called by all waves (it holds a barrier).
+typedef f32x4 f32x4_any __attribute__((aligned(4), may_alias));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2), may_alias));
 template <typename OutT, class Cfg, int EPI>
 __device__ __forceinline__ void fast_store(const GemmArgs& g, f32x16 (&acc)[Cfg::FM][Cfg::FN], int m0, int n0,
                                            int wm, int wn, int64_t bz, int split, char* smem) {
@@ -880,9 +884,9 @@ __device__ __forceinline__ void fast_store(const GemmArgs& g, f32x16 (&acc)[Cfg:
                          : nullptr;
   const int64_t piece = 4 * es;
   const bool vec = (part || (g.c.cidx == nullptr && g.c.col_stride <= 1 && g.c.ridx == nullptr)) &&
-                   (EPI != EPI_COLS || (g.c_nstride % 4 == 0 && g.nvalid % 4 == 0)) && (ld * es) % piece == 0 &&
-                   reinterpret_cast<uintptr_t>(base) % piece == 0 &&
-                   reinterpret_cast<uintptr_t>(gate) % piece == 0;
+                   (EPI != EPI_COLS || (g.c_nstride % 4 == 0 && g.nvalid % 4 == 0)) &&
+                   (EPI == EPI_STORE || ((ld * es) % piece == 0 && reinterpret_cast<uintptr_t>(base) % piece == 0 &&
+                                         reinterpret_cast<uintptr_t>(gate) % piece == 0));
   if (!vec) {
     store_tile<OutT, Cfg, EPI>(g, acc, m0, n0, wm, wn, bz, split);
     return;
@@ -956,7 +960,7 @@ __device__ __forceinline__ void fast_store(const GemmArgs& g, f32x16 (&acc)[Cfg:
       if (part) {
         float* out = reinterpret_cast<float*>(base) + o;
         if (n + 3 < g.N) {
-          *reinterpret_cast<f32x4*>(out) = v;
+          *reinterpret_cast<f32x4_any*>(out) = v;
         } else {
           for (int e = 0; e < 4; ++e)
             if (n + e < g.N) out[e] = v[e];
@@ -977,9 +981,9 @@ __device__ __forceinline__ void fast_store(const GemmArgs& g, f32x16 (&acc)[Cfg:
             if (!(to_f32(gv[e]) > 0.0f)) w[e] = from_f32<OutT>(0.0f);
         }
         if constexpr (sizeof(OutT) == 2)
-          *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(w);
+          *reinterpret_cast<u32x2_any*>(out) = *reinterpret_cast<const u32x2_any*>(w);
         else
-          *reinterpret_cast<f32x4*>(out) = *reinterpret_cast<const f32x4*>(w);
+          *reinterpret_cast<f32x4_any*>(out) = *reinterpret_cast<const f32x4_any*>(w);
       } else {
         for (int e = 0; e < 4; ++e) {
           if (n + e >= g.N) break;
