@@ -98,7 +98,8 @@ struct Chunk {
       return __uint_as_float(raw[e]);
   }
 };
-template <typename T, int VE>
+// NT: past the caches, for what is not read again soon.
+template <typename T, int VE, bool NT = false>
 __device__ __forceinline__ void store_chunk(T* p, const float (&v)[VE], int n) {
   if constexpr (VE == 1) {
     *p = from_f32<T>(v[0]);
@@ -107,7 +108,10 @@ __device__ __forceinline__ void store_chunk(T* p, const float (&v)[VE], int n) {
 #pragma unroll
     for (int e = 0; e < VE; ++e) w[e] = from_f32<T>(v[e]);
     if (n >= VE) {
-      *reinterpret_cast<u32x4_any2*>(p) = *reinterpret_cast<const u32x4_any*>(w);
+      if constexpr (NT)
+        __builtin_nontemporal_store(*reinterpret_cast<const u32x4_any*>(w), reinterpret_cast<u32x4_any2*>(p));
+      else
+        *reinterpret_cast<u32x4_any2*>(p) = *reinterpret_cast<const u32x4_any*>(w);
     } else {
 #pragma unroll
       for (int e = 0; e < VE; ++e)
