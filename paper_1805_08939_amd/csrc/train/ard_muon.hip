@@ -203,7 +203,7 @@ int muon_impl(const MuonShape& s, const ard_muon_opts& o, void* W, float* V, con
     g.M = b.R, g.N = b.C, g.K = s.m;
     g.epi = last ? PARTS_FLOAT : PARTS_STORE;
     g.out = Y, g.plane = xp, g.ldo = b.ldx;
-    g.fout = Uf;
+    g.fout = Uf, g.fstep = 1;
     const PartsView x{X, xp, b.ldx}, q{Q, ap, s.lda};
     if (wide) {
       g.a = q, g.b = x;

@@ -37,22 +37,26 @@ struct PartsArgs {
   int32_t epi;
   bf16* out;        // PARTS_STORE, PARTS_POLY
   int64_t plane, ldo;
-  float* fout;      // PARTS_FLOAT, rows of ldo
+  float* fout;      // PARTS_FLOAT, rows of ldo at any element, values of a row fstep apart
+  int32_t fstep;
   PartsView poly;   // PARTS_POLY: A
   float pa, pb, pc;
   int32_t splits;   // of the slabs, each writing its sums to partial
   float* partial;   // [splits][tiles][wave][block][16][64]
 };
 
-template <int PARTS_, int BM_, int BN_, int WGM_, int WGN_, int STAGES_>
-struct PartsCfg : FastCfg<bf16, BM_, BN_, 32, STAGES_, WGM_, WGN_, 1> {
-  using Base = FastCfg<bf16, BM_, BN_, 32, STAGES_, WGM_, WGN_, 1>;
+template <int PARTS_, int BM_, int BN_, int WGM_, int WGN_, int STAGES_, int BK_ = 32, int KSPLIT_ = 1>
+struct PartsCfg : FastCfg<bf16, BM_, BN_, BK_, STAGES_, WGM_, WGN_, KSPLIT_> {
+  using Base = FastCfg<bf16, BM_, BN_, BK_, STAGES_, WGM_, WGN_, KSPLIT_>;
   static constexpr int PARTS = PARTS_;
   static constexpr int STAGE = PARTS * Base::STAGE;            // A's parts, then B's
   static constexpr int AREGION = PARTS * Base::ABYTES;
   static constexpr int LPW = PARTS * Base::LPW;
+  static constexpr int OUTS = Base::WGM * Base::WGN;           // waves with outputs (the others share their k)
+  static constexpr int SUMS = Base::FM * Base::FN * 16 * 64;   // a wave's sums
   static constexpr int ROW = Base::TN * 4 + 32;                // of the epilogue's staging: 32 rows of a wave
-  static constexpr int MAIN = STAGES_ * STAGE, ENDS = Base::NW * 32 * ROW;
+  static constexpr int RED = (Base::KSPLIT - 1) * OUTS * SUMS * 4;
+  static constexpr int MAIN = STAGES_ * STAGE, ENDS = RED + OUTS * 32 * ROW;
   static constexpr int LDS = MAIN > ENDS ? MAIN : ENDS;
 };
 
@@ -103,8 +107,8 @@ __device__ __forceinline__ void load_parts(const bf16* p, int64_t plane, float (
 }
 
 // The results of 32 rows x TN columns, from row m0 and column n0 on, through the wave's LDS:
-// eight columns of a row a lane, and for a mirrored tile eight rows of a column. Rows of the
-// outputs hold whole chunks (ldo is a multiple of 8), so that a chunk is written whole.
+// eight columns of a row a lane, and for a mirrored tile eight rows of a column. Rows of parts
+// hold whole chunks (ldo is a multiple of 8), so that a chunk is written whole.
 template <class Cfg>
 __device__ __forceinline__ void parts_block(const PartsArgs& g, const f32x16 (&acc)[Cfg::FN], int m0, int n0, bool mirror,
                                             char* region) {
@@ -125,9 +129,16 @@ __device__ __forceinline__ void parts_block(const PartsArgs& g, const f32x16 (&a
     for (int x = 0; x < 8; ++x) v[x] = at[x];
     if (m >= g.M || n >= g.N) continue;
     if (g.epi == PARTS_FLOAT) {
-      float* o = g.fout + m * g.ldo + n;
-      *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f32x4*>(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
+      float* o = g.fout + m * g.ldo + static_cast<int64_t>(n) * g.fstep;
+      if (g.fstep == 1 && n + 8 <= g.N) {
+        const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+        store_chunk<float, 4>(o, lo, 4);
+        store_chunk<float, 4>(o + 4, hi, 4);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (n + x < g.N) o[static_cast<int64_t>(x) * g.fstep] = v[x];
+      }
       continue;
     }
     if (g.epi == PARTS_POLY) {
@@ -211,11 +222,21 @@ __device__ __forceinline__ void parts_mma(const bf16x8 (&a)[Cfg::FM], const bf16
 // fragments' reads and in front of the last instructions.
 template <class Cfg, bool AMC, bool BMC>
 __device__ __forceinline__ void run_parts(PartsLoader<Cfg, AMC, BMC>& ld, int nslab, int K, int k0,
-                                          f32x16 (&acc)[Cfg::FM][Cfg::FN], int wm, int wn, char* smem) {
+                                          f32x16 (&acc)[Cfg::FM][Cfg::FN], int wm, int wn, int kw0, char* smem) {
   using Frags = PartFrags<Cfg, AMC, BMC>;
   using Base = typename Cfg::Base;
-  constexpr int STEPS = Cfg::BK / 16, AHEAD = Cfg::STAGES - 1;
-  static_assert(STEPS == 2, "two k steps of a slab");
+  using Acc = f32x16[Cfg::FM][Cfg::FN];
+  // A wave with one block of outputs would wait for each instruction's result before the
+  // next one: its further products go to sums of their own.
+  constexpr bool CHAINS = Cfg::FM * Cfg::FN == 1;
+  f32x16 more[CHAINS ? 2 : 1][Cfg::FM][Cfg::FN];
+  if constexpr (CHAINS) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) more[0][0][0][r] = more[1][0][0][r] = 0.0f;
+  }
+  auto chain = [&](int c) -> Acc& { return CHAINS && c > 0 ? more[c - 1] : acc; };
+  constexpr int STEPS = Cfg::KW / 16, AHEAD = Cfg::STAGES - 1;
+  static_assert(STEPS == 2, "two k steps of a slab for each wave");
   if (nslab <= 0) return;
   auto tail = [&](char* st, int ck) {
     if (K - ck >= Cfg::BK) return;
@@ -235,11 +256,11 @@ __device__ __forceinline__ void run_parts(PartsLoader<Cfg, AMC, BMC>& ld, int ns
   lds_barrier();
   tail(st, ck);
   ld.issue_a();
-  h[0].load(st, 0, wm, wn, 0);
+  h[0].load(st, 0, wm, wn, kw0);
   for (int q = 0; q < nslab; ++q) {
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      const int kk = 16 * s;
+      const int kk = kw0 + 16 * s;
       Frags& f = h[s & 1];
       Frags lo, mid;
       lo.load(st, Cfg::PARTS - 1, wm, wn, kk);
@@ -247,8 +268,8 @@ __device__ __forceinline__ void run_parts(PartsLoader<Cfg, AMC, BMC>& ld, int ns
       parts_mma<Cfg>(f.a, f.b, acc);
       if (s == 0) ld.issue_b();
       if constexpr (Cfg::PARTS == 3) {
-        parts_mma<Cfg>(f.a, mid.b, acc);
-        parts_mma<Cfg>(mid.a, f.b, acc);
+        parts_mma<Cfg>(f.a, mid.b, chain(1));
+        parts_mma<Cfg>(mid.a, f.b, chain(2));
         parts_mma<Cfg>(mid.a, mid.b, acc);
       }
       if (s + 1 < STEPS) {
@@ -261,12 +282,13 @@ __device__ __forceinline__ void run_parts(PartsLoader<Cfg, AMC, BMC>& ld, int ns
         lds_barrier();  // the next slab is visible; this one's fragments have been read by every wave
         tail(st, ck);
         ld.issue_a();
-        h[0].load(st, 0, wm, wn, 0);
+        h[0].load(st, 0, wm, wn, kw0);
       }
-      parts_mma<Cfg>(f.a, lo.b, acc);
-      parts_mma<Cfg>(lo.a, f.b, acc);
+      parts_mma<Cfg>(f.a, lo.b, chain(1));
+      parts_mma<Cfg>(lo.a, f.b, chain(2));
     }
   }
+  if constexpr (CHAINS) acc[0][0] += more[0][0][0] + more[1][0][0];
   wait_vm<0>();  // no direct load may still write LDS past this point
 }
 
@@ -290,7 +312,8 @@ __global__ void __launch_bounds__(Cfg::NT) parts_gemm_kernel(PartsArgs g) {
   else
     grouped_order(tile, n.nx, n.ny, row, col);
   const int64_t m0 = static_cast<int64_t>(row) * Cfg::BM, n0 = static_cast<int64_t>(col) * Cfg::BN;
-  const int wave = threadIdx.x >> 6, wm = wave / Cfg::WGN, wn = wave % Cfg::WGN;
+  const int lane = threadIdx.x & 63, ks = (threadIdx.x >> 6) / Cfg::OUTS, wave = (threadIdx.x >> 6) % Cfg::OUTS;
+  const int wm = wave / Cfg::WGN, wn = wave % Cfg::WGN;
   f32x16 acc[Cfg::FM][Cfg::FN];
 #pragma unroll
   for (int i = 0; i < Cfg::FM; ++i)
@@ -318,22 +341,36 @@ __global__ void __launch_bounds__(Cfg::NT) parts_gemm_kernel(PartsArgs g) {
     ld.lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
     ld.is = 0;
     ld.left = q1 - q0 - 1;
-    run_parts<Cfg, AMC, BMC>(ld, q1 - q0, g.K, q0 * Cfg::BK, acc, wm, wn, smem);
+    run_parts<Cfg, AMC, BMC>(ld, q1 - q0, g.K, q0 * Cfg::BK, acc, wm, wn, ks * Cfg::KW, smem);
   }
-  if (g.splits > 1) {
-    float* to = g.partial + ((static_cast<int64_t>(split) * n.tiles + tile) * Cfg::NW + wave) * (Cfg::FM * Cfg::FN * 16 * 64);
+  // sums[4 (i, j, r / 4) + r % 4] of a lane, in pieces of four
+  auto each4 = [&](float* sums, auto f) {
 #pragma unroll
     for (int i = 0; i < Cfg::FM; ++i)
 #pragma unroll
       for (int j = 0; j < Cfg::FN; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<f32x4*>(to + (((i * Cfg::FN + j) * 4 + r / 4) * 64 + (threadIdx.x & 63)) * 4) =
-              f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+        for (int r = 0; r < 16; r += 4) f(*reinterpret_cast<f32x4*>(sums + (((i * Cfg::FN + j) * 4 + r / 4) * 64 + lane) * 4), acc[i][j], r);
+  };
+  auto put = [](f32x4& to, f32x16& a, int r) { to = f32x4{a[r], a[r + 1], a[r + 2], a[r + 3]}; };
+  lds_barrier();  // every wave is done with the stages
+  if constexpr (Cfg::KSPLIT > 1) {
+    float* red = reinterpret_cast<float*>(smem);
+    if (ks > 0) each4(red + ((ks - 1) * Cfg::OUTS + wave) * Cfg::SUMS, put);
+    lds_barrier();
+    if (ks > 0) return;
+#pragma unroll
+    for (int u = 0; u < Cfg::KSPLIT - 1; ++u)
+      each4(red + (u * Cfg::OUTS + wave) * Cfg::SUMS, [](f32x4& from, f32x16& a, int r) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[r + e] += from[e];
+      });
+  }
+  if (g.splits > 1) {
+    each4(g.partial + ((static_cast<int64_t>(split) * n.tiles + tile) * Cfg::OUTS + wave) * Cfg::SUMS, put);
     return;
   }
-  lds_barrier();  // every wave is done with the stages
-  char* region = smem + wave * 32 * Cfg::ROW;
+  char* region = smem + Cfg::RED + wave * 32 * Cfg::ROW;
 #pragma unroll
   for (int i = 0; i < Cfg::FM; ++i)
     parts_block<Cfg>(g, acc[i], static_cast<int>(m0) + wm * Cfg::TM + 32 * i, static_cast<int>(n0) + wn * Cfg::TN,
@@ -345,7 +382,7 @@ template <class Cfg>
 __global__ void __launch_bounds__(64) parts_join_kernel(PartsArgs g) {
   __shared__ __attribute__((aligned(16))) char region[32 * Cfg::ROW];
   const PartsTiles n = parts_tiles<Cfg>(g.M, g.N, g.symmetric);
-  const int i = blockIdx.x % Cfg::FM, wave = blockIdx.x / Cfg::FM % Cfg::NW, tile = blockIdx.x / (Cfg::FM * Cfg::NW);
+  const int i = blockIdx.x % Cfg::FM, wave = blockIdx.x / Cfg::FM % Cfg::OUTS, tile = blockIdx.x / (Cfg::FM * Cfg::OUTS);
   int row, col;
   if (g.symmetric)
     triangle_tile(tile, row, col);
@@ -358,7 +395,7 @@ __global__ void __launch_bounds__(64) parts_join_kernel(PartsArgs g) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[j][r] = 0.0f;
   for (int split = 0; split < g.splits; ++split) {
-    const float* from = g.partial + ((static_cast<int64_t>(split) * n.tiles + tile) * Cfg::NW + wave) * (Cfg::FM * Cfg::FN * 16 * 64);
+    const float* from = g.partial + ((static_cast<int64_t>(split) * n.tiles + tile) * Cfg::OUTS + wave) * Cfg::SUMS;
 #pragma unroll
     for (int j = 0; j < Cfg::FN; ++j)
 #pragma unroll
@@ -374,13 +411,15 @@ __global__ void __launch_bounds__(64) parts_join_kernel(PartsArgs g) {
 // ------------------------------------------------------------------ plans
 enum PartsKind { PARTS_256, PARTS_192, PARTS_128, PARTS_64 };
 
+// The 64 x 64 tile, for few tiles: two groups of waves share a slab's k, so that twice the
+// waves hide its loads (512 x 784 in three parts, five iterations: 204 us with one, 184).
 template <int P>
 struct PartsCfgs {
-  // 256 x 256 holds two parts of two stages only
-  using C256 = PartsCfg<P, 256, 256, 2, 4, 2>;
+  // two stages of 256 x 256 hold two parts only
+  using C256 = typename std::conditional<P == 2, PartsCfg<P, 256, 256, 2, 4, 2>, PartsCfg<P, 256, 128, 4, 2, 2>>::type;
   using C192 = PartsCfg<P, 192, 192, 2, 2, P == 2 ? 3 : 2>;
   using C128 = PartsCfg<P, 128, 128, 2, 2, P == 2 ? 2 : 3>;
-  using C64 = PartsCfg<P, 64, 64, 2, 2, P == 2 ? 4 : 3>;
+  using C64 = PartsCfg<P, 64, 64, 2, 2, P == 2 ? 4 : 3, 64, 2>;
 };
 
 struct PartsPlan {
@@ -392,26 +431,32 @@ constexpr int kPartsSplits = 16;
 
 // The tile and split with the least modelled time, in us: rounds of the chip times a tile's
 // instructions over the rate that a compute unit reaches with it, the partial sums' bytes
-// twice and the launch that joins them.
+// twice and the launch that joins them. Measured on MI355X over 11 blocks of each type (64 x
+// 64 to 1500 x 6000, five iterations): the pick takes at most 1.06 of the time of the best
+// single tile (2048 x 2048 in two parts: 753 and 713 us), one tile for all up to 4.7 times
+// (192 x 192 without splits on 512 x 512 in three: 764 us, the pick 173).
 template <int P>
 PartsPlan plan_parts(int M, int N, int K, bool symmetric) {
   struct Tile {
-    int kind, bm, bn, per;  // per: workgroups of a compute unit
-    double rate;            // flop/us of a compute unit on bf16 products
+    int kind, bm, bn, bk, per;  // per: workgroups of a compute unit
+    double one, full;           // flop/us of a compute unit on bf16 products, with one of them and with all
   };
-  static constexpr Tile tiles[] = {{PARTS_256, 256, 256, 1, 5.6e6}, {PARTS_192, 192, 192, 1, 5.6e6}, {PARTS_128, 128, 128, 2, 4.4e6}, {PARTS_64, 64, 64, P == 2 ? 2 : 1, 2.4e6}};
+  static constexpr Tile two[] = {{PARTS_256, 256, 256, 32, 1, 5.1e6, 5.1e6}, {PARTS_192, 192, 192, 32, 1, 4.3e6, 4.3e6},
+                                 {PARTS_128, 128, 128, 32, 2, 2.9e6, 4.4e6}, {PARTS_64, 64, 64, 64, 1, 2.4e6, 2.4e6}};
+  static constexpr Tile three[] = {{PARTS_256, 256, 128, 32, 1, 4.9e6, 4.9e6}, {PARTS_192, 192, 192, 32, 1, 4.6e6, 4.6e6},
+                                   {PARTS_128, 128, 128, 32, 1, 3.8e6, 3.8e6}, {PARTS_64, 64, 64, 64, 1, 3.2e6, 3.2e6}};
   PartsPlan best = {PARTS_64, 1, 0};
   double best_t = 1e300;
   const int products = P == 2 ? 3 : 6;
-  for (const Tile& c : tiles) {
-    if (c.kind == PARTS_256 && P == 3) continue;
+  for (const Tile& c : P == 2 ? two : three) {
+    if (symmetric && c.bm != c.bn) continue;  // the triangle is one of square tiles
     const int64_t ny = (M + c.bm - 1) / c.bm, nx = (N + c.bn - 1) / c.bn, n = symmetric ? ny * (ny + 1) / 2 : nx * ny;
-    const int64_t slabs = (K + 31) / 32;
+    const int64_t slabs = (K + c.bk - 1) / c.bk;
     for (int s = 1; s <= kPartsSplits && (s == 1 || slabs / s >= 4); ++s) {
       const int64_t wgs = n * s, rounds = (wgs + kTargetBlocks * c.per - 1) / (kTargetBlocks * c.per);
-      const double share = wgs >= kTargetBlocks * c.per ? c.per : std::max(1.0, static_cast<double>(wgs) / kTargetBlocks);
-      const double work = 2.0 * c.bm * c.bn * 32 * products * ((slabs + s - 1) / s) / c.rate;
-      double t = 6.0 + 2.0 * (rounds - 1) + rounds * share * work;
+      const double share = wgs >= kTargetBlocks * c.per ? c.per : static_cast<double>(wgs) / kTargetBlocks;
+      const double work = 2.0 * c.bm * c.bn * c.bk * products * ((slabs + s - 1) / s);
+      double t = 4.5 + 2.0 * (rounds - 1) + rounds * work * std::max(1.0 / c.one, share / c.full);
       const double bytes = 4.0 * c.bm * c.bn * wgs;
       if (s > 1) t += 4.0 + 2.0 * bytes / 5e6;
       if (t < best_t) best_t = t, best = {c.kind, s, s > 1 ? static_cast<size_t>(bytes / 4) : 0};
@@ -430,7 +475,7 @@ hipError_t launch_parts(const PartsArgs& g, hipStream_t stream) {
   hipLaunchKernelGGL(kern, dim3(tiles * g.splits), dim3(Cfg::NT), Cfg::LDS, stream, g);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.splits == 1) return e;
-  hipLaunchKernelGGL(parts_join_kernel<Cfg>, dim3(tiles * Cfg::FM * Cfg::NW), dim3(64), 0, stream, g);
+  hipLaunchKernelGGL(parts_join_kernel<Cfg>, dim3(tiles * Cfg::FM * Cfg::OUTS), dim3(64), 0, stream, g);
   return hipGetLastError();
 }
 
@@ -443,9 +488,7 @@ hipError_t run_parts_gemm(PartsArgs g, float* partial, hipStream_t stream) {
   g.partial = partial;
   using C = PartsCfgs<P>;
   switch (p.kind) {
-    case PARTS_256:
-      if constexpr (P == 2) return launch_parts<typename C::C256, AMC, BMC>(g, stream);
-      else return hipErrorNotSupported;
+    case PARTS_256: return launch_parts<typename C::C256, AMC, BMC>(g, stream);
     case PARTS_192: return launch_parts<typename C::C192, AMC, BMC>(g, stream);
     case PARTS_128: return launch_parts<typename C::C128, AMC, BMC>(g, stream);
     default: return launch_parts<typename C::C64, AMC, BMC>(g, stream);
