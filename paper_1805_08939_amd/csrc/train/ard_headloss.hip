@@ -4,17 +4,24 @@
 //
 // Forward: a product whose epilogue reduces each tile's logits to a maximum and a sum of
 // exponentials a column; the tiles' pairs are joined by a second, small kernel. Backward:
-// the classes in pieces; the same product with an epilogue that writes dz of a piece
-// (rounded once, the operand of two products; its row sums, the bias gradient, are taken
-// before that), then dX and dW from it. A piece's dz is a few ten MB, so that the products
+// the classes in pieces; the same product with an epilogue that writes dz of a piece (the
+// operand of two products; its row sums, the bias gradient, are taken before it is rounded
+// for that), then dX and dW from it. A piece's dz is a few ten MB, so that the products
 // find it in the memory-side cache. Logits are fp32 throughout.
+//
+// bf16 operands are read in place where their rows start on 16 bytes, else from copies.
+// fp32 operands, dz among them, are copied into three bf16 parts (ard_parts_gemm.hpp):
+// exact to 2^-24 and, with six bf16 products for one, still faster than fp32 products (8800
+// classes of 750 inputs, batch 700, forward and backward: 418 to 280 us). A part cannot hold
+// what fp32 rounds past the largest bf16 number: an infinite W or X makes NaN in its sums.
+// A few classes take a kernel of their own (head_few_kernel) without any copy.
 //
 // Columns without a label contribute nothing: their loss and dz are 0, and the inputs that
 // meet their dz in dW are 0 too, whatever they hold.
 //
 // Bound by the matrix cores for many columns, by reading W for few.
 
-#include "ard_train.hpp"
+#include "ard_parts_gemm.hpp"
 
 namespace ard {
 namespace {
@@ -48,11 +55,13 @@ struct HeadShape {
   Kept in;
   int64_t ldp;       // row length of dz and of X's copy
   int64_t ldc;       // row length of W's copy
+  int64_t wrows;     // its rows
   size_t es;
   bool input_major;  // W^T[K][V]
   bool zero;         // gradients of dropped inputs are written 0
-  bool copy_w;       // output-major weights of kept inputs, or with rows off 16 bytes, are copied
-  bool copy_x;       // so is X with rows off 16 bytes in the forward (always in the backward)
+  bool few;          // head_few_kernel
+  bool parts;        // operands in parts
+  bool copy_w, copy_x;  // the forward reads a copy of W, of X (the backward's X is always one)
 };
 
 struct TileArgs {
@@ -62,6 +71,7 @@ struct TileArgs {
   const void* W;         // the launch's first class; rows of ldw
   const void* X;         // rows of ldx
   int64_t ldw, ldx;
+  int64_t wplane, xplane;  // elements from a part to the next
   const float* bias;     // of the launch's first class, or NULL
   const int32_t* labels;
   int32_t classes;
@@ -71,8 +81,8 @@ struct TileArgs {
   // backward
   const float* stats;    // [2][B]: maximum, 1 / sum
   const float* dloss;    // [B] or NULL
-  void* P;               // [M][ldp]
-  int64_t ldp;
+  void* P;               // [M][ldp], in parts as W and X are
+  int64_t ldp, pplane;
   float* dbias;          // [parts][classes] row sums from the launch's first class on, or NULL
 };
 
@@ -91,15 +101,13 @@ struct HeadLds {
   static constexpr int one(int way) {
     return Cfg::KSPLIT > 1 ? HEAD + (RED > ZT ? RED : ZT) + ZT : HEAD + (way == WAY_LOSS ? SUMS : STAGE);
   }
-  static constexpr int bytes(int way, int ld) {
-    const int main = ld == LOAD_ANY ? 2 * Cfg::STAGE : Cfg::LDS;
-    return one(way) > main ? one(way) : main;
-  }
+  static constexpr int bytes(int way) { return one(way) > Cfg::LDS ? one(way) : Cfg::LDS; }
 };
 
-template <class Cfg, bool AMC, int LD, int WAY>
+// P parts of each operand, or (0) the operands themselves.
+template <class Cfg, int P, bool AMC, int WAY>
 __global__ void __launch_bounds__(Cfg::NT) head_tile_kernel(TileArgs g) {
-  using T = typename Cfg::T;
+  using T = typename std::conditional<P == 0, typename Cfg::T, float>::type;
   constexpr int ES = Cfg::ES;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int nx = (g.B + Cfg::BN - 1) / Cfg::BN;
@@ -126,7 +134,7 @@ __global__ void __launch_bounds__(Cfg::NT) head_tile_kernel(TileArgs g) {
   const char* wp = static_cast<const char*>(g.W) + (AMC ? m0 : m0 * g.ldw) * ES;
   const char* xp = static_cast<const char*>(g.X) + n0 * ES;
   {
-    using Loader = typename std::conditional<LD == LOAD_ANY, RegLoader<Cfg, AMC, true>, SlabLoader<Cfg, AMC, true>>::type;
+    using Loader = typename std::conditional<P == 0, SlabLoader<Cfg, AMC, true>, PartsLoader<Cfg, AMC, true>>::type;
     Loader ld;
     ld.wv = wv;
     ld.da.init(g.ldw, 0, rows, wv);
@@ -135,16 +143,18 @@ __global__ void __launch_bounds__(Cfg::NT) head_tile_kernel(TileArgs g) {
     ld.ik = 0;
     ld.a_step = (AMC ? g.ldw : 1) * Cfg::BK * ES;
     ld.b_step = g.ldx * Cfg::BK * ES;
-    ld.a_wrap = ld.b_wrap = 0;
     ld.na = uniform_ptr(wp);
     ld.nb = uniform_ptr(xp);
-    if constexpr (LD == LOAD_ANY) {
-      run_slabs_reg<Cfg, AMC, true, false>(ld, nslab, acc, wm, wn, ks * Cfg::KW, smem, nullptr);
-    } else {
-      ld.lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-      ld.is = 0;
-      ld.left = nslab - 1;
+    ld.lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+    ld.is = 0;
+    ld.left = nslab - 1;
+    if constexpr (P == 0) {
+      ld.a_wrap = ld.b_wrap = 0;
       run_slabs<Cfg, AMC, true, true, false>(ld, nslab, g.K, 0, acc, wm, wn, ks * Cfg::KW, smem);
+    } else {
+      ld.a_plane = g.wplane * ES;
+      ld.b_plane = g.xplane * ES;
+      run_parts<Cfg, AMC, true>(ld, nslab, g.K, 0, acc, wm, wn, ks * Cfg::KW, smem);
     }
   }
 
@@ -222,8 +232,11 @@ __global__ void __launch_bounds__(Cfg::NT) head_tile_kernel(TileArgs g) {
       }
     } else {
       // 32 rows of a wave at a time through its own LDS, then 16 bytes of a row a lane
-      constexpr int VE = 16 / ES, CPRW = Cfg::TN / VE, RPI = 64 / CPRW;
+      constexpr int CPRW = Cfg::TN / 8, RPI = 64 / CPRW;
       char* region = stage + wave * 32 * L::ROW;
+      auto put_sum = [&](int row, float sum) {
+        g.dbias[(static_cast<int64_t>(tile_col) * Cfg::WGN + wn) * g.classes + m0 + row] = sum;
+      };
 #pragma unroll
       for (int i = 0; i < Cfg::FM; ++i) {
 #pragma unroll
@@ -235,26 +248,40 @@ __global__ void __launch_bounds__(Cfg::NT) head_tile_kernel(TileArgs g) {
             *reinterpret_cast<float*>(region + rl * L::ROW + (32 * j + lr) * 4) =
                 dz(acc[i][j][r] + b, row, wn * Cfg::TN + 32 * j + lr);
         }
+        if constexpr (P == 0) {
 #pragma unroll
-        for (int q = 0; q < 32 / RPI; ++q) {
-          const int rl = lane / CPRW + RPI * q, ch = lane % CPRW, row = wm * Cfg::TM + 32 * i + rl;
-          const float* from = reinterpret_cast<const float*>(region + rl * L::ROW) + ch * VE;
-          float v[VE], sum = 0.0f;
+          for (int q = 0; q < 32 / RPI; ++q) {
+            const int rl = lane / CPRW + RPI * q, ch = lane % CPRW, row = wm * Cfg::TM + 32 * i + rl;
+            const float* from = reinterpret_cast<const float*>(region + rl * L::ROW) + ch * 8;
+            float v[8], sum = 0.0f;
 #pragma unroll
-          for (int e = 0; e < VE; ++e) v[e] = from[e], sum += v[e];
+            for (int e = 0; e < 8; ++e) v[e] = from[e], sum += v[e];
 #pragma unroll
-          for (int o = CPRW / 2; o > 0; o >>= 1) sum += __shfl_down(sum, o, CPRW);
-          if (row >= rows) continue;
-          const int c = wn * Cfg::TN + ch * VE;
-          if (n0 + c < g.ldp) {
-            T w[VE];
-#pragma unroll
-            for (int e = 0; e < VE; ++e) w[e] = from_f32<T>(v[e]);
-            *reinterpret_cast<u32x4_any*>(static_cast<T*>(g.P) + (m0 + row) * g.ldp + n0 + c) =
-                *reinterpret_cast<const u32x4_any*>(w);
+            for (int o = CPRW / 2; o > 0; o >>= 1) sum += __shfl_down(sum, o, CPRW);
+            if (row >= rows) continue;
+            const int64_t n = n0 + wn * Cfg::TN + ch * 8;
+            if (n < g.ldp) store_parts<1>(static_cast<bf16*>(g.P) + (m0 + row) * g.ldp + n, 0, v);
+            if (g.dbias && ch == 0) put_sum(row, sum);
           }
-          if (g.dbias && ch == 0)
-            g.dbias[(static_cast<int64_t>(tile_col) * Cfg::WGN + wn) * g.classes + m0 + row] = sum;
+        } else {
+          // a row's chunks are no power of two
+#pragma unroll
+          for (int e0 = 0; e0 < 32 * CPRW; e0 += 64) {
+            const int rl = (e0 + lane) / CPRW, ch = (e0 + lane) % CPRW, row = wm * Cfg::TM + 32 * i + rl;
+            const float* from = reinterpret_cast<const float*>(region + rl * L::ROW) + ch * 8;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = from[e];
+            const int64_t n = n0 + wn * Cfg::TN + ch * 8;
+            if (row < rows && n < g.ldp) store_parts<P>(static_cast<bf16*>(g.P) + (m0 + row) * g.ldp + n, g.pplane, v);
+          }
+          const float* half = reinterpret_cast<const float*>(region + lr * L::ROW) + lh * (Cfg::TN / 2);
+          float sum = 0.0f;
+#pragma unroll
+          for (int e = 0; e < Cfg::TN / 2; ++e) sum += half[e];
+          sum += __shfl_xor(sum, 32);
+          const int row = wm * Cfg::TM + 32 * i + lr;
+          if (g.dbias && lh == 0 && row < rows) put_sum(row, sum);
         }
       }
     }
@@ -300,7 +327,13 @@ __global__ void __launch_bounds__(Cfg::NT) head_tile_kernel(TileArgs g) {
       for (int row = part; row < rows; row += PARTS) {
         const float p = dz(zt[row * ZLD + col], row, col);
         zt[row * ZLD + col] = p;
-        if (n0 + col < g.ldp) static_cast<T*>(g.P)[(m0 + row) * g.ldp + n0 + col] = from_f32<T>(p);
+        if (n0 + col < g.ldp) {
+          bf16 part[P > 0 ? P : 1];
+          split_parts(p, part);
+#pragma unroll
+          for (int u = 0; u < (P > 0 ? P : 1); ++u)
+            static_cast<bf16*>(g.P)[u * g.pplane + (m0 + row) * g.ldp + n0 + col] = part[u];
+        }
       }
       __syncthreads();
       if (g.dbias && t < rows) {
@@ -340,46 +373,68 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float2* __restrict
   }
 }
 
-// The kept rows of X with rows of ldp; columns without a label are 0 where they meet dz.
+// A matrix copied into dense rows of ld elements (a multiple of 8; zeros behind cols), as it
+// is or in parts.
+struct PackJob {
+  const void* src;
+  int64_t row_step, col_step;  // elements
+  int32_t rows, cols;
+  int64_t ld, plane;
+  void* out;
+  const int32_t* labels;       // columns without a label are zeros
+  int32_t classes;             // 0: no labels are looked at
+  uint32_t groups;
+};
 template <typename T>
-__global__ void __launch_bounds__(256) head_columns_kernel(const T* __restrict__ X, const int32_t* __restrict__ labels,
-                                                           int32_t classes, int32_t B, Kept in, int64_t ldp,
-                                                           T* __restrict__ Xc) {
-  constexpr int E = 16 / static_cast<int>(sizeof(T));
-  const int64_t per = ldp / E, total = per * in.kept, step = static_cast<int64_t>(gridDim.x) * 256;
-  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < total; at += step) {
-    const int64_t i = at / per, b = (at - i * per) * E;
-    const T* from = X + (in.offset + i * in.period) * B + b;
-    const int n = static_cast<int>(min<int64_t>(E, B - b));
-    u32x4 v = {0u, 0u, 0u, 0u};
-    if (n > 0) {
-      Chunk<T, E> c;
-      c.load(from, n);
-      v = c.raw;
-      if (classes > 0) {
+__device__ __forceinline__ void pack_load(const PackJob& j, int64_t r, int64_t c, float (&v)[8]) {
+  const T* from = static_cast<const T*>(j.src) + r * j.row_step + c * j.col_step;
+  const int n = static_cast<int>(min<int64_t>(8, j.cols - c));
+  if (j.col_step == 1) {
+    constexpr int E = 16 / static_cast<int>(sizeof(T));
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int32_t l = e < n && labels ? labels[b + e] : -1;
-          if (l >= 0 && l < classes) continue;
-          if constexpr (sizeof(T) == 2)
-            v[e / 2] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
-          else
-            v[e] = 0u;
-        }
-      }
+    for (int h = 0; h < 8 / E; ++h) {
+      Chunk<T, E> x{};
+      if (n > h * E) x.load(from + h * E, n - h * E);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[h * E + e] = x.at(e);
     }
-    *reinterpret_cast<u32x4_any*>(Xc + i * ldp + b) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(from[e * j.col_step]) : 0.0f;
+  }
+  if (j.classes > 0) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int32_t l = e < n ? j.labels[c + e] : -1;
+      if (l < 0 || l >= j.classes) v[e] = 0.0f;
+    }
   }
 }
-
-// dbias from the parts of the tile columns, in their order.
-__global__ void __launch_bounds__(256) head_bias_kernel(const float* __restrict__ part, int32_t parts, int32_t classes,
-                                                        float* __restrict__ dbias) {
-  const int64_t v = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (v >= classes) return;
-  float sum = 0.0f;
-  for (int q = 0; q < parts; ++q) sum += part[static_cast<int64_t>(q) * classes + v];
-  dbias[v] = sum;
+// Two chunks of a thread in flight: their loads would else wait for the stores between them.
+template <typename T, int P>
+__device__ __forceinline__ void pack_rows(const PackJob& j, int64_t block) {
+  const int64_t per = j.ld / 8, total = per * j.rows, step = static_cast<int64_t>(j.groups) * 256;
+  for (int64_t at = block * 256 + threadIdx.x; at < total; at += 2 * step) {
+    float v[2][8];
+    int64_t r[2], c[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t q = at + u * step;
+      r[u] = total < int64_t{1} << 31 ? static_cast<uint32_t>(q) / static_cast<uint32_t>(per) : q / per;
+      c[u] = (q - r[u] * per) * 8;
+      if (q < total) pack_load<T>(j, r[u], c[u], v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (at + u * step < total) store_parts<P>(static_cast<bf16*>(j.out) + r[u] * j.ld + c[u], j.plane, v[u]);
+  }
+}
+template <typename T, int P>
+__global__ void __launch_bounds__(256) head_pack_kernel(PackJob a, PackJob b) {
+  if (blockIdx.x < a.groups)
+    pack_rows<T, P>(a, blockIdx.x);
+  else
+    pack_rows<T, P>(b, blockIdx.x - a.groups);
 }
 
 // dX of the pieces: the first is kept in fp32, the next are added, the last is written out.
@@ -398,15 +453,285 @@ __global__ void __launch_bounds__(256) head_add_kernel(float* __restrict__ all, 
   }
 }
 
-// Zeros in the rows (by columns: the columns) of dropped inputs of an array of rows x cols.
-template <typename T>
-__global__ void __launch_bounds__(256) head_clear_kernel(T* __restrict__ p, int64_t rows, int64_t cols, Kept in,
-                                                         bool by_columns) {
-  const int64_t total = rows * cols, step = static_cast<int64_t>(gridDim.x) * 256;
-  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < total; at += step) {
-    const int64_t r = at / cols, x = by_columns ? at - r * cols : r;
-    if (static_cast<int32_t>(x % in.period) != in.offset) p[at] = from_f32<T>(0.0f);
+// What is left behind the products: dbias from the parts of the tile columns, in their
+// order, and zeros in the rows of dropped inputs.
+struct ClearJob {
+  char* p;
+  int64_t row_bytes;  // a multiple of 2
+  int64_t pieces;     // of 4 KB, of all dropped rows
+  Kept in;
+  uint32_t groups;
+};
+struct FinishArgs {
+  const float* part;
+  int32_t parts, classes;
+  float* dbias;
+  uint32_t bias_groups;
+  ClearJob a, b;
+};
+__device__ __forceinline__ void clear_rows(const ClearJob& j, int64_t block) {
+  typedef uint16_t u16_any __attribute__((may_alias));
+  const int64_t per = (j.row_bytes + 4095) / 4096;
+  for (int64_t at = block; at < j.pieces; at += j.groups) {
+    // dropped row d: one of the period - 1 residues but the kept one
+    const int64_t d = at / per, q = d / (j.in.period - 1);
+    const int32_t rem = static_cast<int32_t>(d - q * (j.in.period - 1));
+    const int64_t x = q * j.in.period + (rem < j.in.offset ? rem : rem + 1);
+    if (x >= j.in.n) continue;
+    const int64_t o = (at - d * per) * 4096 + threadIdx.x * 16, left = j.row_bytes - o;
+    char* p = j.p + x * j.row_bytes + o;
+    if (left >= 16) {
+      *reinterpret_cast<u32x4_any2*>(p) = u32x4{0u, 0u, 0u, 0u};
+    } else {
+      for (int e = 0; e < left; e += 2) *reinterpret_cast<u16_any*>(p + e) = 0;
+    }
   }
+}
+__global__ void __launch_bounds__(256) head_finish_kernel(FinishArgs g) {
+  uint32_t block = blockIdx.x;
+  if (block < g.bias_groups) {
+    const int64_t v = static_cast<int64_t>(block) * 256 + threadIdx.x;
+    if (v >= g.classes) return;
+    float sum = 0.0f;
+    for (int q = 0; q < g.parts; ++q) sum += g.part[static_cast<int64_t>(q) * g.classes + v];
+    g.dbias[v] = sum;
+    return;
+  }
+  block -= g.bias_groups;
+  if (block < g.a.groups)
+    clear_rows(g.a, block);
+  else
+    clear_rows(g.b, block - g.a.groups);
+}
+
+// Rows of all inputs from those of the kept ones (rows of ldk): zeros in between. Whole rows
+// are written once; the product writing its columns period elements apart and a pass for
+// the zeros behind it write every line twice in pieces.
+template <typename G>
+__global__ void __launch_bounds__(256) head_expand_kernel(const G* __restrict__ from, int64_t ldk, int64_t rows, Kept in,
+                                                          G* __restrict__ to) {
+  const int64_t per = (static_cast<int64_t>(in.n) + 7) / 8, total = per * rows, step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < total; at += step) {
+    const int64_t r = total < int64_t{1} << 31 ? static_cast<uint32_t>(at) / static_cast<uint32_t>(per) : at / per;
+    const int32_t c = static_cast<int32_t>(at - r * per) * 8, n = min(8, in.n - c);
+    uint32_t q = static_cast<uint32_t>(c) / static_cast<uint32_t>(in.period);
+    int32_t rem = c - static_cast<int32_t>(q) * in.period;
+    const G* f = from + r * ldk;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = e < n && rem == in.offset ? to_f32(f[q]) : 0.0f;
+      if (++rem == in.period) rem = 0, ++q;
+    }
+    G* o = to + r * in.n + c;
+    constexpr int E = 16 / static_cast<int>(sizeof(G));
+#pragma unroll
+    for (int h = 0; h < 8 / E; ++h) {
+      float w[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) w[e] = v[h * E + e];
+      if (n > h * E) store_chunk<G, E>(o + h * E, w, n - h * E);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ few classes
+// A workgroup takes 16 columns and every class and input: its waves share the inputs, their
+// sums meet in LDS, and what follows from a column's logits (loss, dz) is at hand in the same
+// workgroup, dX as well. Products on the fp32 matrix instructions of 16 x 16 x 4, whose lanes
+// hold single values, so that weights and inputs of any layout and alignment are loaded as
+// they lie. fp32 with up to 32 classes; measured on MI355X against tiles on copies in parts,
+// loss alone, and with gradients: 10 classes, 1024 of 2048 inputs, input-major, batch 128:
+// 8.7, 25.7 us, tiles 20.8, 53.7; 32 classes, 4096 inputs, batch 4096: 28.6, 164, tiles 70,
+// 224; 32 classes, 784 inputs, batch 128: 8.9, 29.9, tiles 19.7, 49.2.
+// bf16, whose tiles need no copies, loses with it (10 classes, 4096 inputs, batch 4096: 29.8
+// us, tiles 15.8).
+constexpr int kFewClasses = 32, kFewCols = 16, kFewWaves = 16;
+struct FewArgs {
+  int32_t B, V;
+  Kept in;
+  bool zero;
+  int32_t shares;      // workgroups of 16 columns: each takes a share of dX's rows (the sums are taken by all)
+  const float* X;      // the first kept row
+  const float* W;      // the first kept input
+  int64_t wv, wk;      // elements from a class, from a kept input to the next
+  bool whole;          // four inputs of a class lie together, on 16 bytes
+  const float* bias;
+  const int32_t* labels;
+  float* loss;         // forward
+  float* stats;
+  const float* dloss;  // backward
+  float* dX;           // or NULL
+  float* P;            // dz [V][ldp] and the inputs of the columns with a label [kept][ldp], for dW; or NULL
+  float* Xc;
+  int64_t ldp;
+  float* dbias;        // [workgroups][V], or NULL
+};
+
+template <int VB, int WAY>
+__global__ void __launch_bounds__(64 * kFewWaves) head_few_kernel(FewArgs g) {
+  __shared__ float red[kFewWaves * VB * 256];
+  __shared__ float zs[VB * 16 * 17], es[VB * 16 * 17];
+  constexpr int U = VB == 2 && WAY == WAY_GRAD ? 3 : 4;  // 16 inputs each in flight, as the registers allow
+  const int t = static_cast<int>(threadIdx.x), lane = t & 63, wave = t >> 6, lc = lane & 15, lg = lane >> 4;
+  const int at = xcd_position(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+  const int block = at / g.shares, share = at - block * g.shares;
+  const int64_t n = static_cast<int64_t>(block) * kFewCols + lc;
+  const int64_t nc = n < g.B ? n : g.B - 1;
+  const float* X = g.X + nc;
+  const float* W = g.W;
+  const int64_t xk = static_cast<int64_t>(g.B) * g.in.period;
+  const int K = g.in.kept, chunks = (K + 15) / 16;
+  const int32_t label = n < g.B ? g.labels[n] : -1;
+  const bool on = label >= 0 && label < g.V;
+  f32x4 acc[VB];
+#pragma unroll
+  for (int b = 0; b < VB; ++b) acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int c0 = wave; c0 < chunks; c0 += kFewWaves * U) {
+    float a[U][VB][4], x[U][4];  // of inputs past the last one: the last one's, and 0 below
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t k = min(16 * (c0 + kFewWaves * u) + 4 * lg + j, K - 1);
+        x[u][j] = X[k * xk];
+        if (g.whole) continue;
+#pragma unroll
+        for (int b = 0; b < VB; ++b) a[u][b][j] = W[min(16 * b + lc, g.V - 1) * g.wv + k * g.wk];
+      }
+    if (g.whole) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int b = 0; b < VB; ++b) {
+          const int64_t k = min(16 * (c0 + kFewWaves * u) + 4 * lg, K - 4);
+          const f32x4 w = *reinterpret_cast<const f32x4*>(W + min(16 * b + lc, g.V - 1) * g.wv + k);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) a[u][b][j] = w[j];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool mine = WAY == WAY_GRAD && (c0 + kFewWaves * u) / kFewWaves % g.shares == share;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t k = 16 * (c0 + kFewWaves * u) + 4 * lg + j;
+        const float xv = k < K ? x[u][j] : 0.0f;
+        if constexpr (WAY == WAY_GRAD) {
+          if (g.Xc && mine && k < K && n < g.ldp) g.Xc[k * g.ldp + n] = on ? x[u][j] : 0.0f;
+        }
+#pragma unroll
+        for (int b = 0; b < VB; ++b)
+          acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k < K ? a[u][b][j] : 0.0f, xv, acc[b], 0, 0, 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < VB; ++b)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) red[(wave * VB + b) * 256 + r * 64 + lane] = acc[b][r];
+  __syncthreads();
+  if (t < VB * 256) {
+    const int b = t >> 8, r = (t >> 6) & 3, v = 16 * b + 4 * lg + r;
+    float z = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) z += red[w * VB * 256 + t];
+    zs[v * 17 + lc] = v < g.V ? z + (g.bias ? g.bias[v] : 0.0f) : -kInf;
+  }
+  __syncthreads();
+  const int q = t >> 4;  // of the columns' threads: classes q and q + 16
+  if constexpr (WAY == WAY_LOSS) {
+    float m = -kInf;
+    if (t < 256) {
+      for (int v = 0; v < g.V; ++v) m = fmaxf(m, zs[v * 17 + lc]);
+      m = safe(m);
+#pragma unroll
+      for (int b = 0; b < VB; ++b) es[(16 * b + q) * 17 + lc] = expf(zs[(16 * b + q) * 17 + lc] - m);
+    }
+    __syncthreads();
+    if (t < 16 && n < g.B) {
+      float s = 0.0f;
+      for (int v = 0; v < g.V; ++v) s += es[v * 17 + lc];
+      g.loss[n] = on && s != 0.0f ? logf(s) - (zs[label * 17 + lc] - m) : 0.0f;
+      if (g.stats) {
+        g.stats[n] = m;
+        g.stats[g.B + n] = s != 0.0f ? 1.0f / s : 0.0f;
+      }
+    }
+  } else {
+    if (t < 256) {
+      float cm = 0.0f, inv = 0.0f, d = 0.0f;
+      if (on) {
+        cm = g.stats[n];
+        inv = g.stats[g.B + n];
+        d = g.dloss ? g.dloss[n] : 1.0f;
+      }
+#pragma unroll
+      for (int b = 0; b < VB; ++b) {
+        const int v = 16 * b + q;
+        float p = 0.0f;
+        if (inv != 0.0f && v < g.V) {  // 0: no label, or every class masked
+          p = expf(zs[v * 17 + lc] - cm) * (inv * d);
+          if (v == label) p -= d;
+        }
+        es[v * 17 + lc] = p;
+        if (g.P && share == 0 && v < g.V && n < g.ldp) g.P[v * g.ldp + n] = p;
+      }
+    }
+    __syncthreads();
+    if (g.dbias && share == 0 && t < g.V) {
+      float sum = 0.0f;
+      for (int c = 0; c < 16; ++c) sum += es[t * 17 + c];
+      g.dbias[static_cast<int64_t>(block) * g.V + t] = sum;
+    }
+    if (!g.dX) return;
+    float* dX = g.dX + n;
+    float dz[VB * 4];
+#pragma unroll
+    for (int s = 0; s < VB * 4; ++s) dz[s] = es[(4 * s + lg) * 17 + lc];
+    for (int c0 = share + g.shares * wave; c0 < chunks; c0 += g.shares * kFewWaves * U) {
+      float w[U][VB * 4];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int s = 0; s < VB * 4; ++s)
+          w[u][s] = W[min(4 * s + lg, g.V - 1) * g.wv + min(16 * (c0 + g.shares * kFewWaves * u) + lc, K - 1) * g.wk];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        f32x4 out = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < VB * 4; ++s)
+          out = __builtin_amdgcn_mfma_f32_16x16x4f32(4 * s + lg < g.V ? w[u][s] : 0.0f, dz[s], out, 0, 0, 0);
+        const int k0 = 16 * (c0 + g.shares * kFewWaves * u) + 4 * lg;
+        if (n >= g.B) continue;
+        float* at = dX + (g.in.offset + static_cast<int64_t>(k0) * g.in.period) * g.B;
+#pragma unroll
+        for (int r = 0; r < 4; ++r, at += xk) {
+          if (k0 + r >= K) continue;
+          *at = out[r];
+          if (g.zero) {
+            const int zeros = min(g.in.period, g.in.n - g.in.offset - (k0 + r) * g.in.period);
+            float* z = at;
+            for (int e = 1; e < zeros; ++e) *(z += g.B) = 0.0f;
+          }
+        }
+      }
+    }
+    if (g.zero && n < g.B && share == 0)
+      for (int64_t e = q; e < min(g.in.offset, g.in.n); e += 4 * kFewWaves) dX[e * g.B] = 0.0f;
+  }
+}
+
+template <int WAY>
+hipError_t run_few(FewArgs g, hipStream_t stream) {
+  const int64_t blocks = (static_cast<int64_t>(g.B) + kFewCols - 1) / kFewCols, rows = g.in.kept / (16 * kFewWaves);
+  g.shares = g.dX ? static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({4, rows, kTargetBlocks / blocks}))) : 1;
+  const dim3 grid(static_cast<unsigned>(blocks * g.shares)), threads(64 * kFewWaves);
+  if (g.V <= 16)
+    hipLaunchKernelGGL((head_few_kernel<1, WAY>), grid, threads, 0, stream, g);
+  else
+    hipLaunchKernelGGL((head_few_kernel<2, WAY>), grid, threads, 0, stream, g);
+  return hipGetLastError();
 }
 
 unsigned sweep(int64_t n) { return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(4096, (n + 255) / 256))); }
@@ -428,13 +753,17 @@ int check_desc(const ard_headloss_desc* d, HeadShape* s) {
   s->B = d->batch;
   s->V = d->classes;
   s->in = kept_of(d->in_plan, d->in_features);
-  s->ldp = up8(s->B);
-  s->ldc = up8(s->in.kept);
   s->es = d->dtype == ARD_BF16 ? 2 : 4;
   s->input_major = d->weight_layout == ARD_WEIGHTS_INPUT_MAJOR;
   s->zero = d->dropped == ARD_DROPPED_ZERO;
-  s->copy_w = s->in.kept > 0 && !s->input_major && (s->in.period > 1 || s->in.n * s->es % 16);
-  s->copy_x = s->in.kept > 0 && s->B * s->es % 16;
+  s->few = s->es == 4 && s->V <= kFewClasses;
+  s->parts = !s->few && s->es == 4;
+  s->ldp = up8(s->B);
+  s->wrows = s->input_major ? s->in.kept : s->V;
+  s->ldc = up8(s->input_major ? s->V : s->in.kept);
+  const bool any = s->in.kept > 0 && !s->few;
+  s->copy_w = any && (s->parts || (s->input_major ? s->V % 8 != 0 : s->in.period > 1 || s->in.n % 8 != 0));
+  s->copy_x = any && (s->parts || s->B % 8 != 0);
   return ARD_OK;
 }
 
@@ -442,7 +771,7 @@ int check_desc(const ard_headloss_desc* d, HeadShape* s) {
 constexpr int64_t kMostStride = int64_t{1} << 22;
 int check_strides(const HeadShape& s) {
   const int64_t x = s.copy_x ? s.ldp : static_cast<int64_t>(s.B) * s.in.period;
-  const int64_t w = s.input_major ? static_cast<int64_t>(s.V) * s.in.period : s.copy_w ? s.ldc : s.in.n;
+  const int64_t w = s.copy_w || s.few ? s.ldc : s.input_major ? static_cast<int64_t>(s.V) * s.in.period : s.in.n;
   if (x >= kMostStride || w >= kMostStride || s.ldp >= kMostStride)
     return fail(ARD_ERR_UNSUPPORTED, "rows of the inputs (%lld) and of the weights (%lld elements apart) must be below 2^22",
                 static_cast<long long>(x), static_cast<long long>(w));
@@ -451,68 +780,65 @@ int check_strides(const HeadShape& s) {
   return ARD_OK;
 }
 
-bool any_rows(const HeadShape& s) { return s.input_major && s.V * s.es % 16; }  // weights off 16 bytes in place
+// The tiles of the kernel, with their rates: flop/us of a compute unit (parts: of bf16 products) with as many
+// workgroups on it as it holds. Measured on MI355X over 12 sizes of each type, forward, batch 8 to 4096, 256 to 4096
+// inputs, 100 to 32000 classes: the pick takes at most 1.07 of the best tile's time (bf16 2048 x 256 to 2000: 12.9 and
+// 12.1 us), one tile for all up to 5 times (256 x 256 for 64 x 4096 to 1000: 76 us, 32 x 32 15; that for 512 x 1024 to
+// 32000: 199 us, 256 x 256 42).
+struct HeadTile {
+  int bm, bn, bk, wgn, per;
+  double rate;
+};
+template <class Cfg>
+constexpr HeadTile head_tile(int per, double rate) {
+  return {Cfg::BM, Cfg::BN, Cfg::BK, Cfg::KSPLIT == 1 ? Cfg::WGN : 1, per, rate};
+}
+using HeadMid = FastCfg<bf16, 64, 128, 64, 3, 2, 2, 1>;  // 72 KB, 4 waves
+constexpr HeadTile kTiles[] = {
+    head_tile<FastCfgs<bf16>::Huge>(1, 4.2e6), head_tile<FastCfgs<bf16>::Wide>(1, 3.5e6),
+    head_tile<FastCfgs<bf16>::Tall>(1, 3.4e6), head_tile<FastCfgs<bf16>::Big>(1, 2.7e6),
+    head_tile<HeadMid>(2, 2.4e6),              head_tile<FastCfgs<bf16>::Small>(2, 0.7e6),
+    head_tile<PartsCfgs<3>::C256>(1, 4.9e6),   head_tile<PartsCfgs<3>::C192>(1, 4.6e6),
+    head_tile<PartsCfgs<3>::C128>(1, 3.8e6),   head_tile<PartsCfgs<3>::C64>(1, 3.2e6)};
+constexpr int kFirstParts = 6, kAllTiles = 10;
+template <class F>
+hipError_t with_tile(int kind, F f) {
+  using std::integral_constant;
+  switch (kind) {
+    case 0: return f(FastCfgs<bf16>::Huge{}, integral_constant<int, 0>{});
+    case 1: return f(FastCfgs<bf16>::Wide{}, integral_constant<int, 0>{});
+    case 2: return f(FastCfgs<bf16>::Tall{}, integral_constant<int, 0>{});
+    case 3: return f(FastCfgs<bf16>::Big{}, integral_constant<int, 0>{});
+    case 4: return f(HeadMid{}, integral_constant<int, 0>{});
+    case 5: return f(FastCfgs<bf16>::Small{}, integral_constant<int, 0>{});
+    case 6: return f(PartsCfgs<3>::C256{}, integral_constant<int, 3>{});
+    case 7: return f(PartsCfgs<3>::C192{}, integral_constant<int, 3>{});
+    case 8: return f(PartsCfgs<3>::C128{}, integral_constant<int, 3>{});
+    default: return f(PartsCfgs<3>::C64{}, integral_constant<int, 3>{});
+  }
+}
 
-// The tile with the least modelled time: rounds of the chip times a tile's work over the
-// rate that it reaches with the chip full (bf16), or the layers' cost model (fp32).
-template <typename T>
+// The tile with the least modelled time: rounds of the chip times a workgroup's slabs.
 int plan_tile(const HeadShape& s, int64_t M) {
   const int64_t K = s.in.kept;
-  int best = FAST_SMALL;
+  int best = 0;
   double best_t = 1e300;
-  if constexpr (sizeof(T) == 2) {
-    using C = FastCfgs<bf16>;
-    struct Tile {
-      int kind, bm, bn, bk;
-      double rate;
-    };
-    static constexpr Tile tiles[] = {{FAST_HUGE, 256, 256, C::Huge::BK, 4.2e12}, {FAST_WIDE, 128, 256, C::Wide::BK, 3.5e12},
-                                     {FAST_TALL, 256, 128, C::Tall::BK, 3.4e12}, {FAST_BIG, 128, 128, C::Big::BK, 2.7e12},
-                                     {FAST_SMALL, 32, 32, C::Small::BK, 0.5e12}};
-    for (const Tile& c : tiles) {
-      if (any_rows(s) && c.kind != FAST_BIG && c.kind != FAST_SMALL) continue;
-      const int64_t n = (M + c.bm - 1) / c.bm * ((s.B + c.bn - 1) / c.bn), slabs = (K + c.bk - 1) / c.bk;
-      const double occ = n < kTargetBlocks ? static_cast<double>(n) / kTargetBlocks : 1.0;
-      const double t = static_cast<double>((n + kTargetBlocks - 1) / kTargetBlocks) * 2.0 * c.bm * c.bn * c.bk * slabs /
-                       (c.rate * (1.0 + 0.3 * (1.0 - occ)));
-      if (t < best_t) best_t = t, best = c.kind;
-    }
-  } else {
-    for (const CostF32& c : any_rows(s) ? kCostRegF32[1] : kCostF32) {
-      if (c.kind != FAST_HUGE && c.kind != FAST_MID && c.kind != FAST_SMALL) continue;
-      if (any_rows(s) && c.kind == FAST_HUGE) continue;
-      const double t = time_f32(c, tile_f32(c.kind), static_cast<int>(M), s.B, static_cast<int>(K), 1, 1, 1);
-      if (t < best_t) best_t = t, best = c.kind;
-    }
+  for (int kind = s.parts ? kFirstParts : 0; kind < (s.parts ? kAllTiles : kFirstParts); ++kind) {
+    const HeadTile& c = kTiles[kind];
+    const int64_t n = (M + c.bm - 1) / c.bm * ((s.B + c.bn - 1) / c.bn), slabs = (K + c.bk - 1) / c.bk;
+    const int64_t rounds = (n + kTargetBlocks * c.per - 1) / (kTargetBlocks * c.per);
+    // workgroups that share a compute unit take its rate between them
+    const double share = n >= kTargetBlocks * c.per ? c.per : std::max(1.0, static_cast<double>(n) / kTargetBlocks);
+    const double t = rounds * (2.0 + share * 2.0 * c.bm * c.bn * c.bk * slabs * (s.parts ? 6 : 1) / c.rate);
+    if (t < best_t) best_t = t, best = kind;
   }
   return best;
 }
 
-struct TileDims {
-  int bm, bn, wgn;
-};
-template <typename T>
-TileDims dims_of(int kind) {
-  auto of = [](auto cfg) {
-    using C = decltype(cfg);
-    return TileDims{C::BM, C::BN, C::KSPLIT == 1 ? C::WGN : 1};
-  };
-  using C = FastCfgs<T>;
-  if (kind == FAST_HUGE) return of(typename C::Huge{});
-  if constexpr (sizeof(T) == 2) {
-    if (kind == FAST_WIDE) return of(typename C::Wide{});
-    if (kind == FAST_TALL) return of(typename C::Tall{});
-    if (kind == FAST_BIG) return of(typename C::Big{});
-  } else {
-    if (kind == FAST_MID) return of(typename C::Mid{});
-  }
-  return of(typename C::Small{});
-}
-
-template <class Cfg, bool AMC, int LD, int WAY>
+template <class Cfg, int P, bool AMC, int WAY>
 hipError_t launch_tile(const TileArgs& g, hipStream_t stream) {
-  auto kern = head_tile_kernel<Cfg, AMC, LD, WAY>;
-  constexpr int LDS = HeadLds<Cfg>::bytes(WAY, LD);
+  auto kern = head_tile_kernel<Cfg, P, AMC, WAY>;
+  constexpr int LDS = HeadLds<Cfg>::bytes(WAY);
   static const hipError_t attr =
       hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return attr;
@@ -522,31 +848,13 @@ hipError_t launch_tile(const TileArgs& g, hipStream_t stream) {
   hipLaunchKernelGGL(kern, grid, dim3(Cfg::NT), LDS, stream, g);
   return hipGetLastError();
 }
-
-template <typename T, int WAY>
+template <int WAY>
 hipError_t run_tile(const HeadShape& s, int kind, const TileArgs& g, hipStream_t stream) {
-  using C = FastCfgs<T>;
-  auto go = [&](auto cfg) {
+  return with_tile(kind, [&](auto cfg, auto parts) {
     using Cfg = decltype(cfg);
-    return s.input_major ? launch_tile<Cfg, true, LOAD_DMA, WAY>(g, stream) : launch_tile<Cfg, false, LOAD_DMA, WAY>(g, stream);
-  };
-  if (any_rows(s)) {
-    if constexpr (sizeof(T) == 2) {
-      if (kind == FAST_BIG) return launch_tile<typename C::Big, true, LOAD_ANY, WAY>(g, stream);
-    } else {
-      if (kind == FAST_MID) return launch_tile<typename C::Mid, true, LOAD_ANY, WAY>(g, stream);
-    }
-    return launch_tile<typename C::Small, true, LOAD_ANY, WAY>(g, stream);
-  }
-  if (kind == FAST_HUGE) return go(typename C::Huge{});
-  if constexpr (sizeof(T) == 2) {
-    if (kind == FAST_WIDE) return go(typename C::Wide{});
-    if (kind == FAST_TALL) return go(typename C::Tall{});
-    if (kind == FAST_BIG) return go(typename C::Big{});
-  } else {
-    if (kind == FAST_MID) return go(typename C::Mid{});
-  }
-  return go(typename C::Small{});
+    constexpr int P = decltype(parts)::value;
+    return s.input_major ? launch_tile<Cfg, P, true, WAY>(g, stream) : launch_tile<Cfg, P, false, WAY>(g, stream);
+  });
 }
 
 // Classes of a piece of the backward: dz of at most 128 MB, whole tiles.
@@ -556,147 +864,235 @@ int64_t piece_of(const HeadShape& s) {
   return std::min<int64_t>(s.V, ((s.V + pieces - 1) / pieces + 255) / 256 * 256);
 }
 
+// Bytes of a copy of rows x ld: in three bf16 parts, or as it is.
+size_t copy_bytes(const HeadShape& s, int64_t rows, int64_t ld) {
+  return al256(static_cast<size_t>(rows) * ld * (s.parts ? 6 : s.es));
+}
+bool expands(const HeadShape& s) { return s.zero && !s.input_major && s.in.period > 1; }
+
 // The workspace. fwd: copies, the tiles' pairs, the labels' logits. bwd: copies, dz of a piece, row sums, dX of the
-// pieces, the products' partial sums.
+// pieces, dW of the kept inputs of a piece, the products' partial sums.
 struct FwdSpace {
   size_t wc, xc, part, zl;
   size_t bytes() const { return wc + xc + part + zl; }
 };
 struct BwdSpace {
-  size_t wc, xc, p, db, dx, part;
-  size_t bytes() const { return wc + xc + p + db + 2 * dx + part; }
+  size_t wc, xc, p, db, dx, dw, part;
+  size_t bytes() const { return wc + xc + p + db + 2 * dx + dw + part; }
 };
-template <typename T>
 FwdSpace fwd_space(const HeadShape& s) {
-  const TileDims t = dims_of<T>(plan_tile<T>(s, s.V));
-  return {s.copy_w ? al256(static_cast<size_t>(s.V) * s.ldc * s.es) : 0,
-          s.copy_x ? al256(static_cast<size_t>(s.in.kept) * s.ldp * s.es) : 0,
+  if (s.few) return {0, 0, 0, 0};
+  const HeadTile& t = kTiles[plan_tile(s, s.V)];
+  return {s.copy_w ? copy_bytes(s, s.wrows, s.ldc) : 0, s.copy_x ? copy_bytes(s, s.in.kept, s.ldp) : 0,
           al256(static_cast<size_t>((s.V + t.bm - 1) / t.bm) * s.B * 8), al256(static_cast<size_t>(s.B) * 4)};
 }
-template <typename T>
-BwdSpace bwd_space(const HeadShape& s) {
-  const int64_t piece = piece_of(s);
-  const TileDims t = dims_of<T>(plan_tile<T>(s, piece));
+size_t product_floats(const HeadShape& s, int M, int N, int K) {
+  return s.parts ? plan_parts<3>(M, N, K, false).floats : s.es == 2 ? partial_floats<bf16>(M, N, K) : partial_floats<float>(M, N, K);
+}
+int bias_parts(const HeadShape& s, int64_t piece) {
+  if (s.few) return static_cast<int>((static_cast<int64_t>(s.B) + kFewCols - 1) / kFewCols);
+  const HeadTile& t = kTiles[plan_tile(s, piece)];
+  return static_cast<int>((static_cast<int64_t>(s.B) + t.bn - 1) / t.bn * t.wgn);
+}
+BwdSpace bwd_space(const HeadShape& s, size_t gs) {
+  const int64_t piece = s.few ? s.V : piece_of(s);
   const int m = static_cast<int>(piece), last = static_cast<int>(s.V - (s.V - 1) / piece * piece), k = s.in.kept;
   size_t part = 0;
   if (k > 0)
     for (int v : {m, last}) {
-      part = std::max(part, partial_floats<T>(k, s.B, v));
-      part = std::max(part, s.input_major ? partial_floats<T>(k, v, s.B) : partial_floats<T>(v, k, s.B));
+      if (!s.few) part = std::max(part, product_floats(s, k, s.B, v));
+      part = std::max(part, s.input_major ? product_floats(s, k, v, s.B) : product_floats(s, v, k, s.B));
     }
-  return {s.copy_w ? al256(static_cast<size_t>(s.V) * s.ldc * s.es) : 0, al256(static_cast<size_t>(k) * s.ldp * s.es),
-          al256(static_cast<size_t>(piece) * s.ldp * s.es),
-          al256(static_cast<size_t>((s.B + t.bn - 1) / t.bn) * t.wgn * s.V * 4),
-          piece < s.V ? al256(static_cast<size_t>(k) * s.B * 4) : 0, al256(4 * part)};
+  return {s.copy_w ? copy_bytes(s, s.wrows, s.ldc) : 0, copy_bytes(s, k, s.ldp), copy_bytes(s, piece, s.ldp),
+          al256(static_cast<size_t>(bias_parts(s, piece)) * s.V * 4), piece < s.V ? al256(static_cast<size_t>(k) * s.B * 4) : 0,
+          expands(s) ? al256(static_cast<size_t>(piece) * up8(k) * gs) : 0, al256(4 * part)};
 }
 
-// The operands of the tile kernel from class v on.
+size_t space_bytes(const ard_headloss_desc* d, const HeadShape& s) {
+  return std::max(fwd_space(s).bytes(), bwd_space(s, d->grad_dtype == ARD_BF16 ? 2 : 4).bytes());
+}
+
+// The copies that the tile kernel reads: of W, of X (labels: for the backward).
 template <typename T>
-void tile_operands(const HeadShape& s, const void* W, const char* wc, const void* X, const char* xc, TileArgs* g) {
-  g->B = s.B;
-  g->K = s.in.kept;
-  g->classes = s.V;
-  if (s.input_major) {
-    g->W = static_cast<const T*>(W) + static_cast<int64_t>(s.in.offset) * s.V;
-    g->ldw = static_cast<int64_t>(s.V) * s.in.period;
-  } else {
-    g->W = s.copy_w ? static_cast<const void*>(wc) : W;
-    g->ldw = s.copy_w ? s.ldc : s.in.n;
+int pack(const HeadShape& s, const void* W, char* wc, const void* X, char* xc, const int32_t* labels, hipStream_t stream) {
+  constexpr int P = sizeof(T) == 4 ? 3 : 1;
+  auto groups = [](const PackJob& j) {
+    return static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>(4096, (j.rows * (j.ld / 8) + 511) / 512)));
+  };
+  PackJob w = {}, x = {};
+  if (s.copy_w) {
+    const int64_t p = s.in.period, o = s.in.offset;
+    w.src = static_cast<const T*>(W) + (s.input_major ? o * s.V : o);
+    w.row_step = s.input_major ? s.V * p : s.in.n;
+    w.col_step = s.input_major ? 1 : p;
+    w.rows = static_cast<int32_t>(s.wrows), w.cols = s.input_major ? s.V : s.in.kept;
+    w.ld = s.ldc, w.plane = s.wrows * s.ldc;
+    w.out = wc;
+    w.groups = groups(w);
   }
-  g->X = xc ? static_cast<const void*>(xc) : static_cast<const T*>(X) + static_cast<int64_t>(s.in.offset) * s.B;
-  g->ldx = xc ? s.ldp : static_cast<int64_t>(s.B) * s.in.period;
-}
-
-int copy_weights(const ard_headloss_desc* d, const HeadShape& s, const void* W, char* wc, void* stream) {
-  if (!s.copy_w) return ARD_OK;
-  ard_fc_desc fc = {};
-  fc.dtype = d->dtype;
-  fc.batch = 1;
-  fc.in_features = s.in.n;
-  fc.out_features = s.V;
-  fc.in_plan = d->in_plan;
-  fc.scale = 1.0f;
-  return ard_fc_compact_weights(&fc, W, wc, stream);
-}
-
-template <typename T>
-int copy_columns(const HeadShape& s, const void* X, const int32_t* labels, bool mask, char* xc, hipStream_t stream) {
-  if (s.in.kept == 0) return ARD_OK;
-  hipLaunchKernelGGL(head_columns_kernel<T>, dim3(sweep(s.in.kept * (s.ldp * static_cast<int64_t>(s.es) / 16))), dim3(256), 0,
-                     stream, static_cast<const T*>(X), labels, mask ? s.V : 0, s.B, s.in, s.ldp, reinterpret_cast<T*>(xc));
+  if (xc && s.in.kept > 0) {
+    x.src = static_cast<const T*>(X) + static_cast<int64_t>(s.in.offset) * s.B;
+    x.row_step = static_cast<int64_t>(s.B) * s.in.period, x.col_step = 1;
+    x.rows = s.in.kept, x.cols = s.B;
+    x.ld = s.ldp, x.plane = s.in.kept * s.ldp;
+    x.out = xc;
+    x.labels = labels, x.classes = labels ? s.V : 0;
+    x.groups = groups(x);
+  }
+  if (w.groups + x.groups == 0) return ARD_OK;
+  hipLaunchKernelGGL((head_pack_kernel<T, P>), dim3(w.groups + x.groups), dim3(256), 0, stream, w, x);
   ARD_LAUNCH_CHECK();
   return ARD_OK;
 }
 
+// The operands of the tile kernel from class 0 on.
 template <typename T>
-int fwd_impl(const ard_headloss_desc* d, const HeadShape& s, const void* Xt, const void* W, const float* bias,
-             const int32_t* labels, float* loss, float* stats, char* ws, hipStream_t stream) {
-  const FwdSpace sp = fwd_space<T>(s);
-  char *wc = ws, *xc = wc + sp.wc, *part = xc + sp.xc, *zl = part + sp.part;
-  int st = copy_weights(d, s, W, wc, stream);
-  if (st != ARD_OK) return st;
-  if (s.copy_x && (st = copy_columns<T>(s, Xt, labels, false, xc, stream)) != ARD_OK) return st;
+TileArgs tile_operands(const HeadShape& s, const void* W, const char* wc, const void* X, const char* xc) {
   TileArgs g = {};
-  tile_operands<T>(s, W, wc, Xt, s.copy_x ? xc : nullptr, &g);
+  g.B = s.B;
+  g.K = s.in.kept;
+  g.classes = s.V;
+  if (s.copy_w) {
+    g.W = wc, g.ldw = s.ldc, g.wplane = s.wrows * s.ldc;
+  } else if (s.input_major) {
+    g.W = static_cast<const T*>(W) + static_cast<int64_t>(s.in.offset) * s.V;
+    g.ldw = static_cast<int64_t>(s.V) * s.in.period;
+  } else {
+    g.W = W, g.ldw = s.in.n;
+  }
+  if (xc) {
+    g.X = xc, g.ldx = s.ldp, g.xplane = s.in.kept * s.ldp;
+  } else {
+    g.X = static_cast<const T*>(X) + static_cast<int64_t>(s.in.offset) * s.B;
+    g.ldx = static_cast<int64_t>(s.B) * s.in.period;
+  }
+  return g;
+}
+
+FewArgs few_args(const HeadShape& s, const void* X, const void* W, const float* bias, const int32_t* labels) {
+  FewArgs g = {};
+  g.B = s.B, g.V = s.V, g.in = s.in, g.zero = s.zero;
+  g.X = static_cast<const float*>(X) + static_cast<int64_t>(s.in.offset) * s.B;
+  g.W = static_cast<const float*>(W) + static_cast<int64_t>(s.in.offset) * (s.input_major ? s.V : 1);
+  g.wv = s.input_major ? 1 : s.in.n;
+  g.wk = static_cast<int64_t>(s.in.period) * (s.input_major ? s.V : 1);
+  g.whole = !s.input_major && s.in.period == 1 && s.in.n % 4 == 0;
+  g.bias = bias;
+  g.labels = labels;
+  g.ldp = s.ldp;
+  return g;
+}
+
+template <typename T>
+int fwd_impl(const HeadShape& s, const void* Xt, const void* W, const float* bias, const int32_t* labels, float* loss,
+             float* stats, char* ws, hipStream_t stream) {
+  if (s.few) {
+    FewArgs g = few_args(s, Xt, W, bias, labels);
+    g.loss = loss, g.stats = stats;
+    ARD_HIP_CHECK((run_few<WAY_LOSS>(g, stream)));
+    return ARD_OK;
+  }
+  const FwdSpace sp = fwd_space(s);
+  char *wc = ws, *xc = wc + sp.wc, *part = xc + sp.xc, *zl = part + sp.part;
+  const int st = pack<T>(s, W, wc, Xt, s.copy_x ? xc : nullptr, nullptr, stream);
+  if (st != ARD_OK) return st;
+  TileArgs g = tile_operands<T>(s, W, wc, Xt, s.copy_x ? xc : nullptr);
   g.M = s.V;
   g.bias = bias;
   g.labels = labels;
   g.part = reinterpret_cast<float2*>(part);
   g.zlabel = reinterpret_cast<float*>(zl);
-  const int kind = plan_tile<T>(s, s.V);
-  ARD_HIP_CHECK((run_tile<T, WAY_LOSS>(s, kind, g, stream)));
+  const int kind = plan_tile(s, s.V);
+  ARD_HIP_CHECK(run_tile<WAY_LOSS>(s, kind, g, stream));
   const int64_t groups = (static_cast<int64_t>(s.B) + 15) / 16;
-  const int bm = dims_of<T>(kind).bm;
+  const int bm = kTiles[kind].bm;
   hipLaunchKernelGGL(head_join_kernel<T>, dim3(static_cast<unsigned>(groups)), dim3(256), 0, stream, g.part, g.zlabel, labels,
                      s.B, s.V, (static_cast<int64_t>(s.V) + bm - 1) / bm, loss, stats);
   ARD_LAUNCH_CHECK();
   return ARD_OK;
 }
 
+// A product of A[M][K] (a_across: stored [K][M]) and B[K][N] (b_along: stored [N][K]), both as
+// bf16 matrices of rows lda, ldb, fp32 ones, or in parts, to rows of ldc with values cstep apart.
+struct Operand {
+  const void* p;
+  int64_t ld, plane;
+};
+template <typename T, bool AMC, bool BMC, typename OutT>
+hipError_t head_product(const HeadShape& s, int64_t M, int64_t N, int64_t K, Operand a, Operand b, OutT* c, int64_t ldc,
+                        int32_t cstep, float* partial, size_t floats, hipStream_t stream) {
+  if constexpr (sizeof(T) == 4) {
+    if (s.parts) {
+      PartsArgs g = {};
+      g.M = static_cast<int>(M), g.N = static_cast<int>(N), g.K = static_cast<int>(K);
+      g.a = {static_cast<const bf16*>(a.p), a.plane, a.ld};
+      g.b = {static_cast<const bf16*>(b.p), b.plane, b.ld};
+      g.epi = PARTS_FLOAT;
+      g.fout = c, g.ldo = ldc, g.fstep = cstep;
+      return run_parts_gemm<3, AMC, BMC>(g, partial, stream);
+    }
+  }
+  GemmArgs q = {};
+  q.M = static_cast<int>(M), q.N = static_cast<int>(N), q.K = static_cast<int>(K);
+  q.a = view(a.p, a.ld), q.b = view(b.p, b.ld);
+  q.c.p = c, q.c.ld = ldc, q.c.col_stride = cstep;
+  return product<T, AMC, BMC, OutT>(q, stream, partial, floats);
+}
+
 template <typename T, typename G>
-int bwd_impl(const ard_headloss_desc* d, const HeadShape& s, const void* Xt, const void* W, const float* bias,
-             const int32_t* labels, const float* stats, const float* dloss, void* dXt, void* dW, float* dbias, char* ws,
-             hipStream_t stream) {
-  const BwdSpace sp = bwd_space<T>(s);
-  char *wc = ws, *xc = wc + sp.wc, *p = xc + sp.xc, *db = p + sp.p, *all = db + sp.db, *one = all + sp.dx, *pt = one + sp.dx;
+int bwd_impl(const HeadShape& s, const void* Xt, const void* W, const float* bias, const int32_t* labels, const float* stats,
+             const float* dloss, void* dXt, void* dW, float* dbias, char* ws, hipStream_t stream) {
+  const BwdSpace sp = bwd_space(s, sizeof(G));
+  char *wc = ws, *xc = wc + sp.wc, *p = xc + sp.xc, *db = p + sp.p, *all = db + sp.db, *one = all + sp.dx, *dwk = one + sp.dx,
+       *pt = dwk + sp.dw;
   float* partial = reinterpret_cast<float*>(pt);
-  int st = copy_weights(d, s, W, wc, stream);
-  if (st != ARD_OK) return st;
-  if ((st = copy_columns<T>(s, Xt, labels, true, xc, stream)) != ARD_OK) return st;
-  const int64_t piece = piece_of(s), K = s.in.n, kin = s.in.kept;
-  const int kind = plan_tile<T>(s, piece);
-  const TileDims td = dims_of<T>(kind);
+  const size_t floats = sp.part / 4;
+  const int64_t piece = s.few ? s.V : piece_of(s), K = s.in.n, kin = s.in.kept, xplane = kin * s.ldp;
+  const int parts = bias_parts(s, piece);
+  float* sums = !dbias ? nullptr : parts == 1 ? dbias : reinterpret_cast<float*>(db);
   TileArgs base = {};
-  tile_operands<T>(s, W, wc, Xt, xc, &base);
-  base.labels = labels;
-  base.stats = stats;
-  base.dloss = dloss;
-  base.P = p;
-  base.ldp = s.ldp;
+  int kind = 0;
+  if (s.few) {
+    FewArgs g = few_args(s, Xt, W, bias, labels);
+    g.stats = const_cast<float*>(stats), g.dloss = dloss;
+    g.dX = static_cast<float*>(dXt);
+    if (dW) g.P = reinterpret_cast<float*>(p), g.Xc = reinterpret_cast<float*>(xc);
+    g.dbias = sums;
+    ARD_HIP_CHECK((run_few<WAY_GRAD>(g, stream)));
+  } else {
+    const int st = pack<T>(s, W, wc, Xt, xc, labels, stream);
+    if (st != ARD_OK) return st;
+    base = tile_operands<T>(s, W, wc, Xt, xc);
+    base.labels = labels;
+    base.stats = stats;
+    base.dloss = dloss;
+    base.P = p;
+    base.ldp = s.ldp;
+    kind = plan_tile(s, piece);
+  }
+  const size_t ws_es = s.parts ? 2 : s.es;  // of the copies
   for (int64_t v = 0; v < s.V; v += piece) {
+    const int64_t M = std::min<int64_t>(piece, s.V - v), pplane = M * s.ldp;
     TileArgs g = base;
-    g.M = std::min<int64_t>(piece, s.V - v);
-    g.class0 = v;
-    g.W = static_cast<const T*>(base.W) + (s.input_major ? v : v * base.ldw);
-    g.bias = bias ? bias + v : nullptr;
-    g.dbias = dbias ? reinterpret_cast<float*>(db) + v : nullptr;
-    ARD_HIP_CHECK((run_tile<T, WAY_GRAD>(s, kind, g, stream)));
-    if (dXt && kin > 0) {
-      GemmArgs q = {};
-      q.M = static_cast<int>(kin), q.N = s.B, q.K = static_cast<int>(g.M);
-      q.a = view(g.W, g.ldw);
-      q.b = view(p, s.ldp);
-      const bool whole = piece >= s.V;
-      if (whole) {
-        q.c.p = static_cast<T*>(dXt) + static_cast<int64_t>(s.in.offset) * s.B;
-        q.c.ld = static_cast<int64_t>(s.B) * s.in.period;
-        ARD_HIP_CHECK((s.input_major ? product<T, false, true, T>(q, stream, partial, sp.part / 4)
-                                     : product<T, true, true, T>(q, stream, partial, sp.part / 4)));
+    if (!s.few) {
+      g.M = M;
+      g.class0 = v;
+      g.W = static_cast<const char*>(base.W) + (s.input_major ? v : v * base.ldw) * ws_es;
+      g.bias = bias ? bias + v : nullptr;
+      g.dbias = sums ? sums + v : nullptr;
+      g.pplane = pplane;
+      ARD_HIP_CHECK(run_tile<WAY_GRAD>(s, kind, g, stream));
+    }
+    const Operand dz = {p, s.ldp, pplane}, x = {xc, s.ldp, xplane}, w = {g.W, g.ldw, g.wplane};
+    if (dXt && kin > 0 && !s.few) {
+      auto to = [&](auto* c, int64_t ld) {
+        return s.input_major ? head_product<T, false, true>(s, kin, s.B, M, w, dz, c, ld, 1, partial, floats, stream)
+                             : head_product<T, true, true>(s, kin, s.B, M, w, dz, c, ld, 1, partial, floats, stream);
+      };
+      if (piece >= s.V) {
+        ARD_HIP_CHECK(to(static_cast<T*>(dXt) + static_cast<int64_t>(s.in.offset) * s.B, static_cast<int64_t>(s.B) * s.in.period));
       } else {
-        q.c.p = v == 0 ? all : one;
-        q.c.ld = s.B;
-        ARD_HIP_CHECK((s.input_major ? product<T, false, true, float>(q, stream, partial, sp.part / 4)
-                                     : product<T, true, true, float>(q, stream, partial, sp.part / 4)));
+        ARD_HIP_CHECK(to(reinterpret_cast<float*>(v == 0 ? all : one), s.B));
         if (v > 0) {
           hipLaunchKernelGGL(head_add_kernel<T>, dim3(sweep(kin * s.B)), dim3(256), 0, stream, reinterpret_cast<float*>(all),
                              reinterpret_cast<const float*>(one), s.B, s.in, v + piece >= s.V ? static_cast<T*>(dXt) : nullptr);
@@ -705,40 +1101,41 @@ int bwd_impl(const ard_headloss_desc* d, const HeadShape& s, const void* Xt, con
       }
     }
     if (dW && kin > 0) {
-      GemmArgs q = {};
-      const GemmOperand dz = view(p, s.ldp), x = view(xc, s.ldp);
+      G* out = static_cast<G*>(dW);
       if (s.input_major) {
-        q.M = static_cast<int>(kin), q.N = static_cast<int>(g.M), q.K = s.B;
-        q.a = x, q.b = dz;
-        q.c.p = static_cast<G*>(dW) + static_cast<int64_t>(s.in.offset) * s.V + v;
-        q.c.ld = static_cast<int64_t>(s.V) * s.in.period;
+        ARD_HIP_CHECK((head_product<T, false, false>(s, kin, M, s.B, x, dz, out + static_cast<int64_t>(s.in.offset) * s.V + v,
+                                                     static_cast<int64_t>(s.V) * s.in.period, 1, partial, floats, stream)));
+      } else if (!expands(s)) {
+        ARD_HIP_CHECK((head_product<T, false, false>(s, M, kin, s.B, dz, x, out + v * K + s.in.offset, K, s.in.period, partial,
+                                                     floats, stream)));
       } else {
-        q.M = static_cast<int>(g.M), q.N = static_cast<int>(kin), q.K = s.B;
-        q.a = dz, q.b = x;
-        q.c.p = static_cast<G*>(dW) + v * K + s.in.offset;
-        q.c.ld = K;
-        q.c.col_stride = s.in.period;
+        G* kept = reinterpret_cast<G*>(dwk);
+        ARD_HIP_CHECK((head_product<T, false, false>(s, M, kin, s.B, dz, x, kept, up8(kin), 1, partial, floats, stream)));
+        hipLaunchKernelGGL(head_expand_kernel<G>, dim3(sweep(M * ((K + 7) / 8))), dim3(256), 0, stream, kept, up8(kin), M, s.in,
+                           out + v * K);
+        ARD_LAUNCH_CHECK();
       }
-      ARD_HIP_CHECK((product<T, false, false, G>(q, stream, partial, sp.part / 4)));
     }
   }
-  if (dbias) {
-    const int parts = static_cast<int>((s.B + td.bn - 1) / td.bn) * td.wgn;
-    hipLaunchKernelGGL(head_bias_kernel, dim3(static_cast<unsigned>((static_cast<int64_t>(s.V) + 255) / 256)), dim3(256), 0, stream,
-                       reinterpret_cast<const float*>(db), parts, s.V, dbias);
-    ARD_LAUNCH_CHECK();
+  FinishArgs f = {};
+  if (dbias && parts > 1) {
+    f.part = sums, f.parts = parts, f.classes = s.V, f.dbias = dbias;
+    f.bias_groups = static_cast<uint32_t>((static_cast<int64_t>(s.V) + 255) / 256);
   }
+  auto clear = [&](void* q, int64_t row_bytes) {
+    ClearJob j = {static_cast<char*>(q), row_bytes, 0, s.in, 0};
+    j.pieces = (static_cast<int64_t>(s.in.n) + s.in.period - 1) / s.in.period * (s.in.period - 1) * ((row_bytes + 4095) / 4096);
+    j.groups = static_cast<uint32_t>(std::min<int64_t>(j.pieces, 4096));
+    return j;
+  };
   if (s.in.period > 1 && s.zero) {
-    if (dXt) {
-      hipLaunchKernelGGL(head_clear_kernel<T>, dim3(sweep(K * s.B)), dim3(256), 0, stream, static_cast<T*>(dXt), K,
-                         static_cast<int64_t>(s.B), s.in, false);
-      ARD_LAUNCH_CHECK();
-    }
-    if (dW) {
-      hipLaunchKernelGGL(head_clear_kernel<G>, dim3(sweep(K * s.V)), dim3(256), 0, stream, static_cast<G*>(dW),
-                         s.input_major ? K : s.V, s.input_major ? s.V : K, s.in, !s.input_major);
-      ARD_LAUNCH_CHECK();
-    }
+    if (dXt && !s.few) f.a = clear(dXt, s.B * static_cast<int64_t>(s.es));
+    if (dW && (s.input_major || kin == 0)) f.b = clear(dW, s.V * static_cast<int64_t>(sizeof(G)));
+  }
+  const uint32_t groups = f.bias_groups + f.a.groups + f.b.groups;
+  if (groups > 0) {
+    hipLaunchKernelGGL(head_finish_kernel, dim3(groups), dim3(256), 0, stream, f);
+    ARD_LAUNCH_CHECK();
   }
   return ARD_OK;
 }
@@ -753,8 +1150,7 @@ extern "C" {
 size_t ard_headloss_workspace_bytes(const ard_headloss_desc* desc) {
   HeadShape s;
   if (check_desc(desc, &s) != ARD_OK || check_strides(s) != ARD_OK) return 0;
-  return desc->dtype == ARD_BF16 ? std::max(fwd_space<bf16>(s).bytes(), bwd_space<bf16>(s).bytes())
-                                 : std::max(fwd_space<float>(s).bytes(), bwd_space<float>(s).bytes());
+  return space_bytes(desc, s);
 }
 
 int ard_headloss_fwd(const ard_headloss_desc* desc, const void* Xt, const void* W, const float* bias, const int32_t* labels,
@@ -765,12 +1161,12 @@ int ard_headloss_fwd(const ard_headloss_desc* desc, const void* Xt, const void* 
   if (st != ARD_OK) return st;
   if ((st = check_strides(s)) || (st = need_ptr(Xt, "Xt")) || (st = need_ptr(W, "W")) || (st = may_ptr(bias, "bias")) ||
       (st = need_ptr(labels, "labels")) || (st = need_ptr(loss, "loss")) || (st = may_ptr(stats, "stats")) ||
-      (st = check_space(desc->dtype == ARD_BF16 ? fwd_space<bf16>(s).bytes() : fwd_space<float>(s).bytes(), ws, ws_bytes)))
+      (st = check_space(space_bytes(desc, s), ws, ws_bytes)))
     return st;
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
-  return desc->dtype == ARD_BF16 ? fwd_impl<bf16>(desc, s, Xt, W, bias, labels, loss, stats, w, sm)
-                                 : fwd_impl<float>(desc, s, Xt, W, bias, labels, loss, stats, w, sm);
+  return desc->dtype == ARD_BF16 ? fwd_impl<bf16>(s, Xt, W, bias, labels, loss, stats, w, sm)
+                                 : fwd_impl<float>(s, Xt, W, bias, labels, loss, stats, w, sm);
 }
 
 int ard_headloss_bwd(const ard_headloss_desc* desc, const void* Xt, const void* W, const float* bias, const int32_t* labels,
@@ -783,14 +1179,14 @@ int ard_headloss_bwd(const ard_headloss_desc* desc, const void* Xt, const void* 
   if ((st = check_strides(s)) || (st = need_ptr(Xt, "Xt")) || (st = need_ptr(W, "W")) || (st = may_ptr(bias, "bias")) ||
       (st = need_ptr(labels, "labels")) || (st = need_ptr(stats, "stats")) || (st = may_ptr(dloss, "dloss")) ||
       (st = may_ptr(dXt, "dXt")) || (st = may_ptr(dW, "dW")) || (st = may_ptr(dbias, "dbias")) ||
-      (st = check_space(desc->dtype == ARD_BF16 ? bwd_space<bf16>(s).bytes() : bwd_space<float>(s).bytes(), ws, ws_bytes)))
+      (st = check_space(space_bytes(desc, s), ws, ws_bytes)))
     return st;
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
   if (desc->dtype == ARD_F32)
-    return bwd_impl<float, float>(desc, s, Xt, W, bias, labels, stats, dloss, dXt, dW, dbias, w, sm);
-  return desc->grad_dtype == ARD_BF16 ? bwd_impl<bf16, bf16>(desc, s, Xt, W, bias, labels, stats, dloss, dXt, dW, dbias, w, sm)
-                                      : bwd_impl<bf16, float>(desc, s, Xt, W, bias, labels, stats, dloss, dXt, dW, dbias, w, sm);
+    return bwd_impl<float, float>(s, Xt, W, bias, labels, stats, dloss, dXt, dW, dbias, w, sm);
+  return desc->grad_dtype == ARD_BF16 ? bwd_impl<bf16, bf16>(s, Xt, W, bias, labels, stats, dloss, dXt, dW, dbias, w, sm)
+                                      : bwd_impl<bf16, float>(s, Xt, W, bias, labels, stats, dloss, dXt, dW, dbias, w, sm);
 }
 
 }  // extern "C"
