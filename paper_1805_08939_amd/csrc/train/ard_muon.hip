@@ -22,6 +22,7 @@ struct Block {
   int32_t row_period, row_offset, col_period, col_offset;
   int64_t ld, ldg;
   int64_t ldx;                        // rows of the dense copies
+  int32_t width, row_pieces;          // of the passes over the block: threads on a row, pieces of a row
 };
 __device__ __forceinline__ int64_t place(const Block& b, int64_t i, int64_t j) {
   return (b.row_offset + i * b.row_period) * b.ld + b.col_offset + j * b.col_period;
@@ -29,21 +30,56 @@ __device__ __forceinline__ int64_t place(const Block& b, int64_t i, int64_t j) {
 
 constexpr int kNormBlocks = 1024;  // workgroups of the first pass, at most: one sum of squares each
 
+// The workgroups take pieces in turn: some columns of a row, or of several rows where a row
+// has fewer than 256. f(row, the thread's first column, its columns, their distance): up to four
+// of them, to be in flight together (64 x 8192 fp32, the whole update: 164 us with a row to a
+// workgroup and one place of a thread after the other, 150).
+template <class F>
+__device__ __forceinline__ void each_piece(const Block& b, F f) {
+  const int32_t len = ((b.C + b.row_pieces - 1) / b.row_pieces + b.width - 1) / b.width * b.width;
+  const int32_t t = static_cast<int32_t>(threadIdx.x), rows = 256 / b.width;
+  const int64_t pieces = static_cast<int64_t>(b.row_pieces) * ((b.R + rows - 1) / rows);
+  for (int64_t p = blockIdx.x; p < pieces; p += gridDim.x) {
+    const int64_t q = b.row_pieces == 1 ? p : p / b.row_pieces, i = q * rows + t / b.width;
+    const int32_t first = static_cast<int32_t>(p - q * b.row_pieces) * len, j0 = first + t % b.width;
+    const int32_t end = min(b.C, first + len);
+    if (i < b.R && j0 < end) f(i, j0, (end - j0 + b.width - 1) / b.width, b.width);
+  }
+}
+void plan_pieces(Block* b) {
+  b->width = 32;
+  while (b->width < 256 && b->width < b->C) b->width *= 2;
+  b->row_pieces = std::max(1, (b->C + 1023) / 1024);
+}
+unsigned piece_groups(const Block& b) {
+  const int64_t rows = 256 / b.width;
+  return static_cast<unsigned>(std::min<int64_t>((b.R + rows - 1) / rows * b.row_pieces, kNormBlocks));
+}
+
 // V and U, and the sum of U's squares of each workgroup, in 64 bits (momenta far below 1
 // have squares below the smallest fp32 number).
 __global__ void __launch_bounds__(256) muon_momentum_kernel(Block b, float* __restrict__ V, const float* __restrict__ dW,
                                                             float mu, bool nesterov, float* __restrict__ U,
                                                             double* __restrict__ sums) {
   double sum = 0.0;
-  for (int64_t i = blockIdx.x; i < b.R; i += gridDim.x)
-    for (int64_t j = threadIdx.x; j < b.C; j += 256) {
-      const int64_t at = place(b, i, j);
-      const float g = b.ldg > 0 ? dW[i * b.ldg + j] : dW[at];
-      const float v = mu * V[at] + g, u = nesterov ? g + mu * v : v;
-      V[at] = v;
-      U[i * b.ldx + j] = u;
-      sum += static_cast<double>(u) * u;
-    }
+  each_piece(b, [&](int64_t i, int32_t j0, int n, int32_t step_j) {
+    float g[4], v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) {
+        const int64_t at = place(b, i, j0 + step_j * e);
+        g[e] = b.ldg > 0 ? dW[i * b.ldg + j0 + step_j * e] : dW[at];
+        v[e] = V[at];
+      }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) {
+        const float w = mu * v[e] + g[e], u = nesterov ? g[e] + mu * w : w;
+        V[place(b, i, j0 + step_j * e)] = w;
+        U[i * b.ldx + j0 + step_j * e] = u;
+        sum += static_cast<double>(u) * u;
+      }
+  });
   __shared__ double red[4];
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_down(sum, o);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
@@ -83,11 +119,18 @@ __global__ void __launch_bounds__(256) muon_scale_kernel(Block b, const float* _
 template <typename T>
 __global__ void __launch_bounds__(256) muon_update_kernel(Block b, const float* __restrict__ X, T* __restrict__ W, float keep,
                                                           float step) {
-  for (int64_t i = blockIdx.x; i < b.R; i += gridDim.x)
-    for (int64_t j = threadIdx.x; j < b.C; j += 256) {
-      const int64_t at = place(b, i, j);
-      W[at] = from_f32<T>(keep * to_f32(W[at]) - step * X[i * b.ldx + j]);
-    }
+  each_piece(b, [&](int64_t i, int32_t j0, int n, int32_t step_j) {
+    float w[4], x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) {
+        w[e] = to_f32(W[place(b, i, j0 + step_j * e)]);
+        x[e] = X[i * b.ldx + j0 + step_j * e];
+      }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) W[place(b, i, j0 + step_j * e)] = from_f32<T>(keep * w[e] - step * x[e]);
+  });
 }
 
 // Momentum SGD of the kept outputs' bias.
@@ -127,7 +170,8 @@ int check_desc(const ard_fc_desc* d, MuonShape* s) {
     return fail(ARD_ERR_UNSUPPORTED, "input-major weights need every output kept (out_plan NULL or period 1)");
   const Kept &r = input_major ? in : out, &c = input_major ? out : in;
   s->b = {r.kept, c.kept, r.period, r.offset, c.period, c.offset, c.n,
-          d->weight_layout == ARD_WEIGHTS_COMPACT_GRAD ? up8(c.kept) : 0, up8(c.kept)};
+          d->weight_layout == ARD_WEIGHTS_COMPACT_GRAD ? up8(c.kept) : 0, up8(c.kept), 0, 0};
+  plan_pieces(&s->b);
   s->out = out;
   s->m = std::min(r.kept, c.kept);
   s->l = std::max(r.kept, c.kept);
@@ -177,11 +221,11 @@ int muon_impl(const MuonShape& s, const ard_muon_opts& o, void* W, float* V, con
   char* rest = ws + sp.u + 2 * sp.x + 2 * sp.a;
   double* sums = reinterpret_cast<double*>(rest);
   float* part = reinterpret_cast<float*>(rest + sp.sums);
-  const unsigned rows = static_cast<unsigned>(std::min(b.R, kNormBlocks));
-  hipLaunchKernelGGL(muon_momentum_kernel, dim3(rows), dim3(256), 0, stream, b, V, dW, o.momentum, o.nesterov != 0, Uf, sums);
+  const unsigned groups = piece_groups(b);
+  hipLaunchKernelGGL(muon_momentum_kernel, dim3(groups), dim3(256), 0, stream, b, V, dW, o.momentum, o.nesterov != 0, Uf, sums);
   ARD_LAUNCH_CHECK();
   const unsigned chunks = static_cast<unsigned>(std::min<int64_t>(2048, (xp / 8 + 255) / 256));
-  hipLaunchKernelGGL(muon_scale_kernel<P>, dim3(chunks), dim3(256), 0, stream, b, Uf, sums, static_cast<int>(rows), o.eps, X, xp);
+  hipLaunchKernelGGL(muon_scale_kernel<P>, dim3(chunks), dim3(256), 0, stream, b, Uf, sums, static_cast<int>(groups), o.eps, X, xp);
   ARD_LAUNCH_CHECK();
   const bool wide = b.R <= b.C;
   for (int it = 0; it < o.iterations; ++it) {
@@ -214,7 +258,7 @@ int muon_impl(const MuonShape& s, const ard_muon_opts& o, void* W, float* V, con
     }
     std::swap(X, Y);
   }
-  hipLaunchKernelGGL(muon_update_kernel<T>, dim3(rows), dim3(256), 0, stream, b, Uf, static_cast<T*>(W),
+  hipLaunchKernelGGL(muon_update_kernel<T>, dim3(groups), dim3(256), 0, stream, b, Uf, static_cast<T*>(W),
                      static_cast<float>(1.0 - static_cast<double>(o.lr) * o.weight_decay),
                      static_cast<float>(o.lr * s.stretch));
   ARD_LAUNCH_CHECK();
