@@ -670,7 +670,7 @@ int ard_linattn_step(const ard_linattn_desc* desc, const void* Qt, const void* K
  *   dX = dS + inv (u - xh mean_k(u xh)),  dgain_k = sum_b dY_k xh_k
  * dSt (NULL = 0) is the gradient that reaches s past the norm; dX is that of x
  * and of r. dXt and dgain may be NULL. Outputs may be inputs of the same shape
- * (the same buffer, whole), but St is not Yt.
+ * (the same buffer, whole), but St is not Yt and dgain not gain.
  */
 typedef struct {
   int32_t dtype;
@@ -707,10 +707,12 @@ int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* g
  * reaches no gradient. Classes are masked by a bias of -inf: they have no
  * probability and no gradient, but as a label an infinite loss, with the
  * gradient of the formula. A column whose logits are all -inf has loss and
- * gradient 0. NaN propagates within its column, and from there to dW.
+ * gradient 0. NaN propagates within its column, and from there to dW; with fp32
+ * operands an infinite value in Xt or W makes NaN where it is multiplied.
  * fwd: stats[2][B] (may be NULL) is kept for the backward.
- * bwd: dloss NULL = 1; dXt, dW and dbias may be NULL. dW is of grad_dtype:
- * ARD_F32, as ard_fc_sgd_momentum and ard_fc_muon read it, or dtype.
+ * bwd: dloss NULL = 1; dXt, dW and dbias may be NULL and share no memory with an
+ * input. dW is of grad_dtype: ARD_F32, as ard_fc_sgd_momentum and ard_fc_muon read
+ * it, or dtype.
  */
 typedef struct {
   int32_t dtype;

@@ -1181,6 +1181,8 @@ int ard_headloss_bwd(const ard_headloss_desc* desc, const void* Xt, const void* 
       (st = may_ptr(dXt, "dXt")) || (st = may_ptr(dW, "dW")) || (st = may_ptr(dbias, "dbias")) ||
       (st = check_space(space_bytes(desc, s), ws, ws_bytes)))
     return st;
+  if (dXt == Xt || dW == W || (dbias && (dbias == bias || dbias == dloss)))
+    return fail(ARD_ERR_INVALID_ARG, "a gradient is in the buffer of an input");
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
   if (desc->dtype == ARD_F32)

@@ -548,6 +548,7 @@ int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* g
       (st = need_ptr(dYt, "dYt")) || (st = may_ptr(dSt, "dSt")) || (st = may_ptr(dXt, "dXt")) ||
       (st = may_ptr(dgain, "dgain")) || (st = check_space(sp.part + sp.gain, ws, ws_bytes)))
     return st;
+  if (dgain && dgain == gain) return fail(ARD_ERR_INVALID_ARG, "dgain and gain are the same buffer");
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
   return desc->dtype == ARD_BF16 ? bwd_impl<bf16>(p, St, gain, inv_rms, dYt, dSt, dXt, dgain, w, sm)

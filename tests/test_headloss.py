@@ -72,6 +72,16 @@ def test_refuses_bad_calls():
     assert _ffi.lib().ard_headloss_workspace_bytes(None) == 0
 
 
+@pytest.mark.parametrize("classes", [6, 600])
+def test_refuses_gradients_in_the_inputs_buffers(classes):
+    X, W, b, labels, stats, dl, dX, dW, db = (4096 * (i + 1) for i in range(9))
+    d = api.headloss_desc(api.ARD_F32, 4, 8, classes)
+    for outs in ((X, dW, db), (dX, W, db), (dX, dW, b), (dX, dW, dl)):
+        with pytest.raises(api.ArdError) as e:
+            api.ard_headloss_bwd(d, X, W, b, labels, stats, dl, *outs, (1 << 20, 1 << 40), stream=0)
+        assert e.value.status == 1 and "buffer" in e.value.message
+
+
 # ---------------------------------------------------------------- the kernels
 
 def _fenced(t, dev):

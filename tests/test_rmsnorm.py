@@ -60,6 +60,15 @@ def test_refuses_bad_calls():
     refused(5, api.ard_rmsnorm_bwd, d, *good, (a, api.ard_rmsnorm_workspace_bytes(d) - 1))
 
 
+def test_refuses_the_gain_as_its_gradient():
+    """The gain is read again after the first gradients of it are written."""
+    a, b = 4096, 8192
+    d = api.rmsnorm_desc(api.ARD_F32, 4, 8)
+    with pytest.raises(api.ArdError) as e:
+        api.ard_rmsnorm_bwd(d, a, b, a, a, None, a, b, (a, 1 << 30), stream=0)
+    assert e.value.status == 1 and "dgain" in e.value.message
+
+
 # ---------------------------------------------------------------- the kernels
 
 def _inside(got, want, bound, what):
