@@ -11,7 +11,8 @@
 // order, between two launches. Sums over a column are held in 64 bits: a square of a
 // feature of 2^70 is infinite in 32, and the matrix of a norm has the memory for it anyway.
 // Where the second pass is a launch of its own its results go past the caches (NT), which
-// keeps the inputs there (bf16 8192 x 2048: forward 47.6 to 41.4 us, backward 57.4 to 54.2).
+// keeps the inputs there (bf16 8192 x 2048: forward 47.6 to 41.4 us, backward 57.4 to 54.2; from
+// its last row to the first: 52.9).
 // Bound by HBM.
 
 #include "ard_train.hpp"
@@ -50,6 +51,28 @@ __device__ __forceinline__ Place<VE> place_of(const NormShape& s, int32_t block)
   p.col = (static_cast<int64_t>(block) * s.lanes + p.lane) * VE;
   p.n = static_cast<int>(min<int64_t>(VE, s.B - p.col));
   return p;
+}
+
+// Rows of a thread from r0 to r1.
+template <int VE>
+__device__ __forceinline__ int64_t rows_of(const Place<VE>& p, int64_t r0, int64_t r1) {
+  const int64_t n = r1 - r0 - p.row;
+  return n > 0 ? (n + p.step - 1) / p.step : 0;
+}
+
+// The sum over `lanes` neighbouring threads (a power of two), in a fixed order, in the first
+// of them: exchanges within 16 without LDS.
+__device__ __forceinline__ float row_sum(float v, int lanes) {
+  auto add = [&](auto ctrl) {
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  if (lanes > 1) add(std::integral_constant<int, 0xb1>{});    // neighbours
+  if (lanes > 2) add(std::integral_constant<int, 0x4e>{});    // pairs
+  if (lanes > 4) add(std::integral_constant<int, 0x141>{});   // halves of 8
+  if (lanes > 8) add(std::integral_constant<int, 0x140>{});   // halves of 16
+  if (lanes > 16) v += __shfl_down(v, 16, lanes);
+  if (lanes > 32) v += __shfl_down(v, 32, lanes);
+  return v;
 }
 
 // Sums of the workgroup's columns over its threads, in a fixed order: v[e] of every thread
@@ -136,8 +159,10 @@ __device__ __forceinline__ void fwd_rows(const FwdArgs<T>& a, const Place<VE>& p
     if (a.S) store_chunk<T, VE, NT>(a.S + at, v, p.n);
     store_chunk<T, VE, NT>(a.Y + at, y, p.n);
   };
-  int64_t k = r0 + p.row;
-  for (; k + (U - 1) * p.step < r1; k += U * p.step) {
+  // from the last row to the first: the sums' pass has left the last ones in the L2
+  int64_t left = rows_of(p, r0, r1);
+  for (; left >= U; left -= U) {
+    const int64_t k = r0 + p.row + (left - U) * p.step;
     Chunk<T, VE> x[U], r[U];
     float g[U];
 #pragma unroll
@@ -150,8 +175,8 @@ __device__ __forceinline__ void fwd_rows(const FwdArgs<T>& a, const Place<VE>& p
 #pragma unroll
     for (int u = 0; u < U; ++u) put(x[u], r[u], g[u], (k + u * p.step) * a.s.B + p.col);
   }
-  for (; k < r1; k += p.step) {
-    const int64_t at = k * a.s.B + p.col;
+  for (; left > 0; --left) {
+    const int64_t k = r0 + p.row + (left - 1) * p.step, at = k * a.s.B + p.col;
     Chunk<T, VE> x, r;
     x.load(a.X + at, p.n);
     if (a.R) r.load(a.R + at, p.n);
@@ -268,7 +293,7 @@ __device__ __forceinline__ void bwd_sums(const BwdArgs<T>& a, const Place<VE>& p
       }
     }
     if (row_out) {  // uniform
-      for (int o = lanes / 2; o > 0; o >>= 1) along += __shfl_down(along, o, lanes);
+      along = row_sum(along, lanes);
       if (p.lane == 0 && on) row_out[k] = along;
     }
   };
@@ -308,8 +333,9 @@ __device__ __forceinline__ void bwd_rows(const BwdArgs<T>& a, const Place<VE>& p
     }
     store_chunk<T, VE, NT>(a.dX + at, v, p.n);
   };
-  int64_t k = r0 + p.row;
-  for (; k + (U - 1) * p.step < r1; k += U * p.step) {
+  int64_t left = rows_of(p, r0, r1);  // as in fwd_rows
+  for (; left >= U; left -= U) {
+    const int64_t k = r0 + p.row + (left - U) * p.step;
     Chunk<T, VE> x[U], d[U], r[U];
     float g[U];
 #pragma unroll
@@ -323,8 +349,8 @@ __device__ __forceinline__ void bwd_rows(const BwdArgs<T>& a, const Place<VE>& p
 #pragma unroll
     for (int u = 0; u < U; ++u) put(x[u], d[u], r[u], g[u], (k + u * p.step) * a.s.B + p.col);
   }
-  for (; k < r1; k += p.step) {
-    const int64_t at = k * a.s.B + p.col;
+  for (; left > 0; --left) {
+    const int64_t k = r0 + p.row + (left - 1) * p.step, at = k * a.s.B + p.col;
     Chunk<T, VE> x, d, r;
     x.load(a.S + at, p.n);
     d.load(a.dY + at, p.n);
