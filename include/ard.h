@@ -717,8 +717,8 @@ int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* g
 typedef struct {
   int32_t dtype;
   int32_t batch;          /* B: 1 .. 2^22 - 8 */
-  int32_t in_features;    /* K: 1 .. 2^22 - 8 */
-  int32_t classes;        /* V >= 1; input-major: V times the period below 2^22 */
+  int32_t in_features;    /* K >= 1; output-major: up to 2^22 - 8 kept ones */
+  int32_t classes;        /* V >= 1; input-major: up to 2^22 - 8 */
   const ard_row_plan* in_plan;  /* n == K (a list is not needed), or NULL = every input kept */
   int32_t weight_layout;  /* ARD_WEIGHTS_FULL or ARD_WEIGHTS_INPUT_MAJOR */
   int32_t dropped;        /* ARD_DROPPED_ZERO or ARD_DROPPED_SKIP */

@@ -737,6 +737,9 @@ hipError_t run_few(FewArgs g, hipStream_t stream) {
 unsigned sweep(int64_t n) { return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(4096, (n + 255) / 256))); }
 
 // ------------------------------------------------------------------ host
+// Elements between the rows of the tile kernel's operands: offsets within a slab and a tile have 32 bits.
+constexpr int64_t kMostStride = int64_t{1} << 22;
+
 int check_desc(const ard_headloss_desc* d, HeadShape* s) {
   if (!d) return fail(ARD_ERR_INVALID_ARG, "desc is NULL");
   if (d->dtype != ARD_F32 && d->dtype != ARD_BF16) return fail(ARD_ERR_UNSUPPORTED, "dtype %d not supported", d->dtype);
@@ -762,19 +765,15 @@ int check_desc(const ard_headloss_desc* d, HeadShape* s) {
   s->wrows = s->input_major ? s->in.kept : s->V;
   s->ldc = up8(s->input_major ? s->V : s->in.kept);
   const bool any = s->in.kept > 0 && !s->few;
-  s->copy_w = any && (s->parts || (s->input_major ? s->V % 8 != 0 : s->in.period > 1 || s->in.n % 8 != 0));
-  s->copy_x = any && (s->parts || s->B % 8 != 0);
+  auto in_place = [&](int64_t row) { return !s->parts && row % 8 == 0 && row * s->in.period < kMostStride; };
+  s->copy_w = any && !(s->input_major ? in_place(s->V) : s->in.period == 1 && in_place(s->in.n));
+  s->copy_x = any && !in_place(s->B);
   return ARD_OK;
 }
 
-// The strides of the tile kernel's operands: offsets within a slab and a tile have 32 bits.
-constexpr int64_t kMostStride = int64_t{1} << 22;
 int check_strides(const HeadShape& s) {
-  const int64_t x = s.copy_x ? s.ldp : static_cast<int64_t>(s.B) * s.in.period;
-  const int64_t w = s.copy_w || s.few ? s.ldc : s.input_major ? static_cast<int64_t>(s.V) * s.in.period : s.in.n;
-  if (x >= kMostStride || w >= kMostStride || s.ldp >= kMostStride)
-    return fail(ARD_ERR_UNSUPPORTED, "rows of the inputs (%lld) and of the weights (%lld elements apart) must be below 2^22",
-                static_cast<long long>(x), static_cast<long long>(w));
+  if (s.ldp >= kMostStride || s.ldc >= kMostStride)
+    return fail(ARD_ERR_UNSUPPORTED, "%d columns and rows of %lld weights must be below 2^22", s.B, static_cast<long long>(s.ldc));
   if ((s.V / 32 + int64_t{1}) * (s.B / 32 + int64_t{1}) >= int64_t{1} << 31)  // tiles are counted in 32 bits
     return fail(ARD_ERR_UNSUPPORTED, "%d classes of %d columns are too many tiles", s.V, s.B);
   return ARD_OK;

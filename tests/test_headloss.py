@@ -218,6 +218,13 @@ def test_loss_and_gradients(size):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [("bf16", 2100000, 6, 33, 2, 1, FULL), ("bf16", 24, 8, 2100000, 2, 0, INPUT),
+                                  ("f32", 24, 8, 2100000, 2, 1, INPUT)], ids=lambda s: "-".join(map(str, s)))
+def test_kept_rows_more_than_2_22_elements_apart(size):
+    test_loss_and_gradients(size)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layout", [FULL, INPUT])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_dropped_inputs_left_as_they_are(dtype, layout):
