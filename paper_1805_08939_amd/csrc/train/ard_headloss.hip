@@ -6,8 +6,7 @@
 // exponentials a column; the tiles' pairs are joined by a second, small kernel. Backward:
 // the classes in pieces; the same product with an epilogue that writes dz of a piece (the
 // operand of two products; its row sums, the bias gradient, are taken before it is rounded
-// for that), then dX and dW from it. A piece's dz is a few ten MB, so that the products
-// find it in the memory-side cache. Logits are fp32 throughout.
+// for that), then dX and dW from it. Logits are fp32 throughout.
 //
 // bf16 operands are read in place where their rows start on 16 bytes, else from copies.
 // fp32 operands, dz among them, are copied into three bf16 parts (ard_parts_gemm.hpp):
@@ -884,9 +883,11 @@ hipError_t run_tile(const HeadShape& s, int kind, const TileArgs& g, hipStream_t
   });
 }
 
-// Classes of a piece of the backward: dz of at most 128 MB, whole tiles.
+// Classes of a piece of the backward, whole tiles: dz of at most 512 MB in bf16, 192 in parts. Measured on MI355X,
+// forward and backward, 128, 512 MB of bf16: 4096 x 4096 to 32000 3455, 3417 us, 16384 x 1024 to 32000 4481, 4206 (2 GB:
+// 4052); of parts for 128, 512 MB of fp32: 4096 x 1024 to 32000 5097, 5255.
 int64_t piece_of(const HeadShape& s) {
-  const int64_t most = std::max<int64_t>(256, (int64_t{128} << 20) / (s.ldp * static_cast<int64_t>(s.es)) / 256 * 256);
+  const int64_t most = std::max<int64_t>(256, (int64_t{s.parts ? 128 : 512} << 20) / (s.ldp * static_cast<int64_t>(s.es)) / 256 * 256);
   const int64_t pieces = (s.V + most - 1) / most;
   return std::min<int64_t>(s.V, ((s.V + pieces - 1) / pieces + 255) / 256 * 256);
 }

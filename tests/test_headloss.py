@@ -225,6 +225,13 @@ def test_kept_rows_more_than_2_22_elements_apart(size):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [("bf16", 90000, 16, 3500, 1, 0, FULL), ("bf16", 90009, 24, 3333, 2, 1, FULL),
+                                  ("bf16", 90008, 16, 3400, 2, 1, INPUT)], ids=lambda s: "-".join(map(str, s)))
+def test_gradients_of_several_pieces_in_bf16(size):
+    test_loss_and_gradients(size)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layout", [FULL, INPUT])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_dropped_inputs_left_as_they_are(dtype, layout):
