@@ -25,8 +25,8 @@
 namespace ard {
 namespace {
 
-// exp of a value <= 0; see the forward's roundings: bf16 logits are sums of products of
-// values with 8 bits, for which the hardware's power of two is exact enough by far.
+// exp of a value <= 0. With bf16 operands the hardware's power of two, one rounding off, of an
+// argument that is off by 2^-24 of itself: no more than the logits' own sums are.
 template <typename T>
 __device__ __forceinline__ float exp_neg(float x) {
   if constexpr (sizeof(T) == 2)

@@ -6,6 +6,10 @@
 // Each iteration applies the odd polynomial a s + b s^3 + c s^5 to the singular values of X
 // and leaves its singular vectors; |U| is the Frobenius norm, so that they start within 1.
 //
+// X, A and the polynomial are kept in bf16 parts (ard_parts_gemm.hpp): three for fp32 weights,
+// 2^-24 of a value; two for bf16 ones, 2^-16, where a step is then 2.5e-5 off and the weight
+// that takes it is rounded to 2^-8 of itself. Momentum, norm and the last X are fp32 and 64 bits.
+//
 // The kept block is gathered once, into a dense matrix. A and A^2 are symmetric, the third
 // product has the shape of the block. Bound by the matrix cores, for small blocks by the
 // latency of three products after one another.
