@@ -225,6 +225,34 @@ def test_kept_rows_more_than_2_22_elements_apart(size):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [
+    # 64 x 128 tiles of bf16
+    ("bf16", 331, 520, 5001, 1, 0, FULL), ("bf16", 1024, 300, 1000, 1, 0, INPUT), ("bf16", 331, 522, 5001, 1, 0, INPUT),
+    # 256 x 128 and 128 x 128 tiles of parts, in the products too
+    ("f32", 700, 1500, 8800, 2, 1, INPUT), ("f32", 703, 500, 6001, 1, 0, FULL), ("f32", 1500, 400, 2000, 1, 0, FULL),
+    ("f32", 1024, 64, 3100, 1, 0, INPUT),
+    # few classes: one and two blocks of 16, rows of weights on and off 16 bytes, shares of dX's rows, more inputs than
+    # a pass of the waves
+    ("f32", 37, 130, 32, 1, 0, FULL), ("f32", 16, 260, 17, 1, 0, FULL), ("f32", 100, 777, 20, 2, 1, INPUT),
+    ("f32", 20, 3000, 10, 1, 0, FULL), ("f32", 257, 1100, 25, 3, 2, FULL), ("f32", 5000, 300, 12, 1, 0, INPUT),
+    ("f32", 1, 1024, 16, 2, 0, FULL), ("f32", 48, 2500, 31, 4, 3, INPUT), ("f32", 17, 36, 3, 40, 39, FULL),
+], ids=lambda s: "-".join(map(str, s)))
+def test_further_tiles_and_few_classes(size):
+    test_loss_and_gradients(size)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", [FULL, INPUT])
+def test_few_classes_leave_dropped_inputs_and_masked_columns(layout):
+    _, _, _, labels, _, loss, dX, dW, _, kept = _run("f32", 40, 600, 10, 3, 1, layout, dropped=api.ARD_DROPPED_SKIP)
+    drop = torch.ones(600, dtype=torch.bool, device=dX.device)
+    drop[kept] = False
+    off = (labels < 0) | (labels >= 10)
+    assert (dX[drop] == 3).all() and (dW[:, drop] == 3).all()
+    assert off.any() and (loss[off] == 0).all() and (dX[kept][:, off] == 0).all() and not (dX[kept][:, ~off] == 0).any()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("size", [("bf16", 90000, 16, 3500, 1, 0, FULL), ("bf16", 90009, 24, 3333, 2, 1, FULL),
                                   ("bf16", 90008, 16, 3400, 2, 1, INPUT)], ids=lambda s: "-".join(map(str, s)))
 def test_gradients_of_several_pieces_in_bf16(size):

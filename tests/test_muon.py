@@ -214,6 +214,19 @@ def test_update(size, iterations, nesterov):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("iterations,nesterov", [(1, 0), (5, 1)])
+@pytest.mark.parametrize("size", [
+    # 256 x 256 and 192 x 192 tiles of two parts; 256 x 128, 192 x 192 and 128 x 128 of three, with and without splits
+    ("bf16", 4096, 4090, 1, 0, 1, 0, FULL), ("bf16", 3000, 3100, 1, 0, 1, 0, INPUT), ("f32", 2200, 2300, 1, 0, 1, 0, FULL),
+    ("f32", 1500, 3000, 1, 0, 1, 0, FULL), ("f32", 3000, 1300, 1, 0, 1, 0, FULL),
+    # few rows of many columns and the other way round
+    ("f32", 3, 70001, 1, 0, 1, 0, FULL), ("bf16", 70001, 5, 1, 0, 1, 0, FULL), ("f32", 20, 9000, 1, 0, 2, 1, COMPACT),
+], ids=lambda s: "-".join(map(str, s)))
+def test_update_of_further_blocks(size, iterations, nesterov):
+    test_update(size, iterations, nesterov)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_singular_values_of_the_update(dtype):
     """From no weights and lr 1 the new weights are the negated block: its singular values are near one, and those of
