@@ -1060,11 +1060,15 @@ hipError_t head_product(const HeadShape& s, int64_t M, int64_t N, int64_t K, Ope
       return run_parts_gemm<3, AMC, BMC>(g, partial, stream);
     }
   }
-  GemmArgs q = {};
-  q.M = static_cast<int>(M), q.N = static_cast<int>(N), q.K = static_cast<int>(K);
-  q.a = view(a.p, a.ld), q.b = view(b.p, b.ld);
-  q.c.p = c, q.c.ld = ldc, q.c.col_stride = cstep;
-  return product<T, AMC, BMC, OutT>(q, stream, partial, floats);
+  if constexpr (sizeof(T) == 4 && (AMC || BMC)) {
+    return hipErrorNotSupported;  // of a few classes dW alone is a product
+  } else {
+    GemmArgs q = {};
+    q.M = static_cast<int>(M), q.N = static_cast<int>(N), q.K = static_cast<int>(K);
+    q.a = view(a.p, a.ld), q.b = view(b.p, b.ld);
+    q.c.p = c, q.c.ld = ldc, q.c.col_stride = cstep;
+    return product<T, AMC, BMC, OutT>(q, stream, partial, floats);
+  }
 }
 
 template <typename T, typename G>

@@ -60,8 +60,8 @@ __device__ __forceinline__ int64_t rows_of(const Place<VE>& p, int64_t r0, int64
   return n > 0 ? (n + p.step - 1) / p.step : 0;
 }
 
-// The sum over `lanes` neighbouring threads (a power of two), in a fixed order, in the first
-// of them: exchanges within 16 without LDS.
+// The sum over `lanes` neighbouring threads (1 to 16, a power of two), in a fixed order:
+// exchanges within 16 lanes, without LDS.
 __device__ __forceinline__ float row_sum(float v, int lanes) {
   auto add = [&](auto ctrl) {
     v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
@@ -70,8 +70,6 @@ __device__ __forceinline__ float row_sum(float v, int lanes) {
   if (lanes > 2) add(std::integral_constant<int, 0x4e>{});    // pairs
   if (lanes > 4) add(std::integral_constant<int, 0x141>{});   // halves of 8
   if (lanes > 8) add(std::integral_constant<int, 0x140>{});   // halves of 16
-  if (lanes > 16) v += __shfl_down(v, 16, lanes);
-  if (lanes > 32) v += __shfl_down(v, 32, lanes);
   return v;
 }
 
