@@ -719,7 +719,7 @@ int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* g
 typedef struct {
   int32_t dtype;
   int32_t batch;          /* B: 1 .. 2^22 - 8 */
-  int32_t in_features;    /* K >= 1; output-major: up to 2^22 - 8 kept ones */
+  int32_t in_features;    /* K >= 1; output-major: up to 2^22 - 8 kept ones, input-major: 2^31 - 2^16 */
   int32_t classes;        /* V >= 1; input-major: up to 2^22 - 8 */
   const ard_row_plan* in_plan;  /* n == K (a list is not needed), or NULL = every input kept */
   int32_t weight_layout;  /* ARD_WEIGHTS_FULL or ARD_WEIGHTS_INPUT_MAJOR */

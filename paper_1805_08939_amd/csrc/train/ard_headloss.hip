@@ -766,6 +766,9 @@ unsigned sweep(int64_t n) { return static_cast<unsigned>(std::max<int64_t>(1, st
 // ------------------------------------------------------------------ host
 // Elements between the rows of the tile kernel's operands: offsets within a slab and a tile have 32 bits.
 constexpr int64_t kMostStride = int64_t{1} << 22;
+// Kept inputs: counted in 32 bits, rounded up to a tile or a slab (256) or to what the waves of head_few_kernel
+// take in a turn and load ahead (16 inputs, 4 shares, 16 waves, 7 turns: 7168).
+constexpr int32_t kMostKept = INT32_MAX - (1 << 16) + 1;
 
 int check_desc(const ard_headloss_desc* d, HeadShape* s) {
   if (!d) return fail(ARD_ERR_INVALID_ARG, "desc is NULL");
@@ -799,6 +802,8 @@ int check_desc(const ard_headloss_desc* d, HeadShape* s) {
 }
 
 int check_strides(const HeadShape& s) {
+  if (s.in.kept > kMostKept)
+    return fail(ARD_ERR_UNSUPPORTED, "%d kept inputs: at most 2^31 - 2^16", s.in.kept);
   if (s.ldp >= kMostStride || s.ldc >= kMostStride)
     return fail(ARD_ERR_UNSUPPORTED, "%d columns and rows of %lld weights must be below 2^22", s.B, static_cast<long long>(s.ldc));
   if ((s.V / 32 + int64_t{1}) * (s.B / 32 + int64_t{1}) >= int64_t{1} << 31)  // tiles are counted in 32 bits

@@ -421,3 +421,24 @@ def test_weights_past_2_31_elements(layout):
         assert ((got - want).abs() <= (3 * UBF + 1e-3) * (dz.abs() @ X.double().abs().T)).all()
         assert abs(float(db[at[i]]) - float(dz.sum())) <= 1e-3 * float(dz.abs().sum())
     assert told.max() < 0 and torch.isfinite(dX).all()
+
+
+# ---------------------------------------------------------------- index limits, on the CPU
+
+@pytest.mark.parametrize("dtype", [api.ARD_F32, api.ARD_BF16])
+@pytest.mark.parametrize("classes", [10, 40])
+def test_kept_inputs_of_input_major_weights_stay_in_32_bits(dtype, classes):
+    """The kernels round the kept inputs up to their loops' steps in 32 bits: at most 2^31 - 2^16 of them."""
+    a = 4096  # never read
+    most = 2 ** 31 - 2 ** 16
+
+    def desc(k, plan=None):
+        return api.headloss_desc(dtype, 1, k, classes, plan, INPUT)
+    assert api.ard_headloss_workspace_bytes(desc(most)) > 0
+    assert api.ard_headloss_workspace_bytes(desc(2 ** 31 - 1, api.ard_plan_rows(2 ** 31 - 1, 2, 0, None))) > 0
+    for k in (most + 1, 2 ** 31 - 3100, 2 ** 31 - 1):
+        assert api.ard_headloss_workspace_bytes(desc(k)) == 0
+        for call, n in ((api.ard_headloss_fwd, 6), (api.ard_headloss_bwd, 9)):
+            with pytest.raises(api.ArdError) as e:
+                call(desc(k), *(a * (i + 1) for i in range(n)), (a * 16, 1 << 60), stream=0)
+            assert e.value.status == 2 and "kept inputs" in e.value.message
