@@ -486,8 +486,9 @@ int plan_norm(const ard_rmsnorm_desc* d, NormPlan* p) {
     const int64_t step = kRange / s.lanes;
     const int64_t most_ranges = (s.K + 2 * step - 1) / (2 * step), want = (4 * kTargetBlocks + s.blocks - 1) / s.blocks;
     s.ranges = static_cast<int32_t>(std::max<int64_t>(1, std::min(most_ranges, want)));
-    s.rows = static_cast<int32_t>((s.K + s.ranges - 1) / s.ranges);
-    s.ranges = (s.K + s.rows - 1) / s.rows;
+    const int64_t rows = s.K;
+    s.rows = static_cast<int32_t>((rows + s.ranges - 1) / s.ranges);
+    s.ranges = static_cast<int32_t>((rows + s.rows - 1) / s.rows);
   }
   return ARD_OK;
 }

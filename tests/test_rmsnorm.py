@@ -284,3 +284,39 @@ def test_more_than_2_31_elements():
         assert ((Y[:, at:at + 64].double() - want).abs() <= (UBF + 7 * U) * want.abs()).all()
     api.ard_rmsnorm_bwd(desc, X, None, inv, Y, None, Y, dg, ws)
     assert torch.isfinite(dg).all() and torch.isfinite(Y[:, -64:]).all()
+
+
+# ---------------------------------------------------------------- index limits, on the CPU
+
+@pytest.mark.parametrize("dtype", [api.ARD_F32, api.ARD_BF16])
+@pytest.mark.parametrize("batch", [1, 7, 64])
+def test_plans_of_the_most_features(dtype, batch):
+    """Up to 64 columns make one block of at most 1024 ranges of rows: 8 bytes of sums a range and column."""
+    for features in (2 ** 31 - 1, 2 ** 31 - 2 ** 20, 2 ** 30 + 1):
+        nbytes = api.ard_rmsnorm_workspace_bytes(api.rmsnorm_desc(dtype, batch, features))
+        assert 512 * batch * 8 < nbytes <= 1024 * batch * 8 + 255
+
+
+@pytest.mark.gpu
+def test_most_features():
+    from gpu_util import device, workspace
+    dev, K, eps = device(), 2 ** 31 - 1, float(np.float32(1e-5))
+    desc = api.rmsnorm_desc(api.ARD_BF16, 1, K)
+    ws = workspace(api.ard_rmsnorm_workspace_bytes(desc))
+    X, D = (torch.empty(K, 1, dtype=torch.bfloat16, device=dev).uniform_(-2, 2) for _ in range(2))
+    Y, inv, dX, dg = torch.empty_like(X), torch.empty(1, device=dev), torch.empty_like(X), torch.empty(K, device=dev)
+    api.ard_rmsnorm_fwd(desc, X, None, None, None, Y, inv, ws)
+    squares = sum(float(x.double().square().sum()) for x in X.split(2 ** 27))
+    i = 1.0 / np.sqrt(squares / K + eps)
+    assert abs(float(inv[0]) - i) <= 3 * U * i
+    api.ard_rmsnorm_bwd(desc, X, None, inv, D, None, dX, dg, ws)
+    # u xh has 3 u; the mean is rounded once more
+    mean = sum(float((x.double() * d.double()).sum()) for x, d in zip(X.split(2 ** 27), D.split(2 ** 27))) * i / K
+    size = sum(float((x.double() * d.double()).abs().sum()) for x, d in zip(X.split(2 ** 27), D.split(2 ** 27))) * i / K
+    for at in (0, 2 ** 30 - 32, 2 ** 31 - 2 ** 21 - 32, K - 64):
+        x, d = X[at:at + 64].double(), D[at:at + 64].double()
+        assert ((Y[at:at + 64].double() - x * i).abs() <= (UBF + 7 * U) * (x * i).abs()).all()
+        want, bound = i * (d - x * i * mean), i * (7 * U * d.abs() + (x * i).abs() * 11 * U * size)
+        assert ((dX[at:at + 64].double() - want).abs() <= bound + UBF * (want.abs() + bound)).all()
+        want = (d * x * i)[:, 0]
+        assert ((dg[at:at + 64].double() - want).abs() <= 6 * U * want.abs()).all()
