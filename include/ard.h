@@ -675,7 +675,7 @@ int ard_linattn_step(const ard_linattn_desc* desc, const void* Qt, const void* K
 typedef struct {
   int32_t dtype;
   int32_t batch;     /* B >= 1 */
-  int32_t features;  /* K >= 1 */
+  int32_t features;  /* K >= 1; bwd with dgain and more than 64 columns: below 2^30 - 2^17 */
   float eps;         /* >= 0 */
 } ard_rmsnorm_desc;
 

@@ -523,9 +523,12 @@ int fwd_impl(const NormPlan& p, const void* X, const void* R, const float* gain,
   return p.vec ? run_fwd<T, 16 / sizeof(T)>(p, a, stream) : run_fwd<T, 1>(p, a, stream);
 }
 
+// Workgroups that join dgain from several blocks of columns.
+int64_t join_groups(const NormPlan& p) { return p.s.blocks > 1 ? (static_cast<int64_t>(p.s.K) + kGain - 1) / kGain : 0; }
+
 template <typename T, int VE>
 int run_bwd(const NormPlan& p, const BwdArgs<T>& a, hipStream_t stream) {
-  const unsigned join = a.dgain && a.gpart ? static_cast<unsigned>((static_cast<int64_t>(p.s.K) + kGain - 1) / kGain) : 0;
+  const unsigned join = a.dgain ? static_cast<unsigned>(join_groups(p)) : 0;
   if (p.whole) {
     hipLaunchKernelGGL((norm_bwd_whole_kernel<T, VE>), block_grid(p.s.blocks), dim3(kWhole), 0, stream, a);
     ARD_LAUNCH_CHECK();
@@ -594,6 +597,9 @@ int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* g
       (st = need_ptr(dYt, "dYt")) || (st = may_ptr(dSt, "dSt")) || (st = may_ptr(dXt, "dXt")) ||
       (st = may_ptr(dgain, "dgain")) || (st = check_space(sp.part + sp.gain, ws, ws_bytes)))
     return st;
+  // the threads of a launch stay below 2^32
+  if (dgain && (join_groups(p) + (p.whole ? 0 : static_cast<int64_t>(p.s.blocks) * p.s.ranges)) * kRange >= int64_t{1} << 32)
+    return fail(ARD_ERR_UNSUPPORTED, "dgain of %d features in %d columns: too many features", p.s.K, p.s.B);
   if (dgain && dgain == gain) return fail(ARD_ERR_INVALID_ARG, "dgain and gain are the same buffer");
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);

@@ -320,3 +320,12 @@ def test_most_features():
         assert ((dX[at:at + 64].double() - want).abs() <= bound + UBF * (want.abs() + bound)).all()
         want = (d * x * i)[:, 0]
         assert ((dg[at:at + 64].double() - want).abs() <= 6 * U * want.abs()).all()
+
+
+def test_refuses_more_sums_of_the_gain_than_a_launch_takes():
+    """dgain of several blocks of columns is joined by a workgroup of 256 threads for 64 features: below 2^32 threads."""
+    args = [4096 * (i + 1) for i in range(7)]  # never read
+    d = api.rmsnorm_desc(api.ARD_BF16, 65, 2 ** 30)
+    with pytest.raises(api.ArdError) as e:
+        api.ard_rmsnorm_bwd(d, *args, (1 << 20, 1 << 60), stream=0)
+    assert e.value.status == 2 and "features" in e.value.message
