@@ -669,8 +669,9 @@ int ard_linattn_step(const ard_linattn_desc* desc, const void* Qt, const void* K
  * with u = gain dY and xh = s inv:
  *   dX = dS + inv (u - xh mean_k(u xh)),  dgain_k = sum_b dY_k xh_k
  * dSt (NULL = 0) is the gradient that reaches s past the norm; dX is that of x
- * and of r. dXt and dgain may be NULL. Outputs may be inputs of the same shape
- * (the same buffer, whole), but St is not Yt and dgain not gain.
+ * and of r. dXt and dgain may be NULL. St, Yt and dXt may be inputs of the same
+ * shape (the same buffer, whole), but St is not Yt; inv_rms of the forward and
+ * dgain share memory with no other argument.
  */
 typedef struct {
   int32_t dtype;

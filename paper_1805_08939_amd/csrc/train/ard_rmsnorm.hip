@@ -580,6 +580,9 @@ int ard_rmsnorm_fwd(const ard_rmsnorm_desc* desc, const void* Xt, const void* Rt
       (st = check_space(norm_space(p).part, ws, ws_bytes)))
     return st;
   if (St == Yt) return fail(ARD_ERR_INVALID_ARG, "St and Yt are the same buffer");
+  // written by one workgroup while others read what they normalise and the gain
+  if (same_buffer(inv_rms, {Xt, Rt, gain, St, Yt}))
+    return fail(ARD_ERR_INVALID_ARG, "inv_rms is in the buffer of another argument");
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
   return desc->dtype == ARD_BF16 ? fwd_impl<bf16>(p, Xt, Rt, gain, St, Yt, inv_rms, w, sm)
@@ -600,7 +603,9 @@ int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* g
   // the threads of a launch stay below 2^32
   if (dgain && (join_groups(p) + (p.whole ? 0 : static_cast<int64_t>(p.s.blocks) * p.s.ranges)) * kRange >= int64_t{1} << 32)
     return fail(ARD_ERR_UNSUPPORTED, "dgain of %d features in %d columns: too many features", p.s.K, p.s.B);
-  if (dgain && dgain == gain) return fail(ARD_ERR_INVALID_ARG, "dgain and gain are the same buffer");
+  // written by the sums' pass, in front of the one that reads the other arrays again
+  if (same_buffer(dgain, {St, gain, inv_rms, dYt, dSt, dXt}))
+    return fail(ARD_ERR_INVALID_ARG, "dgain is in the buffer of another argument");
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
   return desc->dtype == ARD_BF16 ? bwd_impl<bf16>(p, St, gain, inv_rms, dYt, dSt, dXt, dgain, w, sm)

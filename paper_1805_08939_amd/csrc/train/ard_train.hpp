@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "../ard_gemm_fast.hpp"
 #include "../ard_internal.hpp"
@@ -27,6 +28,11 @@ inline int check_space(size_t need, const void* ws, size_t ws_bytes) {
     return fail(ARD_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : 0);
   if (!aligned16(ws)) return fail(ARD_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
   return ARD_OK;
+}
+
+// Whether an output starts where one of these arguments does.
+inline bool same_buffer(const void* out, std::initializer_list<const void*> others) {
+  return out && std::find(others.begin(), others.end(), out) != others.end();
 }
 
 inline size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }

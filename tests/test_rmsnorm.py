@@ -329,3 +329,23 @@ def test_refuses_more_sums_of_the_gain_than_a_launch_takes():
     with pytest.raises(api.ArdError) as e:
         api.ard_rmsnorm_bwd(d, *args, (1 << 20, 1 << 60), stream=0)
     assert e.value.status == 2 and "features" in e.value.message
+
+
+# ---------------------------------------------------------------- buffers, on the CPU
+
+@pytest.mark.parametrize("dtype,batch,features", [(api.ARD_F32, 64, 64), (api.ARD_BF16, 64, 64), (api.ARD_F32, 1, 600),
+                                                  (api.ARD_F32, 600, 1), (api.ARD_BF16, 2048, 8192)])
+def test_refuses_sums_in_the_buffers_of_other_arguments(dtype, batch, features):
+    """inv_rms and dgain are written while other workgroups still read every other array."""
+    d = api.rmsnorm_desc(dtype, batch, features)
+    space = (1 << 20, 1 << 60)
+
+    def refused(call, args, at, name):
+        for i in range(len(args)):
+            if i == at:
+                continue
+            with pytest.raises(api.ArdError) as e:
+                call(d, *(args[i] if j == at else x for j, x in enumerate(args)), space, stream=0)
+            assert e.value.status == 1 and name in e.value.message and "buffer" in e.value.message
+    refused(api.ard_rmsnorm_fwd, [4096 * (i + 1) for i in range(6)], 5, "inv_rms")
+    refused(api.ard_rmsnorm_bwd, [4096 * (i + 1) for i in range(7)], 6, "dgain")
