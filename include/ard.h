@@ -712,10 +712,10 @@ int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* g
  * operands an infinite value in Xt or W makes NaN where it is multiplied, and values
  * of Xt, W and dz below 2^-108 are kept to 2^-126 and not to 2^-24 of themselves
  * (with more than 32 classes).
+ * Outputs share no memory with any other argument.
  * fwd: stats[2][B] (may be NULL) is kept for the backward.
- * bwd: dloss NULL = 1; dXt, dW and dbias may be NULL and share no memory with an
- * input. dW is of grad_dtype: ARD_F32, as ard_fc_sgd_momentum and ard_fc_muon read
- * it, or dtype.
+ * bwd: dloss NULL = 1; dXt, dW and dbias may be NULL. dW is of grad_dtype:
+ * ARD_F32, as ard_fc_sgd_momentum and ard_fc_muon read it, or dtype.
  */
 typedef struct {
   int32_t dtype;

@@ -1200,6 +1200,9 @@ int ard_headloss_fwd(const ard_headloss_desc* desc, const void* Xt, const void* 
       (st = need_ptr(labels, "labels")) || (st = need_ptr(loss, "loss")) || (st = may_ptr(stats, "stats")) ||
       (st = check_space(space_bytes(desc, s), ws, ws_bytes)))
     return st;
+  // written by one workgroup while others read the inputs
+  if (same_buffer(loss, {Xt, W, bias, labels, stats}) || same_buffer(stats, {Xt, W, bias, labels}))
+    return fail(ARD_ERR_INVALID_ARG, "loss or stats is in the buffer of another argument");
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
   return desc->dtype == ARD_BF16 ? fwd_impl<bf16>(s, Xt, W, bias, labels, loss, stats, w, sm)
@@ -1218,8 +1221,9 @@ int ard_headloss_bwd(const ard_headloss_desc* desc, const void* Xt, const void* 
       (st = may_ptr(dXt, "dXt")) || (st = may_ptr(dW, "dW")) || (st = may_ptr(dbias, "dbias")) ||
       (st = check_space(space_bytes(desc, s), ws, ws_bytes)))
     return st;
-  if (dXt == Xt || dW == W || (dbias && (dbias == bias || dbias == dloss)))
-    return fail(ARD_ERR_INVALID_ARG, "a gradient is in the buffer of an input");
+  if (same_buffer(dXt, {Xt, W, bias, labels, stats, dloss, dW, dbias}) || same_buffer(dW, {Xt, W, bias, labels, stats, dloss, dbias}) ||
+      same_buffer(dbias, {Xt, W, bias, labels, stats, dloss}))
+    return fail(ARD_ERR_INVALID_ARG, "a gradient is in the buffer of another argument");
   hipStream_t sm = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
   if (desc->dtype == ARD_F32)

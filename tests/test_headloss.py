@@ -442,3 +442,19 @@ def test_kept_inputs_of_input_major_weights_stay_in_32_bits(dtype, classes):
             with pytest.raises(api.ArdError) as e:
                 call(desc(k), *(a * (i + 1) for i in range(n)), (a * 16, 1 << 60), stream=0)
             assert e.value.status == 2 and "kept inputs" in e.value.message
+
+
+# ---------------------------------------------------------------- buffers, on the CPU
+
+@pytest.mark.parametrize("classes", [6, 600])
+def test_refuses_outputs_in_the_buffers_of_other_arguments(classes):
+    """As many columns as classes give loss and bias one shape: a workgroup would write what others still read."""
+    d = api.headloss_desc(api.ARD_F32, classes, 8, classes)
+    for call, n, outs in ((api.ard_headloss_fwd, 6, (4, 5)), (api.ard_headloss_bwd, 9, (6, 7, 8))):
+        args = [4096 * (i + 1) for i in range(n)]
+        for out in outs:
+            for i in range(n):
+                if i != out:
+                    with pytest.raises(api.ArdError) as e:
+                        call(d, *(args[i] if j == out else x for j, x in enumerate(args)), (1 << 20, 1 << 60), stream=0)
+                    assert e.value.status == 1 and "buffer" in e.value.message
