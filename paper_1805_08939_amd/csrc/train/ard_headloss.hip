@@ -11,8 +11,8 @@
 // bf16 operands are read in place where their rows start on 16 bytes, else from copies.
 // fp32 operands, dz among them, are copied into three bf16 parts (ard_parts_gemm.hpp):
 // exact to 2^-24 and, with six bf16 products for one, still faster than fp32 products (8800
-// classes of 750 inputs, batch 700, forward and backward: 418 to 280 us). A part cannot hold
-// what fp32 rounds past the largest bf16 number: an infinite W or X makes NaN in its sums.
+// classes of 750 inputs, batch 700, forward and backward: 418 to 280 us). The rest of an
+// infinite value is NaN: an infinite W or X makes NaN in its sums.
 // A few classes take a kernel of their own (head_few_kernel) without any copy.
 //
 // Columns without a label contribute nothing: their loss and dz are 0, and the inputs that

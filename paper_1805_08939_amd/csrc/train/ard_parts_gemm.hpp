@@ -60,11 +60,15 @@ struct PartsCfg : FastCfg<bf16, BM_, BN_, BK_, STAGES_, WGM_, WGN_, KSPLIT_> {
   static constexpr int LDS = MAIN > ENDS ? MAIN : ENDS;
 };
 
+// The parts of a value. Of three, the first of a finite value that would round to infinity is
+// the largest bf16 number, and the others hold the rest as for any value.
 template <int PARTS>
 __device__ __forceinline__ void split_parts(float v, bf16 (&p)[PARTS]) {
 #pragma unroll
   for (int q = 0; q < PARTS; ++q) {
     p[q] = static_cast<bf16>(v);
+    if (PARTS == 3 && q == 0 && fabsf(v) >= 0x1.ffp127f)  // an infinite one stays infinite
+      p[0] = __builtin_bit_cast(bf16, static_cast<uint16_t>(__float_as_uint(v) >> 16));
     if (q + 1 < PARTS) v -= static_cast<float>(p[q]);
   }
 }

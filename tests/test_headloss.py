@@ -458,3 +458,47 @@ def test_refuses_outputs_in_the_buffers_of_other_arguments(classes):
                     with pytest.raises(api.ArdError) as e:
                         call(d, *(args[i] if j == out else x for j, x in enumerate(args)), (1 << 20, 1 << 60), stream=0)
                     assert e.value.status == 1 and "buffer" in e.value.message
+
+
+# ---------------------------------------------------------------- values next to the largest
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,K,V", [(8, 40, 10), (33, 65, 70), (700, 100, 3000), (703, 500, 6001), (1500, 400, 2000)])
+def test_fp32_operands_past_the_largest_bf16_number(B, K, V):
+    """3.4e38 is finite in fp32 and rounds to infinity in bf16; so do weights and inputs of it, and dz."""
+    from gpu_util import device, workspace
+    dev = device()
+    gen = torch.Generator(device=dev).manual_seed(B + V)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=dev)  # noqa: E731
+    big = float(np.float32(3.4e38))
+    assert torch.isinf(torch.tensor(big).bfloat16()) and torch.isfinite(torch.tensor(big))
+    desc = api.headloss_desc(api.ARD_F32, B, K, V)
+    ws = workspace(api.ard_headloss_workspace_bytes(desc))
+    labels = torch.randint(0, V, (B,), generator=gen, device=dev, dtype=torch.int32)
+    sign = torch.tensor([1.0, -1.0, 1.0, -1.0], device=dev)
+    tiny = lambda *s: (1 + rand(*s).abs()).bfloat16().float()  # noqa: E731  one part of a product, above 2^-126
+    for which in ("W", "X", "dloss"):
+        W, X, b, dl = rand(V, K) / K ** 0.5, rand(K, B), rand(V), rand(B).clamp(-0.9, 0.9)
+        rows = torch.arange(4, device=dev)
+        if which == "W":     # four weights, each alone on its input, whose values are small
+            W[:, :4] = 0
+            W[2 * rows, rows], X[:4] = big * sign, 2.0 ** -120 * tiny(4, B)
+        elif which == "X":
+            X[rows, rows], W[:, :4] = big * sign, 2.0 ** -122 * tiny(V, 4)
+        else:                # dz of the label is all of dloss
+            dl[3], b[labels[3].long()] = big, -40.0
+            X *= 2.0 ** -4
+        loss, stats = torch.empty(B, device=dev), torch.empty(2, B, device=dev)
+        dX, dW, db = torch.empty_like(X), torch.empty_like(W), torch.empty(V, device=dev)
+        api.ard_headloss_fwd(desc, X, W, b, labels, loss, stats, ws)
+        api.ard_headloss_bwd(desc, X, W, b, labels, stats, dl, dX, dW, db, ws)
+        X, W = X.double(), W.double()
+        want, eloss, dz, edz = _reference(X, W, b.double(), labels.long(), dl.double())
+        edz = edz + 2.0 ** -126  # what parts hold
+        _inside(loss, want, eloss, which + ": loss")
+        _inside(db, dz.sum(1), edz.sum(1) + B * U * dz.abs().sum(1), which + ": dbias")
+        # of each term six products, each lost below 2^-126
+        want, bound = W.T @ dz, W.abs().T @ (edz + (V + 2) * U * dz.abs()) + (6 * V + 1) * 2.0 ** -126
+        _inside(dX, want, bound + U * (want.abs() + bound), which + ": dX")
+        want, bound = dz @ X.T, (edz + (B + 2) * U * dz.abs()) @ X.abs().T + (6 * B + 1) * 2.0 ** -126
+        _inside(dW, want, bound + U * (want.abs() + bound), which + ": dW")
