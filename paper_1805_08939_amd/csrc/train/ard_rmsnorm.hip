@@ -230,10 +230,12 @@ __global__ void __launch_bounds__(kRange) norm_fwd_sums_kernel(FwdArgs<T> a) {
 
 // The sum of n values `step` apart, of the last index of which this thread's is `part` of
 // `parts`: eight loads in flight, the threads' shares added in their order by the first of them.
-// red: parts x cols values of the workgroup; every thread of it calls.
+// In 64 bits: a norm of heads has millions of blocks of columns, and a chain of equal ones in 32
+// was up to 1.5e-3 off. red: parts x cols values of the workgroup; every thread of it calls.
 template <typename V>
-__device__ __forceinline__ V share_sum(const V* from, bool on, int n, int64_t step, int col, int cols, int part, int parts, V* red) {
-  V v = 0;
+__device__ __forceinline__ double share_sum(const V* from, bool on, int n, int64_t step, int col, int cols, int part, int parts,
+                                            double* red) {
+  double v = 0.0;
   if (on && part < parts) {
 #pragma unroll 8
     for (int q = part; q < n; q += parts) v += from[q * step];
@@ -421,11 +423,11 @@ __global__ void __launch_bounds__(kRange) norm_bwd_sums_kernel(BwdArgs<T> a) {
 constexpr int kGain = 64;
 template <typename T>
 __device__ __forceinline__ void join_gain(const BwdArgs<T>& a, int64_t group) {
-  __shared__ float red[kRange];
+  __shared__ double red[kRange];
   const int t = threadIdx.x, c = t % kGain;
   const int64_t k = group * kGain + c;
-  const float v = share_sum(a.gpart + k, k < a.s.K, a.s.blocks, a.s.K, c, kGain, t / kGain, kRange / kGain, red);
-  if (t < kGain && k < a.s.K) a.dgain[k] = v;
+  const double v = share_sum(a.gpart + k, k < a.s.K, a.s.blocks, a.s.K, c, kGain, t / kGain, kRange / kGain, red);
+  if (t < kGain && k < a.s.K) a.dgain[k] = static_cast<float>(v);
 }
 
 // The workgroups behind those of the rows join dgain.

@@ -349,3 +349,25 @@ def test_refuses_sums_in_the_buffers_of_other_arguments(dtype, batch, features):
             assert e.value.status == 1 and name in e.value.message and "buffer" in e.value.message
     refused(api.ard_rmsnorm_fwd, [4096 * (i + 1) for i in range(6)], 5, "inv_rms")
     refused(api.ard_rmsnorm_bwd, [4096 * (i + 1) for i in range(7)], 6, "dgain")
+
+
+# ---------------------------------------------------------------- many columns
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,B,K", [("bf16", 2 ** 23, 4), ("f32", 2 ** 23 + 5, 2), ("bf16", 2 ** 25, 1), ("bf16", 32000, 4000)])
+@pytest.mark.parametrize("equal", [True, False])
+def test_gradient_of_the_gain_over_many_columns(dtype, B, K, equal):
+    """The error does not grow with the columns, also where each of them adds the same. w = dY xh 3 u, 64 columns in fp32 at
+    most 7 and 4 u (eight of a thread and 16 threads), the join 64 bits wide, a rounding of the result."""
+    from gpu_util import ard_dtype, device, workspace
+    dev, st = device(), synth.storage_dtype(dtype)
+    desc = api.rmsnorm_desc(ard_dtype(dtype), B, K)
+    ws = workspace(api.ard_rmsnorm_workspace_bytes(desc))
+    S, D = torch.full((K, B), 1.5, dtype=st, device=dev), torch.full((K, B), 0.7, dtype=st, device=dev)
+    inv, dg = torch.full((B,), 0.6666, device=dev), torch.empty(K, device=dev)
+    if not equal:
+        S.uniform_(0.5, 2), D.uniform_(-0.1, 1), inv.uniform_(0.5, 1)
+    api.ard_rmsnorm_bwd(desc, S, None, inv, D, None, None, dg, ws)
+    for k in range(0, K, max(1, K // 8)):
+        w = S[k].double() * D[k].double() * inv.double()
+        assert abs(float(dg[k]) - float(w.sum())) <= 15 * U * float(w.abs().sum())
