@@ -480,7 +480,8 @@ __global__ void __launch_bounds__(256) head_add_kernel(float* __restrict__ all, 
 }
 
 // What is left behind the products: dbias from the parts of the tile columns, in their
-// order, and zeros in the rows of dropped inputs.
+// order, and zeros in the rows of dropped inputs. The parts are added in 64 bits: 2^21 equal
+// columns make up to 2^17 of them, whose chain in 32 was 1.4e-3 off.
 struct ClearJob {
   char* p;
   int64_t row_bytes;  // a multiple of 2
@@ -518,10 +519,10 @@ __global__ void __launch_bounds__(256) head_finish_kernel(FinishArgs g) {
   if (block < g.bias_groups) {
     const int64_t v = static_cast<int64_t>(block) * 256 + threadIdx.x;
     if (v >= g.classes) return;
-    float sum = 0.0f;
+    double sum = 0.0;
 #pragma unroll 8
     for (int q = 0; q < g.parts; ++q) sum += g.part[static_cast<int64_t>(q) * g.classes + v];
-    g.dbias[v] = sum;
+    g.dbias[v] = static_cast<float>(sum);
     return;
   }
   block -= g.bias_groups;

@@ -502,3 +502,26 @@ def test_fp32_operands_past_the_largest_bf16_number(B, K, V):
         _inside(dX, want, bound + U * (want.abs() + bound), which + ": dX")
         want, bound = dz @ X.T, (edz + (B + 2) * U * dz.abs()) @ X.abs().T + (6 * B + 1) * 2.0 ** -126
         _inside(dW, want, bound + U * (want.abs() + bound), which + ": dW")
+
+
+# ---------------------------------------------------------------- many columns
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,V", [("f32", 10), ("f32", 32), ("f32", 40), ("f32", 200), ("bf16", 40), ("bf16", 200)])
+def test_gradient_of_the_bias_over_many_columns(dtype, V):
+    """The error does not grow with the columns, also where each of them adds the same: up to 64 columns are added in fp32 one
+    after the other, their sums in 64 bits."""
+    from gpu_util import ard_dtype, device, workspace
+    dev, st, B, K = device(), synth.storage_dtype(dtype), 2 ** 21, 8
+    gen = torch.Generator(device=dev).manual_seed(V)
+    X = torch.full((K, B), 0.5, dtype=st, device=dev)
+    W = torch.randn(V, K, generator=gen, device=dev).to(st)
+    labels = torch.zeros(B, dtype=torch.int32, device=dev)
+    desc = api.headloss_desc(ard_dtype(dtype), B, K, V)
+    ws = workspace(api.ard_headloss_workspace_bytes(desc))
+    loss, stats, db = torch.empty(B, device=dev), torch.empty(2, B, device=dev), torch.empty(V, device=dev)
+    api.ard_headloss_fwd(desc, X, W, None, labels, loss, stats, ws)
+    api.ard_headloss_bwd(desc, X, W, None, labels, stats, None, None, None, db, ws)
+    one = torch.ones(1, dtype=torch.float64, device=dev)
+    _, _, dz, edz = _reference(X[:, :1].double(), W.double(), 0 * one.repeat(V), labels[:1].long(), one)
+    _inside(db, B * dz[:, 0], B * (edz[:, 0] + 66 * U * dz[:, 0].abs()), "dbias")
