@@ -444,6 +444,38 @@ def test_kept_inputs_of_input_major_weights_stay_in_32_bits(dtype, classes):
             assert e.value.status == 2 and "kept inputs" in e.value.message
 
 
+# ---------------------------------------------------------------- each argument, on the CPU
+
+FWD = ("Xt", "W", "bias", "labels", "loss", "stats")
+BWD = ("Xt", "W", "bias", "labels", "stats", "dloss", "dXt", "dW", "dbias")
+NEEDED = {"fwd": {"Xt", "W", "labels", "loss"}, "bwd": {"Xt", "W", "labels", "stats"}}
+
+
+@pytest.mark.parametrize("classes", [6, 600])
+@pytest.mark.parametrize("way", ["fwd", "bwd"])
+def test_refuses_each_argument_by_its_name(way, classes):
+    """Arguments at addresses of their own, one of them wrong: no other check stands in for its own."""
+    call, names = (api.ard_headloss_fwd, FWD) if way == "fwd" else (api.ard_headloss_bwd, BWD)
+    d = api.headloss_desc(api.ARD_F32, 4, 8, classes)
+    good, space = [4096 * (i + 1) for i in range(len(names))], (1 << 20, 1 << 40)
+
+    def refused(status, what, args, ws):
+        with pytest.raises(api.ArdError) as e:
+            call(d, *args, ws, stream=0)
+        assert e.value.status == status and what in e.value.message
+    for at, name in enumerate(names):
+        wrong = lambda x: [x if i == at else g for i, g in enumerate(good)]  # noqa: E731
+        for off in (2, 4, 8):
+            refused(1, name + " is not 16-byte aligned", wrong(good[at] + off), space)
+        if name in NEEDED[way]:
+            refused(1, name + " is NULL", wrong(None), space)
+    need = api.ard_headloss_workspace_bytes(d)
+    assert need > 0
+    refused(5, "workspace", good, None)
+    refused(5, "workspace", good, (1 << 20, need - 1))
+    refused(1, "workspace", good, ((1 << 20) + 8, need))
+
+
 # ---------------------------------------------------------------- buffers, on the CPU
 
 @pytest.mark.parametrize("classes", [6, 600])

@@ -331,6 +331,37 @@ def test_refuses_more_sums_of_the_gain_than_a_launch_takes():
     assert e.value.status == 2 and "features" in e.value.message
 
 
+# ---------------------------------------------------------------- each argument, on the CPU
+
+FWD = ("Xt", "Rt", "gain", "St", "Yt", "inv_rms")
+BWD = ("St", "gain", "inv_rms", "dYt", "dSt", "dXt", "dgain")
+NEEDED = {"fwd": {"Xt", "Yt"}, "bwd": {"St", "inv_rms", "dYt"}}
+
+
+@pytest.mark.parametrize("way", ["fwd", "bwd"])
+def test_refuses_each_argument_by_its_name(way):
+    """Arguments at addresses of their own, one of them wrong: no other check stands in for its own."""
+    call, names = (api.ard_rmsnorm_fwd, FWD) if way == "fwd" else (api.ard_rmsnorm_bwd, BWD)
+    d = api.rmsnorm_desc(api.ARD_BF16, 2048, 4096)
+    good, space = [4096 * (i + 1) for i in range(len(names))], (1 << 20, 1 << 40)
+
+    def refused(status, what, args, ws):
+        with pytest.raises(api.ArdError) as e:
+            call(d, *args, ws, stream=0)
+        assert e.value.status == status and what in e.value.message
+    for at, name in enumerate(names):
+        wrong = lambda x: [x if i == at else g for i, g in enumerate(good)]  # noqa: E731
+        for off in (2, 4, 8):
+            refused(1, name + " is not 16-byte aligned", wrong(good[at] + off), space)
+        if name in NEEDED[way]:
+            refused(1, name + " is NULL", wrong(None), space)
+    refused(5, "workspace", good, None)
+    refused(5, "workspace", good, (1 << 20, 16))
+    refused(1, "workspace", good, ((1 << 20) + 8, 1 << 40))
+    if way == "bwd":  # the forward needs none of dgain's part
+        refused(5, "workspace", good, (1 << 20, api.ard_rmsnorm_workspace_bytes(d) - 1))
+
+
 # ---------------------------------------------------------------- buffers, on the CPU
 
 @pytest.mark.parametrize("dtype,batch,features", [(api.ARD_F32, 64, 64), (api.ARD_BF16, 64, 64), (api.ARD_F32, 1, 600),
