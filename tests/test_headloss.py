@@ -557,3 +557,37 @@ def test_gradient_of_the_bias_over_many_columns(dtype, V):
     one = torch.ones(1, dtype=torch.float64, device=dev)
     _, _, dz, edz = _reference(X[:, :1].double(), W.double(), 0 * one.repeat(V), labels[:1].long(), one)
     _inside(db, B * dz[:, 0], B * (edz[:, 0] + 66 * U * dz[:, 0].abs()), "dbias")
+
+
+# ---------------------------------------------------------------- past 2^31 elements
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", [FULL, INPUT])
+def test_input_gradients_of_weights_past_2_31_elements(layout):
+    """dX against W^T dz in 64 bits; the labels' classes, all over the weights, carry most of it."""
+    from gpu_util import device, workspace
+    dev = device()
+    B, K, V = 16, 4096, 600_064
+    gen = torch.Generator(device=dev).manual_seed(3)
+    W = torch.empty((V, K) if layout == FULL else (K, V), dtype=torch.bfloat16, device=dev).uniform_(-0.05, 0.05, generator=gen)
+    X = torch.randn(K, B, generator=gen, device=dev).to(torch.bfloat16)
+    labels = torch.tensor([0, V - 1, V // 2, 2 ** 31 // K + 5, 2 ** 31 // K - 1, V - 65, 1, 2 ** 30 // K] * 2, dtype=torch.int32, device=dev)
+    desc = api.headloss_desc(api.ARD_BF16, B, K, V, None, layout)
+    ws = workspace(api.ard_headloss_workspace_bytes(desc))
+    loss, stats, dX = torch.empty(B, device=dev), torch.empty(2, B, device=dev), torch.empty_like(X)
+    api.ard_headloss_fwd(desc, X, W, None, labels, loss, stats, ws)
+    api.ard_headloss_bwd(desc, X, W, None, labels, stats, None, dX, None, None, ws)
+    chunks = torch.arange(V, device=dev).split(100_000)
+    rows = lambda v: (W[v[0]:v[-1] + 1] if layout == FULL else W[:, v[0]:v[-1] + 1].T.contiguous()).double()  # noqa: E731
+    total = sum(torch.exp(rows(v) @ X.double()).sum(0) for v in chunks)
+    # a logit: K terms of at most 0.05 |x|, a rounding each at worst; p: that twice, and the exponentials' 2^-17
+    ez = 2 * K * U * 0.05 * X.double().abs().sum(0) + 2.0 ** -17
+    want, bound = torch.zeros(K, B, dtype=torch.float64, device=dev), torch.zeros(K, B, dtype=torch.float64, device=dev)
+    for v in chunks:
+        w = rows(v)
+        p = torch.exp(w @ X.double()) / total
+        dz = p - (v[:, None] == labels[None].long()).double()
+        want += w.T.contiguous() @ dz
+        bound += w.abs().T.contiguous() @ (p * torch.expm1(ez) + (UBF + (V + 2) * U) * dz.abs())
+    assert ((dX.double() - want).abs() <= bound + UBF * (want.abs() + bound)).all()
+    assert (want.abs() > 4 * bound).float().mean() > 0.5  # the bound tells a wrong row from the right one

@@ -402,3 +402,37 @@ def test_gradient_of_the_gain_over_many_columns(dtype, B, K, equal):
     for k in range(0, K, max(1, K // 8)):
         w = S[k].double() * D[k].double() * inv.double()
         assert abs(float(dg[k]) - float(w.sum())) <= 15 * U * float(w.abs().sum())
+
+
+# ---------------------------------------------------------------- past 2^31 elements
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sparse", [False, True])
+def test_gradients_past_2_31_elements(sparse):
+    """dX in columns all over the arrays; dgain of every column and, with a dY of zeros elsewhere, of these columns alone."""
+    from gpu_util import device, workspace
+    dev, K, B = device(), 5, 460_000_009
+    desc = api.rmsnorm_desc(api.ARD_BF16, B, K)
+    ws = workspace(api.ard_rmsnorm_workspace_bytes(desc))
+    S, D = (torch.empty(K, B, dtype=torch.bfloat16, device=dev).uniform_(-2, 2) for _ in range(2))
+    inv, gain = torch.empty(B, device=dev).uniform_(0.5, 2), torch.empty(K, device=dev).uniform_(0.5, 2)
+    spans = [slice(at, at + 64) for at in (0, 12345, 2 ** 31 // K - 32, 2 ** 31 % B - 32, B - 64)]
+    if sparse:
+        kept = [D[:, c].clone() for c in spans]
+        D.zero_()
+        for c, d in zip(spans, kept):
+            D[:, c] = d
+    dX, dg = torch.full_like(S, float("nan")), torch.empty(K, device=dev)
+    api.ard_rmsnorm_bwd(desc, S, gain, inv, D, None, dX, dg, ws)
+    for c in spans:
+        s, d, i, g = S[:, c].double(), D[:, c].double(), inv[c].double(), gain.double()[:, None]
+        xh, u = s * i, g * d
+        want, bound = i * (u - xh * (u * xh).mean(0)), i * (7 * U * u.abs() + 11 * U * xh.abs() * (u * xh).abs().mean(0))
+        assert ((dX[:, c].double() - want).abs() <= bound + UBF * (want.abs() + bound)).all()
+    assert not any(torch.isnan(x).any() for row in dX for x in row.split(2 ** 28))
+    for k in range(K):
+        sums = [(w.sum(), w.abs().sum()) for w in (D[k, c].double() * S[k, c].double() * inv[c].double()
+                                                   for c in (spans if sparse else
+                                                             [slice(a, a + 2 ** 26) for a in range(0, B, 2 ** 26)]))]
+        # as over many columns above
+        assert abs(float(dg[k]) - sum(float(a) for a, _ in sums)) <= 15 * U * sum(float(b) for _, b in sums)
