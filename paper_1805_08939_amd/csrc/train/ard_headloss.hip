@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(Cfg::NT) head_tile_kernel(TileArgs g) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = from[e];
             const int64_t n = n0 + wn * Cfg::TN + ch * 8;
-            if (row < rows && n < g.ldp) store_parts<P>(static_cast<bf16*>(g.P) + (m0 + row) * g.ldp + n, g.pplane, v);
+            if (row < rows && n < g.ldp) store_parts<P, true>(static_cast<bf16*>(g.P) + (m0 + row) * g.ldp + n, g.pplane, v);
           }
           const float* half = reinterpret_cast<const float*>(region + lr * L::ROW) + lh * (Cfg::TN / 2);
           float sum = 0.0f;
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(Cfg::NT) head_tile_kernel(TileArgs g) {
         zt[row * ZLD + col] = p;
         if (n0 + col < g.ldp) {
           bf16 part[P > 0 ? P : 1];
-          split_parts(p, part);
+          split_parts<(P > 0 ? P : 1), true>(p, part);
 #pragma unroll
           for (int u = 0; u < (P > 0 ? P : 1); ++u)
             static_cast<bf16*>(g.P)[u * g.pplane + (m0 + row) * g.ldp + n0 + col] = part[u];
@@ -399,7 +399,7 @@ __device__ __forceinline__ void pack_one(const PackJob& j, int64_t r, int64_t c)
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     v[e] = e >= n || (j.classes > 0 && (l[e] < 0 || l[e] >= j.classes)) ? 0.0f : to_f32(x[e]);
-  store_parts<P>(static_cast<bf16*>(j.out) + r * j.ld + c, j.plane, v);
+  store_parts<P, true>(static_cast<bf16*>(j.out) + r * j.ld + c, j.plane, v);
 }
 // Chunks of a thread are in flight together, without a branch between them; a row's last,
 // partial one is read as the row's last eight values and moved down (bf16 4096 x 4096 with
@@ -451,7 +451,7 @@ __device__ __forceinline__ void pack_rows(const PackJob& j, int64_t block) {
       for (int by = 4; by > 0; by /= 2)
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = down & by ? (e + by < 8 ? v[e + by] : 0.0f) : v[e];
-      if (at + u * step < total) store_parts<P>(static_cast<bf16*>(j.out) + r[u] * j.ld + c[u], j.plane, v);
+      if (at + u * step < total) store_parts<P, true>(static_cast<bf16*>(j.out) + r[u] * j.ld + c[u], j.plane, v);
     }
   }
 }

@@ -60,14 +60,15 @@ struct PartsCfg : FastCfg<bf16, BM_, BN_, BK_, STAGES_, WGM_, WGN_, KSPLIT_> {
   static constexpr int LDS = MAIN > ENDS ? MAIN : ENDS;
 };
 
-// The parts of a value. Of three, the first of a finite value that would round to infinity is
-// the largest bf16 number, and the others hold the rest as for any value.
-template <int PARTS>
+// The parts of a value. ANY: of any finite one in three parts; where the first would round to
+// infinity it is the largest bf16 number, and the others hold the rest. (An iterate's values are
+// about 1 at most; the comparison would cost 512 x 784 in three parts 188 us for 186.)
+template <int PARTS, bool ANY = false>
 __device__ __forceinline__ void split_parts(float v, bf16 (&p)[PARTS]) {
 #pragma unroll
   for (int q = 0; q < PARTS; ++q) {
     p[q] = static_cast<bf16>(v);
-    if (PARTS == 3 && q == 0 && fabsf(v) >= 0x1.ffp127f)  // an infinite one stays infinite
+    if (ANY && PARTS == 3 && q == 0 && fabsf(v) >= 0x1.ffp127f)  // an infinite one stays infinite
       p[0] = __builtin_bit_cast(bf16, static_cast<uint16_t>(__float_as_uint(v) >> 16));
     if (q + 1 < PARTS) v -= static_cast<float>(p[q]);
   }
@@ -83,13 +84,13 @@ __device__ __forceinline__ void triangle_tile(int t, int& row, int& col) {
 }
 
 // Splits eight values and writes a chunk of each part.
-template <int PARTS>
+template <int PARTS, bool ANY = false>
 __device__ __forceinline__ void store_parts(bf16* out, int64_t plane, const float (&v)[8]) {
   bf16 w[PARTS][8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     bf16 p[PARTS];
-    split_parts<PARTS>(v[e], p);
+    split_parts<PARTS, ANY>(v[e], p);
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) w[q][e] = p[q];
   }
