@@ -661,8 +661,9 @@ int ard_linattn_step(const ard_linattn_desc* desc, const void* Qt, const void* K
  *   s = x + r,  inv = 1 / sqrt(mean_k s_k^2 + eps),  y_k = gain_k s_k inv
  * Layouts: Xt, Rt, St, Yt and the gradients [K][B] (dtype), gain and dgain [K]
  * fp32 (gain NULL = 1), inv_rms[B] fp32. s is taken in fp32, before it is
- * rounded into St; the sums over a column are 64 bits wide. A column that is
- * not finite affects no other; with eps = 0 one of zeros gives NaN.
+ * rounded into St; the sums over a column, and dgain's over blocks of 64
+ * columns, are 64 bits wide. A column that is not finite affects no other, but
+ * reaches dgain; with eps = 0 one of zeros gives NaN.
  * fwd: St (may be NULL) receives s, the residual stream of the next layer,
  * inv_rms (may be NULL) is kept for the backward.
  * bwd, from St (Xt where there was no Rt) and inv_rms as the forward left them,
@@ -714,7 +715,8 @@ int ard_rmsnorm_bwd(const ard_rmsnorm_desc* desc, const void* St, const float* g
  * (with more than 32 classes).
  * Outputs share no memory with any other argument.
  * fwd: stats[2][B] (may be NULL) is kept for the backward.
- * bwd: dloss NULL = 1; dXt, dW and dbias may be NULL. dW is of grad_dtype:
+ * bwd: dloss NULL = 1; dXt, dW and dbias may be NULL. dbias is summed over blocks
+ * of at most 64 columns in fp32, over the blocks in 64 bits. dW is of grad_dtype:
  * ARD_F32, as ard_fc_sgd_momentum and ard_fc_muon read it, or dtype.
  */
 typedef struct {
@@ -748,8 +750,10 @@ int ard_headloss_bwd(const ard_headloss_desc* desc, const void* Xt, const void* 
  *   X = U / (|U| + eps)  (Frobenius norm), then `iterations` times
  *   X = (a + b A + c A^2) X with A = X X^T,
  *   W = (1 - lr weight_decay) W - lr sqrt(max(1, kept outputs / kept inputs)) X
- * Each iteration maps the singular values s to a s + b s^3 + c s^5: with the
- * defaults those above a few thousandths end between 0.7 and 1.2 after five.
+ * Each iteration maps the singular values s to a s + b s^3 + c s^5 (the method,
+ * its coefficients and the step's scale are those of Jordan et al., "Muon: an
+ * optimizer for hidden layers in neural networks", 2024): with the defaults those
+ * above a few thousandths end between 0.7 and 1.2 after five.
  * The kept biases take momentum SGD with bias_lr: Vb = momentum Vb + dbias,
  * bias -= bias_lr Vb. What is dropped is frozen for the step. W, V and dW as
  * ard_fc_sgd_momentum takes them (FULL, COMPACT and COMPACT_GRAD: dW[N][K] or

@@ -11,7 +11,7 @@
 // bf16 operands are read in place where their rows start on 16 bytes, else from copies.
 // fp32 operands, dz among them, are copied into three bf16 parts (ard_parts_gemm.hpp):
 // exact to 2^-24 and, with six bf16 products for one, still faster than fp32 products (8800
-// classes of 750 inputs, batch 700, forward and backward: 418 to 280 us). The rest of an
+// classes of 750 inputs, batch 700, forward and backward: 418 to 287 us). The rest of an
 // infinite value is NaN: an infinite W or X makes NaN in its sums.
 // A few classes take a kernel of their own (head_few_kernel) without any copy.
 //
@@ -384,7 +384,7 @@ struct PackJob {
   int32_t classes;             // 0: no labels are looked at
   uint32_t groups;
 };
-// Any chunk, value by value where it is not whole.
+// A chunk value by value: of rows shorter than one, and of the kept columns of output-major weights, which lie apart.
 template <typename T, int P>
 __device__ __forceinline__ void pack_one(const PackJob& j, int64_t r, int64_t c) {
   const T* from = static_cast<const T*>(j.src) + r * j.row_step + c * j.col_step;
@@ -401,9 +401,11 @@ __device__ __forceinline__ void pack_one(const PackJob& j, int64_t r, int64_t c)
     v[e] = e >= n || (j.classes > 0 && (l[e] < 0 || l[e] >= j.classes)) ? 0.0f : to_f32(x[e]);
   store_parts<P, true>(static_cast<bf16*>(j.out) + r * j.ld + c, j.plane, v);
 }
-// Chunks of a thread are in flight together, without a branch between them; a row's last,
-// partial one is read as the row's last eight values and moved down (bf16 4096 x 4096 with
-// labels: 42 us one chunk after the other, 19).
+// Whole rows: chunks of a thread are in flight together, without a branch between them; a
+// row's last, partial one is read as the row's last eight values and moved down (bf16 4096 x
+// 4096 with labels: 42 us one chunk after the other, 19). Columns that lie apart are taken chunk
+// after chunk (pack_one): with every other of 1500 inputs kept, 8800 classes and batch 700 in
+// bf16 the loss takes 39.4 us, input-major, without a copy of the weights, 26.5.
 template <typename T, int P>
 __device__ __forceinline__ void pack_rows(const PackJob& j, int64_t block) {
   constexpr int U = P == 1 ? 4 : 2, E = 16 / static_cast<int>(sizeof(T)), H = 8 / E;

@@ -5,6 +5,8 @@
 //   W = (1 - lr decay) W - lr sqrt(max(1, outputs / inputs)) X
 // Each iteration applies the odd polynomial a s + b s^3 + c s^5 to the singular values of X
 // and leaves its singular vectors; |U| is the Frobenius norm, so that they start within 1.
+// Method, default coefficients and the step's scale: Jordan et al., "Muon: an optimizer for
+// hidden layers in neural networks", 2024.
 //
 // X, A and the polynomial are kept in bf16 parts (ard_parts_gemm.hpp): three for fp32 weights,
 // 2^-24 of a value; two for bf16 ones, 2^-16, where a step is then 2.5e-5 off and the weight

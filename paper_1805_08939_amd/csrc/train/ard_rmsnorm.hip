@@ -481,6 +481,10 @@ int plan_norm(const ard_rmsnorm_desc* d, NormPlan* p) {
   // Measured on MI355X, forward, up to 128 and 32 KB of a block in one workgroup: bf16 4544 x 9 36.6, 18.5 us, 1024 x 64
   // 15.5, 9.8, fp32 126 x 1632 7.2, 7.1; ranges of at least four and two rows of a thread: bf16 4544 x 9 18.5, 10.9, 631 x
   // 433 18.7, 11.6, 8192 x 2048 35.3, 34.9.
+  // More than 32704 columns always go to one workgroup a block: one launch whose threads stay below 2^32 whatever the
+  // batch. Against ranges, forward and backward: fp32 256 x 262144 256, 339 us, ranges 316, 368; 1024 x 65536 279, 292 and
+  // 299, 311; 1024 x 32768 151, 151 and 132, 146; bf16 512 x 131072 170, 201 and 157, 202; 1024 x 65536 168, 179 and 144,
+  // 172; 512 x 32768 42.0, 49.0 and 36.4, 44.2: fp32 0.81 to 1.14 times ranges' time, bf16 0.98 to 1.17.
   p->whole = bytes <= 32 << 10 || s.blocks >= 2 * kTargetBlocks;
   s.ranges = 1;
   s.rows = s.K;
